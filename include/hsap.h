@@ -700,6 +700,57 @@ hsap_status hsap_sum_parts(int32_t num_parts, const float* const* parts, int64_t
 hsap_status hsap_convert_f32_bf16(const float* src, void* dst, int64_t count, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Window attention with sinks -- the layers of a model whose attention is local: query i of a document that starts at
+ * start(i) attends key j iff
+ *   start(i) <= j <= i  and  (i - j < window  or  j - start(i) < sinks),
+ * i.e. the last `window` tokens up to itself and the document's first `sinks` tokens.  (Not in the paper, whose
+ * attention is full; such layers alternate with full ones over the same packed, sharded batch.)  Same descriptor,
+ * layouts and head rules as hsap_attn_fwd_fused / hsap_attn_bwd_bf16, without a plan: the kernels take the ranges
+ * from cu_seqlens, so block_m and block_n are not read and N need only be a multiple of P (ZIGZAG: 2P).
+ *
+ *   desc        N, P, layout, r, batch, heads, head_dim (64 or 128), softmax scale.
+ *   window      >= 1 (a query always sees itself); N or more: full causal attention.
+ *   sinks       >= 0.
+ *   q           device bf16 [n, Hq, d]: shard r's queries, local row order.
+ *   k, v        device bf16 [P, n, Hkv, d] sharded order; only rows that some query of the shard sees are read.
+ *   cu_seqlens  DEVICE int32 [num_docs + 1], 0 = cu[0] <= cu[1] <= ... <= cu[num_docs] <= B * N, a boundary at every
+ *               b * N (rules of hsap_plan; read by the kernels, so not checked).  Positions at or behind
+ *               cu[num_docs] are padding: their q, k, v rows are not read, their rows of every output not written.
+ *   q, k, v and d_o are finite in the rows of the documents.
+ * --------------------------------------------------------------------- */
+
+/*
+ * hsap_window_attn_fwd -- output and log-sum-exp of the shard's queries.
+ *   o_out    device bf16 [n, Hq, d], 8-byte aligned (rounded to nearest even once).
+ *   lse_out  device fp32 [Hq, n].
+ * q, k, v 16-byte aligned.  One launch on `stream`; no workspace.
+ */
+hsap_status hsap_window_attn_fwd(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const void* q,
+                                 const void* k, const void* v, const int32_t* cu_seqlens, int32_t num_docs,
+                                 void* o_out, float* lse_out, void* hip_stream);
+
+/* Bytes of device workspace hsap_window_attn_bwd needs (host); -1 for invalid arguments. */
+int64_t hsap_window_attn_bwd_workspace(const hsap_attn_desc* desc, int32_t window, int32_t sinks);
+
+/*
+ * hsap_window_attn_bwd -- gradients of hsap_window_attn_fwd.
+ *   q, k, v, cu_seqlens, num_docs  as for the forward; d_o, o device bf16 [n, Hq, d] (o: the forward's output), lse
+ *               device fp32 [Hq, n] (the forward's).
+ *   dq          device bf16 [n, Hq, d].
+ *   dk, dv      device [P, n, Hkv, d] sharded order, bf16 (dkv_f32 = 0) or fp32 (dkv_f32 != 0, e.g. to be summed over
+ *               the shards): what this shard's queries give every key, summed over the query heads of its K/V head;
+ *               0 for a key that none of them sees.  Every row of the documents is written (not accumulated).
+ *   workspace   device, 16-byte aligned, at least hsap_window_attn_bwd_workspace bytes (workspace_bytes: its size);
+ *               contents on entry ignored.  Calls that overlap in time need workspaces of their own.
+ * sinks <= 128 wherever window < N, else HSAP_ERR_UNSUPPORTED.  Two to four launches on `stream`; no atomics: the same
+ * inputs give the same bits.
+ */
+hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const void* q,
+                                 const void* k, const void* v, const void* d_o, const void* o, const float* lse,
+                                 const int32_t* cu_seqlens, int32_t num_docs, void* dq, void* dk, void* dv,
+                                 int32_t dkv_f32, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Step executor -- the library's runtime for one shard geometry: each packed
  * batch is planned on the host and run with one call per stage.  Not in the
  * paper; it sequences the entry points above the way a training step uses

@@ -42,8 +42,11 @@ What it computes, with the passages it follows (HSAP paper, arxiv 2606.30460):
   instruction set: q, kv, o, dq, dkv, do messages), arranged in stages with
   matched sends and receives.
 
-Parity status: every function above is pinned by ``tests/test_oracle_pins.py``
-against brute force, closed forms, library routines or invariants; none is
+* ``window`` -- window attention with sinks over the packed documents (an extension beyond the paper's full
+  attention), with derived error bounds.
+
+Parity status: every function above is pinned by ``tests/test_oracle_pins.py`` (``window``:
+``tests/test_window_oracle.py``) against brute force, closed forms, library routines or invariants; none is
 "parity unpinned".
 """
 from .attention import (  # noqa: F401
@@ -66,3 +69,4 @@ from .balance import load_matrix, q_transfer_balance  # noqa: F401
 from .schedule import backward_program, forward_program  # noqa: F401
 from .batch import batch_plan_shard, batch_shard_backward, batch_shard_forward, split_batch  # noqa: F401
 from .fp8 import decode_fp8, dequantize_fp8, quantize_fp8  # noqa: F401
+from .window import window_allowed, window_attention  # noqa: F401

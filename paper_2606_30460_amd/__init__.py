@@ -33,4 +33,7 @@ from ._lib import (  # noqa: F401
     plan_runs,
     shard_desc,
     shard_gather,
+    window_attn_bwd,
+    window_attn_bwd_workspace,
+    window_attn_fwd,
 )

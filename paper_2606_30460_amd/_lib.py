@@ -42,6 +42,7 @@ EXPORTED = (
     "hsap_partial_attn_bwd_runs", "hsap_attn_bwd_bf16", "hsap_sum_parts", "hsap_convert_f32_bf16", "hsap_executor_create", "hsap_executor_destroy",
     "hsap_executor_plan", "hsap_executor_info", "hsap_executor_forward", "hsap_executor_partial_forward",
     "hsap_executor_merge", "hsap_executor_backward",
+    "hsap_window_attn_fwd", "hsap_window_attn_bwd_workspace", "hsap_window_attn_bwd",
 )
 
 EXEC_BACKWARD = 1
@@ -127,6 +128,10 @@ _SIG = {
     "hsap_executor_partial_forward": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P]),
     "hsap_executor_merge": (ctypes.c_int, [_P, _P, _P, _P]),
     "hsap_executor_backward": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "hsap_window_attn_fwd": (ctypes.c_int, [_P, _I32, _I32, _P, _P, _P, _P, _I32, _P, _P, _P]),
+    "hsap_window_attn_bwd_workspace": (ctypes.c_int64, [_P, _I32, _I32]),
+    "hsap_window_attn_bwd": (ctypes.c_int, [_P, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _I32, _P, _I64,
+                                            _P]),
 }
 
 
@@ -658,6 +663,80 @@ def convert_f32_bf16(src, dst, stream=None) -> None:
     _dev(src, "float32", "src")
     _dev(dst, "bfloat16", "dst", src.numel())
     _check(lib().hsap_convert_f32_bf16(_ptr(src), _ptr(dst), src.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# window attention with sinks
+# ---------------------------------------------------------------------------
+
+MAX_WINDOW = 2 ** 31 - 1  # a window that ends nothing
+
+
+def _one_device(*tensors) -> None:
+    """Every tensor on the current device (the stream and the launch are that device's)."""
+    here = _torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError("tensor on cuda:%d, but cuda:%d is the current device" % (t.device.index, here))
+
+
+def _extent(value: int, what: str) -> int:
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError("%s %d outside 32 bits" % (what, value))
+    return value
+
+
+def window_attn_fwd(desc: AttnDesc, window: int, sinks: int, q, k, v, cu_seqlens_dev, o_out, lse_out,
+                    stream=None) -> None:
+    """hsap_window_attn_fwd: q bf16 [n, Hq, d] against k / v bf16 [P, n, Hkv, d] through a window of ``window`` tokens
+    and the first ``sinks`` tokens of each document (cu_seqlens_dev int32 [num_docs + 1] on the device) -> o_out bf16
+    [n, Hq, d], lse_out fp32 [Hq, n]."""
+    s = desc.shard
+    n = s.rows
+    hq, hkv, d, P = desc.heads_q, desc.heads_kv, desc.head_dim, s.sp_degree
+    _dev(q, "bfloat16", "q", n * hq * d)
+    _dev(k, "bfloat16", "k", P * n * hkv * d)
+    _dev(v, "bfloat16", "v", P * n * hkv * d)
+    _dev(cu_seqlens_dev, "int32", "cu_seqlens")
+    _dev(o_out, "bfloat16", "o_out", n * hq * d)
+    _dev(lse_out, "float32", "lse_out", hq * n)
+    _one_device(q, k, v, cu_seqlens_dev, o_out, lse_out)
+    _check(lib().hsap_window_attn_fwd(ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q),
+                                      _ptr(k), _ptr(v), _ptr(cu_seqlens_dev), cu_seqlens_dev.numel() - 1, _ptr(o_out),
+                                      _ptr(lse_out), _stream(stream)))
+
+
+def window_attn_bwd_workspace(desc: AttnDesc, window: int, sinks: int) -> int:
+    """hsap_window_attn_bwd_workspace: bytes of workspace window_attn_bwd needs."""
+    v = lib().hsap_window_attn_bwd_workspace(ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"))
+    if v < 0:
+        raise HsapError(HSAP_ERR_INVALID_ARG, lib().hsap_last_error().decode())
+    return v
+
+
+def window_attn_bwd(desc: AttnDesc, window: int, sinks: int, q, k, v, d_o, o, lse, cu_seqlens_dev, dq, dk, dv, workspace,
+                    stream=None) -> None:
+    """hsap_window_attn_bwd: gradients of window_attn_fwd (o, lse: its outputs) into dq bf16 [n, Hq, d] and dk / dv
+    [P, n, Hkv, d], both bf16 or both fp32; workspace: uint8, window_attn_bwd_workspace bytes."""
+    s = desc.shard
+    n = s.rows
+    hq, hkv, d, P = desc.heads_q, desc.heads_kv, desc.head_dim, s.sp_degree
+    for t, name in ((q, "q"), (d_o, "d_o"), (o, "o"), (dq, "dq")):
+        _dev(t, "bfloat16", name, n * hq * d)
+    for t, name in ((k, "k"), (v, "v")):
+        _dev(t, "bfloat16", name, P * n * hkv * d)
+    _dev(lse, "float32", "lse", hq * n)
+    _dev(cu_seqlens_dev, "int32", "cu_seqlens")
+    wide = getattr(dk, "dtype", None) is _dtypes["float32"]
+    for t, name in ((dk, "dk"), (dv, "dv")):
+        _dev(t, "float32" if wide else "bfloat16", name, P * n * hkv * d)
+    _dev(workspace, "uint8", "workspace")
+    _one_device(q, k, v, d_o, o, lse, cu_seqlens_dev, dq, dk, dv, workspace)
+    _check(lib().hsap_window_attn_bwd(ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q),
+                                      _ptr(k), _ptr(v), _ptr(d_o), _ptr(o), _ptr(lse), _ptr(cu_seqlens_dev),
+                                      cu_seqlens_dev.numel() - 1, _ptr(dq), _ptr(dk), _ptr(dv), int(wide), _ptr(workspace),
+                                      workspace.numel(), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------

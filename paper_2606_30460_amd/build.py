@@ -34,7 +34,8 @@ CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
 # Per-source additions.  The forward kernels never see a NaN (finite bf16 inputs; masked scores are
 # -inf, which stays honoured): without NaN semantics the compiler drops the canonicalising maxes
 # around the row maximum (5 VALU instructions per 64-key step; c4 forward +0.6-0.8 % on one box).
-EXTRA_FLAGS = {"attn_fwd.hip": ["-fno-honor-nans"]}
+# The window forward follows it for the same reason.
+EXTRA_FLAGS = {"attn_fwd.hip": ["-fno-honor-nans"], "window_fwd.hip": ["-fno-honor-nans"]}
 
 
 def _hipcc() -> str:

@@ -1,0 +1,151 @@
+// Device helpers of the window-attention kernels: document bounds of a wave's positions, the row of a position in
+// sharded order, and the direct-to-LDS transfer of a 64-row tile.
+#pragma once
+
+#include "hsap_internal.h"
+#include "mfma.h"
+
+namespace hsap {
+
+#if defined(__HIPCC__)
+
+// Queries of one chunk's sink pass (see window_bwd.hip).
+constexpr int32_t kSinkChunk = 1024;
+// Most sink tokens per document that the backward takes: one workgroup holds them all (4 waves x 32 keys).
+constexpr int32_t kMaxBwdSinks = 128;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Shard segments: local rows in pieces of consecutive positions, one (CONTIGUOUS) or two (ZIGZAG) per sequence of the
+// batch, each of geom.m rows.  Segment sg holds local rows sg * m .. sg * m + m - 1.
+__host__ __device__ inline int32_t segments_per_sequence(const Geom& g) { return g.layout == HSAP_LAYOUT_CONTIGUOUS ? 1 : 2; }
+
+// First position of segment sg of chunk x.
+__device__ __forceinline__ int32_t segment_start(const Geom& g, int32_t x, int32_t sg) {
+  return (int32_t)global_pos(g, x, (int64_t)sg * g.m);
+}
+
+// Storage of keys in sharded order as runs of consecutive positions: [lo, hi) are the positions whose row is
+// position + delta.  One chunk of a contiguous layout of one shard holds everything.
+struct KeySpan {
+  int32_t lo, hi;
+  int32_t delta;
+};
+
+__device__ __forceinline__ KeySpan key_span(const Geom& g, int32_t pos) {
+  if (g.P == 1 && g.layout == HSAP_LAYOUT_CONTIGUOUS) return KeySpan{0, (int32_t)g.N, 0};
+  const uint32_t Ns = (uint32_t)g.Ns, m = (uint32_t)g.m;
+  const uint32_t b = (uint32_t)pos / Ns, at = (uint32_t)pos - b * Ns;
+  const uint32_t piece = at / m;
+  const uint32_t P = (uint32_t)g.P;
+  uint32_t row = b * (uint32_t)g.ns;  // first row of the piece within its chunk
+  uint32_t chunk = piece;
+  if (g.layout != HSAP_LAYOUT_CONTIGUOUS && piece >= P) {
+    chunk = 2 * P - 1 - piece;
+    row += m;
+  }
+  const int32_t lo = (int32_t)(b * Ns + piece * m);
+  return KeySpan{lo, lo + (int32_t)m, (int32_t)(chunk * (uint32_t)g.n + row) - lo};
+}
+
+// Document [start, end) of this lane's position gq, for a wave whose lanes 0..31 hold positions that rise by at most one
+// from lane to lane (lane l ^ 32 holds the position of lane l).  A position at or behind the last boundary cu[nd]
+// has none: start = end = INT32_MAX.  One 64-entry window of boundaries serves the wave unless documents without
+// tokens fill it; then each lane searches.
+struct DocSpan {
+  int32_t start, end;
+};
+
+__device__ __forceinline__ DocSpan doc_span(const int32_t* cu, int32_t nd, int32_t gq, int lane) {
+  const DocWindow r = doc_window(nullptr, cu, nd, gq, lane);
+  const int32_t lo = __popcll(__builtin_amdgcn_ballot_w64(r.w <= r.g_lo)) - 1;
+  const int32_t last = __popcll(__builtin_amdgcn_ballot_w64(r.w <= r.g_hi)) - 1;
+  if (last >= 63) {
+    int32_t l = 0, h = nd + 1;  // cu[l] <= gq, cu[h] > gq (cu[nd + 1] standing for infinity)
+    while (h - l > 1) {
+      const int32_t mid = (l + h) >> 1;
+      if (cu[mid] <= gq) l = mid;
+      else h = mid;
+    }
+    if (l == nd) return DocSpan{INT32_MAX, INT32_MAX};
+    return DocSpan{cu[l], cu[l + 1]};
+  }
+  DocSpan d{__builtin_amdgcn_readlane(r.w, lo), INT32_MAX};
+  for (int32_t j = lo + 1; j <= last + 1; ++j) {
+    const int32_t b = __builtin_amdgcn_readlane(r.w, j);
+    if (gq >= b) d.start = b;
+    else d.end = min(d.end, b);
+  }
+  return d;
+}
+
+// Transfers of a [64][D] bf16 tile from global memory to a swizzled LDS tile (mfma.h), WAVES waves, 64 16-byte chunks
+// per instruction.  Issued from asm and ordered by the kernels' own vmcnt waits (vm_wait_barrier): the compiler would
+// wait for every transfer before any later LDS read.
+template <int D, int WAVES>
+struct TileStage {
+  static constexpr int CPR = D / 8, WCH = 64 * CPR / WAVES, U = WCH / 64;
+  uint32_t off[U];  // byte offset of this lane's chunk of instruction u from the tile's first row
+  uint32_t lds0;    // the wave's first chunk within a tile, in bytes
+  int first;        // this lane's chunk of instruction 0
+
+  __device__ __forceinline__ void init(int wave, int lane, int64_t row_bytes) {
+    first = WCH * wave + lane;
+    lds0 = (uint32_t)(WCH * 16 * wave);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = first + 64 * u, row = p / CPR;
+      off[u] = (uint32_t)(row * row_bytes + swz_chunk<CPR>(row, p % CPR) * 16);
+    }
+  }
+  // 64 readable rows at src, row_bytes apart; src and dst uniform over the wave
+  __device__ __forceinline__ void rows(const void* src, const __bf16* dst) const {
+    typedef __attribute__((address_space(3))) void* lds_void;
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void)dst + lds0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off[u]), "s"(src), "{m0}"(lds + 1024 * u));
+  }
+  // row r at address row(r), any order (rows may repeat)
+  template <typename F>
+  __device__ __forceinline__ void gather(F row, const __bf16* dst) const {
+    typedef __attribute__((address_space(3))) void* lds_void;
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void)dst + lds0;
+#pragma unroll 1  // (the rare path: one address at a time, the kernels have no registers to spare)
+    for (int u = 0; u < U; ++u) {
+      const int p = first + 64 * u, r = p / CPR;
+      const char* src = (const char*)row(r) + swz_chunk<CPR>(r, p % CPR) * 16;
+      asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds + 1024 * u));
+    }
+  }
+};
+
+// Uniform copy of a value that is the same on every lane.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Stages keys j0 .. j0 + 63 (clamped to jmax) of one K/V head: `base` is the head's row 0, rows `row_bytes` apart.
+// `span` is the run of positions that held the last tile's first key.
+template <int D, int WAVES>
+__device__ __forceinline__ void stage_keys(const TileStage<D, WAVES>& st, const Geom& g, KeySpan& span, int32_t j0,
+                                           int32_t jmax, const __bf16* base, int64_t row_elems, const __bf16* dst) {
+  if (j0 < span.lo || j0 >= span.hi) {
+    const KeySpan s = key_span(g, j0);
+    span = KeySpan{uniform(s.lo), uniform(s.hi), uniform(s.delta)};
+  }
+  if (j0 + 63 <= jmax && j0 + 63 < span.hi) {
+    st.rows(base + (int64_t)(j0 + span.delta) * row_elems, dst);
+  } else {
+    st.gather(
+        [&](int r) {
+          const int32_t pos = min(j0 + r, jmax);
+          const int32_t delta = pos < span.hi ? span.delta : key_span(g, pos).delta;
+          return base + (int64_t)(pos + delta) * row_elems;
+        },
+        dst);
+  }
+}
+
+#endif
+
+}  // namespace hsap

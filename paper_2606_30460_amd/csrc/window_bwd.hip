@@ -1,0 +1,607 @@
+// Window attention with sinks, backward.  With P_ij = exp(scale q_i . k_j - LSE_i) over the pairs the forward allows
+// and delta_i = sum_d dO_id O_id:
+//
+//   dV_j = sum_i P_ij dO_i,   dS_ij = P_ij (dO_i . v_j - delta_i),
+//   dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i   (dK, dV over the query heads of the K/V head)
+//
+// Every gradient row has one owner, which forms it whole in registers and stores it once: no atomics, the same bits
+// each time.  Four launches:
+//   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; also delta
+//   sinks    a document's sinks are seen by all its later queries, far more than a window's worth.  The shard's rows
+//            are cut into chunks of 1024 queries; one workgroup per (chunk, K/V head) forms what the chunk's queries
+//            give to the sinks of the document that reaches into it from before (outside their windows): fp32 partials
+//   sum      the chunks of one document are added up, in order, into the first one's partial
+//   dK, dV   one workgroup per (128 consecutive keys, K/V head), over the queries whose window holds one of them --
+//            and, for sinks, over the queries of their own chunk -- for every query head of the group; a sink's
+//            partial is added before the gradient is rounded
+// The middle two run only where some query can be further than a window from a sink.
+#include <algorithm>
+#include <type_traits>
+
+#include "window.h"
+
+namespace hsap {
+
+hsap_status check_window(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const int32_t* cu, int32_t num_docs,
+                         Geom* g);
+
+struct WindowBwdArgs {
+  const __bf16* q;
+  const __bf16* k;
+  const __bf16* v;
+  const __bf16* d_o;
+  const __bf16* o;
+  const float* lse;
+  float* delta;    // [Hq, n]
+  float* partial;  // [chunks, Hkv, sinks, 2, D]: dK (unscaled) and dV of the sinks per chunk of queries
+  const int32_t* cu;
+  __bf16* dq;
+  void* dk;
+  void* dv;
+  Geom geom;
+  int32_t num_docs;
+  int32_t shard;
+  int32_t hq;
+  int32_t hkv;
+  int32_t window;
+  int32_t sinks;
+  int32_t tiles;   // q-tiles (dQ) or key tiles (dK, dV) per segment
+  int32_t chunks;  // sink chunks per segment
+  int32_t dkv_f32;
+  float scale;
+  float scale_log2;
+};
+
+// ---------------------------------------------------------------------------
+// dQ: the forward's ranges, three products per 64-key step (S, dP and dS K).  dP - delta is formed by the matrix
+// product itself, whose accumulator starts at -delta.
+// ---------------------------------------------------------------------------
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs a) {
+  constexpr int KB = 64, CPR = D / 8, TILE = KB * D, BM = 32 * WAVES;
+  constexpr float NEG_INF = -__builtin_inff();
+  __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // K slots 0, 1, then V slots 0, 1
+  __shared__ int32_t tile_start;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int w = uniform(tid >> 6);
+  auto Ks = [&](int slot) { return ring + slot * TILE; };
+  auto Vs = [&](int slot) { return ring + (2 + slot) * TILE; };
+  int t, h;
+  run_and_head(blockIdx.x, a.hq, a.hkv, t, h);
+  const int32_t segs = (int32_t)(a.geom.n / a.geom.m);
+  const int32_t seg = t % segs, qt = a.tiles - 1 - t / segs;
+  const int g = h / (a.hq / a.hkv);
+  const int64_t n = a.geom.n;
+  const int32_t m = (int32_t)a.geom.m;
+  const int32_t p0 = uniform(segment_start(a.geom, a.shard, seg));
+  const int32_t cu_end = a.cu[a.num_docs];
+  const int32_t i0 = p0 + qt * BM;
+  const int32_t i1 = min(min(i0 + BM - 1, p0 + m - 1), cu_end - 1);
+  if (i1 < i0) return;
+  const int32_t gq = min(i0 + 32 * w + l32, i1);
+  const bool valid = i0 + 32 * w + l32 <= i1;
+  const int64_t qrow = (int64_t)seg * m + (gq - p0);
+
+  bf16x8 qf[D / 16], df[D / 16];
+  float delta = 0.f;
+  {
+    const int64_t at = (qrow * a.hq + h) * D + 8 * hi;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      qf[kk] = *(const bf16x8*)(a.q + at + 16 * kk);
+      df[kk] = *(const bf16x8*)(a.d_o + at + 16 * kk);
+      const bf16x8 of = *(const bf16x8*)(a.o + at + 16 * kk);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)df[kk][e], (float)of[e], delta);
+    }
+  }
+  delta = pair_sum(delta);
+  const float lse2 = a.lse[(int64_t)h * n + qrow] * kLog2e;
+  if (hi == 0 && valid) a.delta[(int64_t)h * n + qrow] = delta;
+  const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
+  if (tid == 0) tile_start = doc.start;
+  __syncthreads();
+  const int32_t start0 = uniform(tile_start);
+  const int32_t win_lo = max(start0, i0 - (a.window - 1));
+  const int32_t sink_hi = start0 + min(a.sinks, win_lo - start0);
+  const int32_t sink_steps = (sink_hi - start0 + KB - 1) / KB;
+  const int32_t total = sink_steps + (i1 - win_lo + KB) / KB;
+  const int32_t wlo = max(doc.start, gq - (a.window - 1));
+  const int32_t slen = min(a.sinks, wlo - doc.start);
+
+  const int64_t rstride = (int64_t)a.hkv * D;
+  const __bf16* kbase = a.k + (int64_t)g * D;
+  const __bf16* vbase = a.v + (int64_t)g * D;
+  TileStage<D, WAVES> st;
+  st.init(w, lane, rstride * 2);
+  KeySpan span{0, 0, 0};
+  auto stage = [&](int s, int slot) {
+    const int32_t j0 = s < sink_steps ? start0 + KB * s : win_lo + KB * (s - sink_steps);
+    const int32_t jmax = s < sink_steps ? sink_hi - 1 : i1;
+    stage_keys<D, WAVES>(st, a.geom, span, j0, jmax, kbase, rstride, Ks(slot));
+    stage_keys<D, WAVES>(st, a.geom, span, j0, jmax, vbase, rstride, Vs(slot));
+  };
+  const int tr_row = 4 * hi + ((lane & 15) >> 2);
+  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  int rowoff[D / 16], troff[D / 32][2];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) rowoff[kk] = swz<CPR>(l32, 16 * kk + 8 * hi);
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) troff[mb][k] = swz<CPR>(8 * k + tr_row, 32 * mb + tr_col) - 8 * k * D;
+
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb) dq[mb] = f32x16{};
+  f32x16 minus_delta;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) minus_delta[j] = -delta;
+
+  stage(0, 0);
+  vm_wait_barrier<0>();
+  auto step = [&](int s, auto par) __attribute__((always_inline)) {
+    constexpr int S0 = decltype(par)::value, S1 = S0 ^ 1;
+    if (s + 1 < total) stage(s + 1, S1);
+    const bool sink_step = s < sink_steps;
+    const int32_t j0 = sink_step ? start0 + KB * s : win_lo + KB * (s - sink_steps);
+    const uint32_t wlen = sink_step || !valid ? 0u : (uint32_t)(gq - wlo + 1);
+    const uint32_t sl = !valid ? 0u : (uint32_t)(sink_step ? min(slen, max(sink_hi - doc.start, 0)) : slen);
+    const int32_t rw = j0 - wlo, rs = j0 - doc.start;
+    const bool all = !valid || (rw >= 0 && rw + KB <= (int32_t)wlen);
+    const bool masked = __builtin_amdgcn_ballot_w64(!all) != 0;
+    const __bf16 *K = Ks(S0), *V = Vs(S0);
+#pragma unroll
+    for (int nb = 0; nb < KB / 32; ++nb) {
+      f32x16 sc = f32x16{}, dp = minus_delta;
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(K + 32 * nb * D + rowoff[kk]), qf[kk], sc);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) dp = mfma32(*(const bf16x8*)(V + 32 * nb * D + rowoff[kk]), df[kk], dp);
+      if (masked) {
+        const int32_t rw0 = rw + 4 * hi, rs0 = rs + 4 * hi;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int c = 32 * nb + c_row(j, 0);
+          if ((uint32_t)(rw0 + c) >= wlen && (uint32_t)(rs0 + c) >= sl) sc[j] = NEG_INF;
+        }
+      }
+      bf16x8 ds[2];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) ds[j >> 3][j & 7] = (__bf16)(fast_exp2(__builtin_fmaf(sc[j], a.scale_log2, -lse2)) * dp[j]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int rb = (32 * nb + 16 * half) * D;
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb)
+          dq[mb] = mfma32(cat4(ds_read_tr16(K + rb + troff[mb][0]), ds_read_tr16(K + rb + 8 * D + troff[mb][1])), ds[half],
+                          dq[mb]);
+      }
+    }
+    vm_wait_barrier<0>();
+  };
+  for (int s = 0; s < total; s += 2) {
+    step(s, std::integral_constant<int, 0>{});
+    if (s + 1 < total) step(s + 1, std::integral_constant<int, 1>{});
+  }
+
+  if (!valid) return;
+  __bf16* op = a.dq + (qrow * a.hq + h) * D + 4 * hi;
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+    for (int grp = 0; grp < 4; ++grp)
+      *(bf16x4*)(op + 32 * mb + 8 * grp) =
+          bf16x4{(__bf16)(dq[mb][4 * grp] * a.scale), (__bf16)(dq[mb][4 * grp + 1] * a.scale),
+                 (__bf16)(dq[mb][4 * grp + 2] * a.scale), (__bf16)(dq[mb][4 * grp + 3] * a.scale)};
+}
+
+// ---------------------------------------------------------------------------
+// dK, dV.  Wave w holds 32 keys (K and V rows in registers as the products' B operand, key = column), the workgroup
+// walks the queries in steps of 64 rows staged in LDS, head by head.  Per 32 queries: S and dP (rows = queries), then
+// dV^T += dO^T P and dK^T += Q^T dS with P and dS straight from registers and dO^T, Q^T by LDS transpose reads.
+//
+// Queries of key j in segment [a0, b0): j .. j + len - 1, where len ends with the window or the document -- a sink's
+// with its chunk or the window, whichever is later (pairs of a sink with queries behind both are the sink pass's).
+//
+// SINKS: the keys are the sinks, up to the chunk's first position, of the document that holds that position and began
+// before it; the queries those of the chunk outside the window.
+// ---------------------------------------------------------------------------
+template <int D, bool SINKS>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(WindowBwdArgs a) {
+  constexpr int WAVES = 4, QB = 64, CPR = D / 8, TILE = QB * D, BN = 32 * WAVES;
+  constexpr float NEG_INF = -__builtin_inff();
+  __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // Q slots 0, 1, then dO slots 0, 1
+  __shared__ __attribute__((aligned(16))) float rows_s[2][2][QB];   // [slot][LSE in log2 units, -delta]
+  __shared__ int32_t last_s[WAVES][2];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int w = uniform(tid >> 6);
+  const int grp = a.hq / a.hkv;
+  const int g = blockIdx.x % a.hkv;
+  const int32_t tile = blockIdx.x / a.hkv;
+  const int64_t n = a.geom.n;
+  const int32_t m = (int32_t)a.geom.m;
+  const int32_t per_seq = segments_per_sequence(a.geom);
+  const int32_t cu_end = a.cu[a.num_docs];
+
+  // this lane's key: position, row, and its queries [qlo, qlo + len[x]) in the shard's segment x of the sequence
+  int32_t key, qlo, first_seg;
+  int64_t krow;
+  bool key_ok;
+  int32_t len[2] = {0, 0}, seg_lo[2] = {0, 0}, seg_hi[2] = {0, 0};
+  DocSpan doc;
+  int32_t t_doc = 0;  // SINKS: the document's start
+  if constexpr (SINKS) {
+    first_seg = tile / a.chunks;
+    const int32_t a0 = uniform(segment_start(a.geom, a.shard, first_seg));
+    const int32_t c0 = a0 + (tile - first_seg * a.chunks) * kSinkChunk;
+    if (c0 >= cu_end) return;
+    doc = doc_span(a.cu, a.num_docs, c0, lane);
+    t_doc = uniform(doc.start);
+    const int32_t doc_end = uniform(doc.end);
+    const int32_t count = min(a.sinks, c0 - t_doc);
+    if (count <= 0) return;  // the document begins here: its sinks' far queries are other chunks'
+    key_ok = 32 * w + l32 < count;
+    key = t_doc + min(32 * w + l32, count - 1);
+    krow = key + key_span(a.geom, key).delta;
+    seg_lo[0] = c0;
+    seg_hi[0] = min(min(c0 + kSinkChunk, a0 + m), doc_end);
+    qlo = max(c0, (int32_t)min((int64_t)key + a.window, (int64_t)INT32_MAX));
+    len[0] = key_ok ? max(seg_hi[0] - qlo, 0) : 0;
+  } else {
+    // tile of 128 rows within a run of consecutive positions of the sharded order
+    const int32_t run = tile / a.tiles, at = (tile - run * a.tiles) * BN;
+    const int32_t runs = (int32_t)(n / m);  // per chunk
+    const int32_t chunk = run / runs, rseg = run - chunk * runs;
+    const int32_t r0 = uniform(segment_start(a.geom, chunk, rseg));
+    const int32_t j0 = r0 + at;
+    const int32_t jl = min(min(j0 + BN - 1, r0 + m - 1), cu_end - 1);
+    if (jl < j0) return;
+    key = min(j0 + 32 * w + l32, jl);
+    key_ok = j0 + 32 * w + l32 <= jl;
+    krow = (int64_t)chunk * n + (int64_t)rseg * m + (key - r0);
+    doc = doc_span(a.cu, a.num_docs, key, lane);
+    qlo = key;
+    const int32_t b = rseg / per_seq;  // sequence of the batch
+    first_seg = b * per_seq;
+    const int32_t near = (int32_t)min((int64_t)doc.end, (int64_t)key + a.window);  // end of the queries whose window holds it
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      if (x >= per_seq) break;
+      const int32_t a0 = uniform(segment_start(a.geom, a.shard, first_seg + x)), b0 = a0 + m;
+      int32_t end = near;
+      if (key - doc.start < a.sinks && key >= a0 && key < b0)
+        end = max(end, min(doc.end, a0 + ((key - a0) / kSinkChunk + 1) * kSinkChunk));
+      len[x] = key_ok ? max(min(end, b0) - key, 0) : 0;
+      seg_lo[x] = max(a0, j0);
+      seg_hi[x] = b0;
+    }
+  }
+  // the workgroup's queries per segment: from the first that any key has to the last
+  if constexpr (!SINKS) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      int32_t e = key + len[x];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o));
+      if (lane == 0) last_s[w][x] = e;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      int32_t e = last_s[0][x];
+      for (int y = 1; y < WAVES; ++y) e = max(e, last_s[y][x]);
+      seg_hi[x] = min(seg_hi[x], uniform(e));
+    }
+  } else {
+    seg_lo[0] = max(seg_lo[0], (int32_t)min((int64_t)t_doc + a.window, (int64_t)INT32_MAX));
+  }
+  const int32_t cnt0 = max(0, (seg_hi[0] - seg_lo[0] + QB - 1) / QB);
+  const int32_t cnt1 = SINKS ? 0 : max(0, (seg_hi[1] - seg_lo[1] + QB - 1) / QB);
+  const int32_t total = (cnt0 + cnt1) * grp;
+
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb) dk[mb] = dv[mb] = f32x16{};
+
+  if (total > 0) {
+    bf16x8 kf[D / 16], vf[D / 16];
+    {
+      const int64_t at = (krow * a.hkv + g) * D + 8 * hi;
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        kf[kk] = *(const bf16x8*)(a.k + at + 16 * kk);
+        vf[kk] = *(const bf16x8*)(a.v + at + 16 * kk);
+      }
+    }
+    const int64_t rstride = (int64_t)a.hq * D;
+    TileStage<D, WAVES> st;
+    st.init(w, lane, rstride * 2);
+    // step i: segment x, head hh of the group, 64 queries from position pos; segment by segment, head by head
+    struct Step {
+      int32_t x, hh, s;
+    };
+    auto advance = [&](Step& p) {
+      if (++p.s < (p.x ? cnt1 : cnt0)) return;
+      p.s = 0;
+      if (++p.hh < grp) return;
+      p.hh = 0;
+      ++p.x;
+    };
+    float row_next = 0.f;  // the next step's LSE (wave 0) or delta (wave 1) of row `lane`
+    auto stage = [&](const Step& p, int slot) {
+      const int32_t lo = p.x ? seg_lo[1] : seg_lo[0], top = p.x ? seg_hi[1] : seg_hi[0];
+      const int32_t pos = lo + QB * p.s;
+      const int32_t a0 = segment_start(a.geom, a.shard, first_seg + p.x);
+      const int64_t r0 = (int64_t)(first_seg + p.x) * m + (pos - a0);  // local row of the step's first query
+      const int h = g * grp + p.hh;
+      const __bf16* qb = a.q + (r0 * a.hq + h) * D;
+      const __bf16* ob = a.d_o + (r0 * a.hq + h) * D;
+      const int32_t most = top - 1 - pos;  // rows behind the last query repeat it (masked)
+      if (most >= QB - 1) {
+        st.rows(qb, ring + slot * TILE);
+        st.rows(ob, ring + (2 + slot) * TILE);
+      } else {
+        st.gather([&](int r) { return qb + min(r, most) * rstride; }, ring + slot * TILE);
+        st.gather([&](int r) { return ob + min(r, most) * rstride; }, ring + (2 + slot) * TILE);
+      }
+      if (w < 2) row_next = (w == 0 ? a.lse : a.delta)[(int64_t)h * n + r0 + min(lane, most)];
+    };
+    auto store_rows = [&](int slot) {
+      if (w < 2) rows_s[slot][w][lane] = w == 0 ? row_next * kLog2e : -row_next;
+    };
+    const int tr_row = 4 * hi + ((lane & 15) >> 2);
+    const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    int rowoff[D / 16], troff[D / 32][2];
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) rowoff[kk] = swz<CPR>(l32, 16 * kk + 8 * hi);
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) troff[mb][k] = swz<CPR>(8 * k + tr_row, 32 * mb + tr_col) - 8 * k * D;
+
+    Step cur{cnt0 > 0 ? 0 : 1, 0, 0}, nxt = cur;
+    stage(cur, 0);
+    store_rows(0);
+    vm_wait_barrier<0>();
+    advance(nxt);
+    auto step = [&](int i, auto par) __attribute__((always_inline)) {
+      constexpr int S0 = decltype(par)::value, S1 = S0 ^ 1;
+      if (i + 1 < total) stage(nxt, S1);
+      const __bf16 *Q = ring + S0 * TILE, *O = ring + (2 + S0) * TILE;
+      const int32_t pos = (cur.x ? seg_lo[1] : seg_lo[0]) + QB * cur.s;
+      const uint32_t ln = (uint32_t)(cur.x ? len[1] : len[0]);
+#pragma unroll
+      for (int nb = 0; nb < QB / 32; ++nb) {
+        const int32_t r = pos + 32 * nb - qlo;  // first query of the block relative to the key's first
+        const bool some = r < (int32_t)ln && r + 31 >= 0;
+        const bool all = !key_ok || (r >= 0 && r + 32 <= (int32_t)ln);
+        if (__builtin_amdgcn_ballot_w64(some) == 0) continue;
+        f32x16 sc = f32x16{}, dp;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dp[j] = rows_s[S0][1][32 * nb + c_row(j, hi)];
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(Q + 32 * nb * D + rowoff[kk]), kf[kk], sc);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) dp = mfma32(*(const bf16x8*)(O + 32 * nb * D + rowoff[kk]), vf[kk], dp);
+        if (__builtin_amdgcn_ballot_w64(!all) != 0) {
+          const int32_t r4 = r + 4 * hi;
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if ((uint32_t)(r4 + c_row(j, 0)) >= ln) sc[j] = NEG_INF;
+        }
+        bf16x8 pb[2], ds[2];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float p = fast_exp2(__builtin_fmaf(sc[j], a.scale_log2, -rows_s[S0][0][32 * nb + c_row(j, hi)]));
+          pb[j >> 3][j & 7] = (__bf16)p;
+          ds[j >> 3][j & 7] = (__bf16)(p * dp[j]);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int rb = (32 * nb + 16 * half) * D;
+#pragma unroll
+          for (int mb = 0; mb < D / 32; ++mb) {
+            dv[mb] = mfma32(cat4(ds_read_tr16(O + rb + troff[mb][0]), ds_read_tr16(O + rb + 8 * D + troff[mb][1])), pb[half],
+                            dv[mb]);
+            dk[mb] = mfma32(cat4(ds_read_tr16(Q + rb + troff[mb][0]), ds_read_tr16(Q + rb + 8 * D + troff[mb][1])), ds[half],
+                            dk[mb]);
+          }
+        }
+      }
+      if (i + 1 < total) store_rows(S1);
+      vm_wait_barrier<0>();
+      cur = nxt;
+      if (i + 2 < total) advance(nxt);
+    };
+    for (int i = 0; i < total; i += 2) {
+      step(i, std::integral_constant<int, 0>{});
+      if (i + 1 < total) step(i + 1, std::integral_constant<int, 1>{});
+    }
+  }
+
+  if constexpr (SINKS) {
+    // every sink of the document, those without a query here as zeros
+    const int32_t s = 32 * w + l32;
+    if (s >= a.sinks) return;
+    float* out = a.partial + (((int64_t)tile * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 x{dk[mb][4 * q], dk[mb][4 * q + 1], dk[mb][4 * q + 2], dk[mb][4 * q + 3]};
+        f32x4 y{dv[mb][4 * q], dv[mb][4 * q + 1], dv[mb][4 * q + 2], dv[mb][4 * q + 3]};
+        *(f32x4*)(out + 32 * mb + 8 * q) = x;
+        *(f32x4*)(out + D + 32 * mb + 8 * q) = y;
+      }
+  } else {
+    if (!key_ok) return;
+    const int32_t s = key - doc.start;
+    if (s < a.sinks && a.partial) {
+      // the summed partials of the document's chunks in each of the shard's segments
+      for (int x = 0; x < per_seq; ++x) {
+        const int32_t a0 = segment_start(a.geom, a.shard, first_seg + x);
+        const int32_t c = doc.start < a0 ? 0 : (doc.start - a0) / kSinkChunk + 1;  // first chunk that begins inside it
+        const int64_t c0 = (int64_t)a0 + (int64_t)c * kSinkChunk;
+        if (c0 >= min(doc.end, a0 + m)) continue;
+        const float* in = a.partial + ((((int64_t)(first_seg + x) * a.chunks + c) * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 y = *(const f32x4*)(in + 32 * mb + 8 * q), z = *(const f32x4*)(in + D + 32 * mb + 8 * q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              dk[mb][4 * q + e] += y[e];
+              dv[mb][4 * q + e] += z[e];
+            }
+          }
+      }
+    }
+    const int64_t at = (krow * a.hkv + g) * D + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x{dk[mb][4 * q] * a.scale, dk[mb][4 * q + 1] * a.scale, dk[mb][4 * q + 2] * a.scale, dk[mb][4 * q + 3] * a.scale};
+        const f32x4 y{dv[mb][4 * q], dv[mb][4 * q + 1], dv[mb][4 * q + 2], dv[mb][4 * q + 3]};
+        const int64_t e = at + 32 * mb + 8 * q;
+        if (a.dkv_f32) {
+          *(f32x4*)((float*)a.dk + e) = x;
+          *(f32x4*)((float*)a.dv + e) = y;
+        } else {
+          *(bf16x4*)((__bf16*)a.dk + e) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+          *(bf16x4*)((__bf16*)a.dv + e) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+        }
+      }
+  }
+}
+
+// Sum of the sink partials of one document over a segment's chunks, in order, into the first one's: one workgroup per
+// (chunk, K/V head), idle unless its chunk is a document's first.
+__global__ __launch_bounds__(256) void window_sink_sum_kernel(WindowBwdArgs a, int elems) {
+  const int lane = threadIdx.x & 63;
+  const int g = blockIdx.x % a.hkv;
+  const int32_t tile = blockIdx.x / a.hkv;
+  const int32_t seg = tile / a.chunks, c = tile - seg * a.chunks;
+  const int32_t a0 = segment_start(a.geom, a.shard, seg);
+  const int64_t c0 = (int64_t)a0 + (int64_t)c * kSinkChunk;
+  if (c0 >= a.cu[a.num_docs]) return;
+  const DocSpan doc = doc_span(a.cu, a.num_docs, (int32_t)c0, lane);
+  if (doc.start >= c0 || (c > 0 && doc.start < c0 - kSinkChunk)) return;
+  const int64_t end = min((int64_t)doc.end, a0 + a.geom.m);
+  const int32_t more = (int32_t)((end - 1 - c0) / kSinkChunk);  // chunks of the document behind this one
+  if (more == 0) return;
+  const int64_t step = (int64_t)a.hkv * elems;
+  float* p = a.partial + ((int64_t)tile * a.hkv + g) * elems;
+  for (int e = 4 * threadIdx.x; e < elems; e += 4 * 256) {
+    f32x4 sum = *(const f32x4*)(p + e);
+    for (int x = 1; x <= more; ++x) sum += *(const f32x4*)(p + x * step + e);
+    *(f32x4*)(p + e) = sum;
+  }
+}
+
+static hsap_status check_launch_window(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
+  return HSAP_OK;
+}
+
+// Sink chunks per segment that the sink pass runs over; 0 where no query is further than a window from a sink.
+static int32_t sink_chunks(const Geom& g, int32_t window, int32_t sinks) {
+  return sinks > 0 && window < g.Ns ? (int32_t)((g.m + kSinkChunk - 1) / kSinkChunk) : 0;
+}
+
+static int64_t delta_bytes(const hsap_attn_desc* d, const Geom& g) { return (4 * g.n * d->heads_q + 255) / 256 * 256; }
+
+static int64_t bwd_workspace(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
+  return delta_bytes(d, g) + g.n / g.m * sink_chunks(g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
+}
+
+template <int D>
+static hsap_status launch_window_bwd(WindowBwdArgs& a, hipStream_t s) {
+  const Geom& g = a.geom;
+  const int64_t segs = g.n / g.m;
+  a.tiles = (int32_t)((g.m + 127) / 128);
+  const int64_t q_blocks = segs * a.tiles * a.hq, k_blocks = segs * g.P * a.tiles * a.hkv, s_blocks = segs * a.chunks * a.hkv;
+  if (q_blocks > INT32_MAX || k_blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
+  hipLaunchKernelGGL((window_dq_kernel<D, 4>), dim3((unsigned)q_blocks), dim3(256), 0, s, a);
+  hsap_status st = check_launch_window("window_attn_bwd dQ");
+  if (st != HSAP_OK) return st;
+  if (s_blocks) {
+    hipLaunchKernelGGL((window_dkv_kernel<D, true>), dim3((unsigned)s_blocks), dim3(256), 0, s, a);
+    st = check_launch_window("window_attn_bwd sinks");
+    if (st != HSAP_OK) return st;
+    if (a.chunks > 1) {
+      hipLaunchKernelGGL(window_sink_sum_kernel, dim3((unsigned)s_blocks), dim3(256), 0, s, a, a.sinks * 2 * D);
+      st = check_launch_window("window_attn_bwd sink sum");
+      if (st != HSAP_OK) return st;
+    }
+  } else {
+    a.partial = nullptr;
+  }
+  hipLaunchKernelGGL((window_dkv_kernel<D, false>), dim3((unsigned)k_blocks), dim3(256), 0, s, a);
+  return check_launch_window("window_attn_bwd dK/dV");
+}
+
+}  // namespace hsap
+
+using namespace hsap;
+
+extern "C" int64_t hsap_window_attn_bwd_workspace(const hsap_attn_desc* desc, int32_t window, int32_t sinks) {
+  clear_error();
+  Geom g;
+  static const int32_t none = 0;
+  if (check_window(desc, window, sinks, &none, 1, &g) != HSAP_OK) return -1;
+  const int32_t s = (int32_t)std::min<int64_t>(sinks, g.Ns);
+  return bwd_workspace(desc, g, window, s);
+}
+
+extern "C" hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const void* q,
+                                            const void* k, const void* v, const void* d_o, const void* o, const float* lse,
+                                            const int32_t* cu_seqlens, int32_t num_docs, void* dq, void* dk, void* dv,
+                                            int32_t dkv_f32, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  clear_error();
+  WindowBwdArgs a{};
+  hsap_status st = check_window(desc, window, sinks, cu_seqlens, num_docs, &a.geom);
+  if (st != HSAP_OK) return st;
+  a.window = (int32_t)std::min<int64_t>(window, a.geom.Ns);
+  a.sinks = (int32_t)std::min<int64_t>(sinks, a.geom.Ns);
+  a.chunks = sink_chunks(a.geom, a.window, a.sinks);
+  if (a.chunks && a.sinks > kMaxBwdSinks)
+    HSAP_FAIL(HSAP_ERR_UNSUPPORTED, "sinks %d above %d in the backward", sinks, kMaxBwdSinks);
+  if (!q || !k || !v || !d_o || !o || !lse || !dq || !dk || !dv || !workspace)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)d_o | (uintptr_t)o | (uintptr_t)workspace) & 15)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "q, k, v, d_o, o and workspace must be 16-byte aligned");
+  if (((uintptr_t)dq & 7) || (((uintptr_t)dk | (uintptr_t)dv) & (dkv_f32 ? 15 : 7)))
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "dq, dk and dv must be 8-byte aligned (16-byte as fp32)");
+  if (workspace_bytes < bwd_workspace(desc, a.geom, a.window, a.sinks))
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
+              (long long)bwd_workspace(desc, a.geom, a.window, a.sinks));
+  a.q = (const __bf16*)q;
+  a.k = (const __bf16*)k;
+  a.v = (const __bf16*)v;
+  a.d_o = (const __bf16*)d_o;
+  a.o = (const __bf16*)o;
+  a.lse = lse;
+  a.delta = (float*)workspace;
+  a.partial = (float*)((char*)workspace + delta_bytes(desc, a.geom));
+  a.cu = cu_seqlens;
+  a.dq = (__bf16*)dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.num_docs = num_docs;
+  a.shard = desc->shard.shard_id;
+  a.hq = desc->heads_q;
+  a.hkv = desc->heads_kv;
+  a.dkv_f32 = dkv_f32 != 0;
+  a.scale = desc->softmax_scale;
+  a.scale_log2 = desc->softmax_scale * kLog2e;
+  return desc->head_dim == 128 ? launch_window_bwd<128>(a, (hipStream_t)hip_stream)
+                               : launch_window_bwd<64>(a, (hipStream_t)hip_stream);
+}
