@@ -751,6 +751,95 @@ hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int
                                  int32_t dkv_f32, void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Paged K/V cache in 8 bits -- serving a model trained with the layers above: the keys and values of every
+ * sequence's tokens in pages, e4m3 codes with one scale per page and head (an extension beyond the paper, as
+ * hsap_quantize_fp8's codes are).  A token's value is code * scale of its page and head.
+ *
+ *   codes       device uint8 [num_pages, Hkv, page_size, d], 16-byte aligned, K and V each.
+ *   scales      device fp32 [num_pages, Hkv], K and V each.
+ *   page_table  device int32 [num_seqs, table_width]: sequence s keeps positions p * page_size .. of its own in page
+ *               page_table[s, p].  Entries of pages without a token that a call reads or writes are not looked at
+ *               (a window lets a serving loop hand old pages back).  An entry outside [0, num_pages) is no page:
+ *               nothing is written there and its tokens are not seen.  Several sequences may share pages they only
+ *               read; a page that two sequences append to in one call holds either's codes.
+ *   seq_lens    device int32 [num_seqs]: tokens of each sequence, the new ones included.  0 (or less): an idle slot.
+ *   cu_new      device int32 [num_seqs + 1], 0 = cu[0] <= ... <= cu[num_seqs] <= total_new: sequence s has the rows
+ *               cu[s] .. cu[s + 1] - 1 of the new-token tensors, its last tokens, at positions seq_lens[s] - count ..
+ *               seq_lens[s] - 1.  Rows at or behind cu[num_seqs] belong to no sequence: not read, not written.
+ *               NULL: one row for each sequence (total_new = num_seqs).
+ * These arrays are read by the kernels, so a captured call follows their contents at each replay.  No entry point below
+ * allocates or synchronises.
+ * --------------------------------------------------------------------- */
+typedef struct {
+  int32_t num_pages;    /* >= 1                                     */
+  int32_t page_size;    /* tokens per page: 16, 32, 64 or 128       */
+  int32_t heads_kv;     /* Hkv                                      */
+  int32_t head_dim;     /* d: 64 or 128                             */
+  int32_t num_seqs;     /* sequences of this call                   */
+  int32_t table_width;  /* pages per row of the page table          */
+} hsap_cache_desc;
+
+typedef struct {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+} hsap_cache;
+
+/*
+ * hsap_cache_append -- the new tokens' K and V into the cache, K rotated by its position on the way, and Q's rows
+ * rotated likewise.
+ *   k, v        device bf16, row t at t * stride elements: [Hkv, d] contiguous; 16-byte aligned, strides multiples of
+ *               8 (a fused projection's rows are read in place).
+ *   cos_sin     device fp32 [cos_sin_rows, rot_dim], 16-byte aligned: row p holds cos (rot_dim / 2) then sin of
+ *               position p.  The pair of values (i, i + rot_dim / 2) -- with interleaved != 0: (2 i, 2 i + 1) -- becomes
+ *               (a cos_i - b sin_i, b cos_i + a sin_i), each operation in fp32; values behind rot_dim stay.
+ *   rot_dim     a multiple of 16 up to d; 0: no rotation, cos_sin not read.
+ *   k_out       device bf16 [total_new, Hkv, d] or NULL: K rotated (for the prompt's own attention).
+ *   q, q_out    device bf16 [total_new, heads_q, d] (q with a row stride as k; q_out contiguous), both or neither.
+ * Scales are powers of two: the smallest 2^e, -100 <= e <= 120, with 448 * 2^e >= every value of the page and head, among
+ * the tokens it holds (a token overwritten at its position still counts until the page is begun anew).  Codes are
+ * e4m3 of value / scale, fp32 rounded to nearest even, once.  When a new token raises a page's scale, the codes of
+ * its older tokens are encoded for the new one.  NaN becomes the NaN code, an infinity saturates at 448 * scale;
+ * neither moves the scale.
+ * A token at a position below 0, at or behind cos_sin_rows (rot_dim > 0) is skipped (nothing of it written); at or
+ * behind table_width * page_size or on no page it is not cached (its k_out and q_out rows are written).
+ * One launch on `stream`.
+ */
+hsap_status hsap_cache_append(const hsap_cache_desc* desc, const hsap_cache* cache, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, const int32_t* cu_new, int64_t total_new,
+                              const float* cos_sin, int64_t cos_sin_rows, int32_t rot_dim, int32_t interleaved,
+                              void* k_out, const void* q, int64_t q_stride, int32_t heads_q, void* q_out,
+                              void* hip_stream);
+
+/* Bytes of device workspace hsap_cache_attn needs for any window (host); -1 for invalid arguments.  desc's num_pages is
+ * not read. */
+int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each);
+
+/*
+ * hsap_cache_attn -- attention of the newest tokens over the cache: row t of sequence s at position
+ * p = seq_lens[s] - count + (t - cu_new[s]) sees the tokens j <= p with p - j < window or j < sinks.
+ *   heads_q, softmax_scale  query head h reads K/V head h / (heads_q / Hkv); scores are softmax_scale * q . k.
+ *   window, sinks  as in hsap_window_attn_fwd (window >= 1).
+ *   q           device bf16, row t at t * q_stride elements: [heads_q, d] contiguous; 16-byte aligned, q_stride a
+ *               multiple of 8.  Rotated already.
+ *   cu_new, total_q  the rows of each sequence (NULL: one each).
+ *   o_out       device bf16 [total_q, heads_q, d], 16-byte aligned.
+ *   lse_out     device fp32 [heads_q, total_q], or NULL.
+ *   workspace   device, 16-byte aligned, workspace_bytes >= hsap_cache_attn_workspace; contents ignored.  Calls that
+ *               overlap in time need workspaces of their own.
+ * A row that sees no token (an idle slot, position below 0) gets O = 0, LSE = -inf.  What the cache holds at positions no
+ * row sees is not used, whatever it is.  q and the cached values a row sees are finite.
+ * One or two launches on `stream`.
+ */
+hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
+                            int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
+                            int64_t total_q, void* o_out, float* lse_out, void* workspace, int64_t workspace_bytes,
+                            void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Step executor -- the library's runtime for one shard geometry: each packed
  * batch is planned on the host and run with one call per stage.  Not in the
  * paper; it sequences the entry points above the way a training step uses

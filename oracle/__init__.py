@@ -44,9 +44,10 @@ What it computes, with the passages it follows (HSAP paper, arxiv 2606.30460):
 
 * ``window`` -- window attention with sinks over the packed documents (an extension beyond the paper's full
   attention), with derived error bounds.
+* ``cache`` -- the paged 8-bit K/V cache: rotation, codes and scales of an append, attention over it (an extension).
 
 Parity status: every function above is pinned by ``tests/test_oracle_pins.py`` (``window``:
-``tests/test_window_oracle.py``) against brute force, closed forms, library routines or invariants; none is
+``tests/test_window_oracle.py``, ``cache``: ``tests/test_cache_oracle.py``) against brute force, closed forms, library routines or invariants; none is
 "parity unpinned".
 """
 from .attention import (  # noqa: F401
@@ -70,3 +71,4 @@ from .schedule import backward_program, forward_program  # noqa: F401
 from .batch import batch_plan_shard, batch_shard_backward, batch_shard_forward, split_batch  # noqa: F401
 from .fp8 import decode_fp8, dequantize_fp8, quantize_fp8  # noqa: F401
 from .window import window_allowed, window_attention  # noqa: F401
+from . import cache  # noqa: F401

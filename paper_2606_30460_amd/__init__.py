@@ -16,11 +16,15 @@ from ._lib import (  # noqa: F401
     AttnDesc,
     Executor,
     HsapError,
+    KVCache,
     ShardDesc,
     attn_bwd_bf16,
     attn_bwd_preprocess,
     attn_desc,
     attn_fwd_fused,
+    cache_append,
+    cache_attn,
+    cache_attn_workspace,
     convert_f32_bf16,
     doc_start,
     lib,

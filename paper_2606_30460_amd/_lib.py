@@ -43,6 +43,7 @@ EXPORTED = (
     "hsap_executor_plan", "hsap_executor_info", "hsap_executor_forward", "hsap_executor_partial_forward",
     "hsap_executor_merge", "hsap_executor_backward",
     "hsap_window_attn_fwd", "hsap_window_attn_bwd_workspace", "hsap_window_attn_bwd",
+    "hsap_cache_append", "hsap_cache_attn_workspace", "hsap_cache_attn",
 )
 
 EXEC_BACKWARD = 1
@@ -85,6 +86,16 @@ class ExecInfo(ctypes.Structure):
                 ("num_runs_q", ctypes.c_int64), ("num_runs_k", ctypes.c_int64), ("num_runs_all", ctypes.c_int64),
                 ("num_parts", ctypes.c_int32), ("split_length", ctypes.c_int32),
                 ("chunks_with_tiles", ctypes.c_int32), ("final_q_tiles", ctypes.c_int32), ("chunk_mask", ctypes.c_uint64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class CacheBuffers(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -132,6 +143,10 @@ _SIG = {
     "hsap_window_attn_bwd_workspace": (ctypes.c_int64, [_P, _I32, _I32]),
     "hsap_window_attn_bwd": (ctypes.c_int, [_P, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _I32, _P, _I64,
                                             _P]),
+    "hsap_cache_append": (ctypes.c_int, [_P, _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _I32, _P, _P, _I64, _I32, _P,
+                                         _P]),
+    "hsap_cache_attn_workspace": (ctypes.c_int64, [_P, _I32, _I64, _I32]),
+    "hsap_cache_attn": (ctypes.c_int, [_P, _P, _I32, ctypes.c_float, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P]),
 }
 
 
@@ -737,6 +752,112 @@ def window_attn_bwd(desc: AttnDesc, window: int, sinks: int, q, k, v, d_o, o, ls
                                       _ptr(k), _ptr(v), _ptr(d_o), _ptr(o), _ptr(lse), _ptr(cu_seqlens_dev),
                                       cu_seqlens_dev.numel() - 1, _ptr(dq), _ptr(dk), _ptr(dv), int(wide), _ptr(workspace),
                                       workspace.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# paged K/V cache in 8 bits
+# ---------------------------------------------------------------------------
+
+class KVCache:
+    """The tensors of a paged e4m3 K/V cache (hsap_cache): codes uint8 [num_pages, Hkv, page_size, d], scales fp32
+    [num_pages, Hkv], page_table int32 [num_seqs, table_width], seq_lens int32 [num_seqs].  The tensors are the
+    caller's: writing other pages or lengths into them changes the next call."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens):
+        _dev(k_codes, "uint8", "k_codes")
+        if k_codes.dim() != 4 or page_table.dim() != 2:
+            raise ValueError("codes must be [num_pages, heads_kv, page_size, head_dim], page_table [num_seqs, table_width]")
+        pages, hkv, size, d = k_codes.shape
+        seqs, width = page_table.shape
+        _dev(v_codes, "uint8", "v_codes", k_codes.numel())
+        _dev(k_scale, "float32", "k_scale", pages * hkv)
+        _dev(v_scale, "float32", "v_scale", pages * hkv)
+        _dev(page_table, "int32", "page_table")
+        _dev(seq_lens, "int32", "seq_lens", seqs)
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.page_table, self.seq_lens = page_table, seq_lens
+        self.tensors = (k_codes, v_codes, k_scale, v_scale, page_table, seq_lens)
+        if any(t.device != k_codes.device for t in self.tensors):
+            raise ValueError("the cache's tensors are on several devices")
+        self.desc = CacheDesc(pages, size, hkv, d, seqs, width)
+        self.buffers = CacheBuffers(*[_ptr(t) for t in self.tensors])
+
+
+def _token_rows(t, what: str, rows: int, heads: int, d: int) -> int:
+    """Row stride (elements) of a bf16 tensor [rows, heads, d] whose rows are contiguous."""
+    torch = _torch or _load_torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a device tensor" % what)
+    if t.dtype is not _dtypes["bfloat16"]:
+        raise TypeError("%s must be bfloat16, got %s" % (what, t.dtype))
+    if tuple(t.shape) != (rows, heads, d):
+        raise ValueError("%s is %s, expected [%d, %d, %d]" % (what, list(t.shape), rows, heads, d))
+    row, head, one = t.stride()
+    if (one != 1 or (head != d and heads > 1)) and rows:
+        raise ValueError("%s must have contiguous rows [heads, head_dim]" % what)
+    return row if rows > 1 else heads * d
+
+
+def cache_append(cache: KVCache, k, v, cu_new, cos_sin=None, interleaved: bool = False, k_out=None, q=None, q_out=None,
+                 stream=None) -> None:
+    """hsap_cache_append: new tokens' k / v bf16 [total_new, Hkv, d] (rows may be strided) into the cache, K (and q bf16
+    [total_new, Hq, d] -> q_out) rotated by the rows of cos_sin fp32 [positions, rot_dim] (None: not rotated); k_out
+    takes the rotated K.  cu_new int32 [num_seqs + 1], or None for one token per sequence."""
+    c = cache.desc
+    total = k.shape[0]
+    ks = _token_rows(k, "k", total, c.heads_kv, c.head_dim)
+    vs = _token_rows(v, "v", total, c.heads_kv, c.head_dim)
+    if cu_new is not None:
+        _dev(cu_new, "int32", "cu_new", c.num_seqs + 1)
+    rows = rot = 0
+    if cos_sin is not None:
+        _dev(cos_sin, "float32", "cos_sin")
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [positions, rot_dim]")
+        rows, rot = cos_sin.shape
+    if k_out is not None:
+        _dev(k_out, "bfloat16", "k_out", total * c.heads_kv * c.head_dim)
+    heads = qs = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is not None:
+        heads = q.shape[1]
+        qs = _token_rows(q, "q", total, heads, c.head_dim)
+        _dev(q_out, "bfloat16", "q_out", total * heads * c.head_dim)
+    _one_device(k, v, cu_new, cos_sin, k_out, q, q_out, cache.tensors[0])
+    _check(lib().hsap_cache_append(ctypes.byref(c), ctypes.byref(cache.buffers), _ptr(k), ks, _ptr(v), vs, _ptr(cu_new), total,
+                                   _ptr(cos_sin), rows, rot, int(bool(interleaved)), _ptr(k_out), _ptr(q), qs, heads,
+                                   _ptr(q_out), _stream(stream)))
+
+
+def cache_attn_workspace(cache: KVCache, heads_q: int, total_q: int, one_each: Optional[bool] = None) -> int:
+    """hsap_cache_attn_workspace: bytes that cache_attn needs for total_q rows.  one_each: whether the calls pass no
+    cu_new; None: the larger of both."""
+    if one_each is None:
+        return max(cache_attn_workspace(cache, heads_q, total_q, x) for x in (True, False))
+    v = lib().hsap_cache_attn_workspace(ctypes.byref(cache.desc), int(heads_q), int(total_q), int(one_each))
+    if v < 0:
+        raise HsapError(HSAP_ERR_INVALID_ARG, lib().hsap_last_error().decode())
+    return v
+
+
+def cache_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_new, o_out, lse_out, workspace,
+               window: int = MAX_WINDOW, sinks: int = 0, stream=None) -> None:
+    """hsap_cache_attn: q bf16 [total_q, Hq, d] (rows may be strided; the sequences' newest tokens) over the cache ->
+    o_out bf16 [total_q, Hq, d], lse_out fp32 [Hq, total_q] or None; workspace: uint8, cache_attn_workspace bytes."""
+    c = cache.desc
+    total = q.shape[0]
+    qs = _token_rows(q, "q", total, int(heads_q), c.head_dim)
+    if cu_new is not None:
+        _dev(cu_new, "int32", "cu_new", c.num_seqs + 1)
+    _dev(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim)
+    if lse_out is not None:
+        _dev(lse_out, "float32", "lse_out", total * heads_q)
+    _dev(workspace, "uint8", "workspace")
+    _one_device(q, cu_new, o_out, lse_out, workspace, cache.tensors[0])
+    _check(lib().hsap_cache_attn(ctypes.byref(c), ctypes.byref(cache.buffers), int(heads_q), float(softmax_scale),
+                                 _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q), qs, _ptr(cu_new), total,
+                                 _ptr(o_out), _ptr(lse_out), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,538 @@
+// Attention of the newest tokens over the paged 8-bit K/V cache.
+//
+//   s_j = scale ks(page of j) q . k8_j,   O = sum_j exp(s_j - LSE) vs(page of j) v8_j
+//
+// Few rows against many cached tokens: bound by reading the codes, 2 d bytes per token and K/V head.  So the query
+// heads of a K/V head (and a sequence's several new tokens) share one pass: rows r = (token, head of the group) in
+// tiles of 16 MT, one workgroup per (row tile, K/V head, split of the tile's tokens), a running maximum and sum per
+// wave, the waves' results joined in LDS, the splits' by a second launch over fp32 partials.
+//
+// A wave takes 32 tokens at a time (its workgroup's four waves take turns), with the next ones' codes in flight in
+// registers: no LDS on the way.  S^T = K Q^T by 16x16x32 products, tokens as rows: lane l holds row l % 16 of K and
+// of Q, sixteen of a token's values at a time (the order of d is the same for both, so any will do).  The result
+// has query l % 16 on lane l and tokens 4 (l / 16) .. +3 of each 16, which is the layout of the B operand of
+// O^T += V^T P^T if its eight tokens per lane are 4 (l / 16) + 0..3 of both halves; V's rows are loaded by those tokens
+// and turned in registers, two codes of two tokens at a time (v_perm, then the conversion to bf16, which e4m3 fits
+// exactly).
+#include <algorithm>
+#include <type_traits>
+
+#include "cache.h"
+#include "hsap_internal.h"
+#include "mfma.h"
+
+namespace hsap {
+
+hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c);
+
+struct CacheAttnArgs {
+  hsap_cache_desc d;
+  hsap_cache c;
+  const __bf16* q;
+  int64_t q_stride;
+  const int32_t* cu;
+  int64_t total_q;
+  __bf16* o;
+  float* lse;      // may be NULL
+  float* part_o;   // [splits, total_q, Hq, d], normalised
+  float* part_lse; // [splits, total_q, Hq], log2 units
+  int32_t heads_q;
+  int32_t group;
+  int32_t window;
+  int32_t sinks;
+  int32_t tiles;   // row tiles, all sequences
+  int32_t splits;
+  float scale_log2;
+};
+
+// Token ranges that the rows at positions plo .. phi of one sequence see, in steps of 32: the sinks' from 0 on, then the
+// windows'.  Tokens at or behind cap are in no page.
+struct Steps {
+  int32_t sinks;   // sink steps
+  int32_t win0;    // first token of the window steps (a multiple of 32)
+  int32_t total;
+};
+
+__device__ __forceinline__ Steps cache_steps(int32_t plo, int32_t phi, int32_t cap, int32_t window, int32_t sinks) {
+  phi = min(phi, cap - 1);
+  if (phi < 0) return Steps{0, 0, 0};
+  const int32_t lo = max(0, max(plo, 0) - (window - 1));
+  const int32_t win0 = min(lo, phi + 1) & ~31;
+  const int32_t ns = (min(sinks, win0) + 31) / 32;
+  return Steps{ns, win0, ns + (phi >= win0 ? (phi - win0) / 32 + 1 : 0)};
+}
+
+// Splits that have work, of `total` steps dealt to at most `splits`, and the steps of each.
+__device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// four e4m3 codes to bf16 (exact)
+__device__ __forceinline__ void decode4(uint32_t w, bf16x2& lo, bf16x2& hi) {
+  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true);
+}
+
+__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// The sequence, first row and rows of a row tile; false where the tile is empty.
+struct RowTile {
+  int32_t seq, t0, count, row0;  // row0: first row (token * group + head) of the tile within the sequence
+};
+__device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, int rows, RowTile& t) {
+  if (!a.cu) {
+    const int32_t per = (a.group + rows - 1) / rows;
+    t.seq = tile / per;
+    t.t0 = t.seq;
+    t.count = 1;
+    t.row0 = (tile - t.seq * per) * rows;
+    return t.seq < a.d.num_seqs;
+  }
+  int32_t s = 0, r = a.d.num_seqs;
+  while (r - s > 1) {
+    const int32_t mid = (s + r) >> 1;
+    if (item_base(a.cu[mid], a.group, rows, 1, mid) <= tile) s = mid;
+    else r = mid;
+  }
+  t.seq = s;
+  t.t0 = a.cu[s];
+  t.count = (int32_t)min((int64_t)a.cu[s + 1], a.total_q) - t.t0;
+  const int64_t row0 = (tile - item_base(t.t0, a.group, rows, 1, s)) * rows;
+  t.row0 = (int32_t)row0;
+  return t.count > 0 && row0 < (int64_t)t.count * a.group;
+}
+
+template <int D, int MT>
+__global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) void cache_attn_kernel(CacheAttnArgs a) {
+  constexpr int KX = D / 64, CB = D / 16, ROWS = 16 * MT;  // 16-byte loads per K row and lane; d values per lane of V
+  constexpr float NEG_INF = -__builtin_inff();
+  constexpr float RESCALE_SLACK = 8.f;
+  using VT = typename std::conditional<D == 128, uint2, uint32_t>::type;  // a lane's CB codes of a V row
+  constexpr int SLOT = MT * (CB * 4 + 2) * 64;                          // floats of one wave's results
+  __shared__ float join[2 * SLOT];
+
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = blockIdx.x % a.d.heads_kv;
+  const int32_t rest = blockIdx.x / a.d.heads_kv;
+  const int32_t split = rest % a.splits, tile = rest / a.splits;
+  RowTile rt;
+  if (!row_tile(a, tile, ROWS, rt)) return;
+  const int32_t len = max(0, a.c.seq_lens[rt.seq]);
+  const int32_t ps = a.d.page_size, cap = a.d.table_width * ps;
+  const int32_t nrows = rt.count * a.group;
+  const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
+  const int32_t pos0 = len - rt.count;  // position of the sequence's first new token
+  const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
+  const Steps steps = cache_steps(plo, phi, cap, a.window, a.sinks);
+  const int32_t per = steps_per_split(steps.total, a.splits);
+  const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
+  if (s_begin >= s_end && split > 0) return;  // (split 0 writes the rows of a tile that sees nothing)
+
+  // this lane's query of each 16-row block: row, position, Q fragments
+  int32_t pos[MT];
+  bf16x8 qf[MT][2 * KX];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int32_t r = min(rt.row0 + 16 * mt + l16, nrows - 1);
+    const int32_t t = r / a.group;
+    pos[mt] = pos0 + t;
+    const __bf16* qp = a.q + (int64_t)(rt.t0 + t) * a.q_stride + (int64_t)(g * a.group + (r - t * a.group)) * D + 16 * grp;
+#pragma unroll
+    for (int x = 0; x < KX; ++x) {
+      qf[mt][2 * x] = *(const bf16x8*)(qp + 64 * x);
+      qf[mt][2 * x + 1] = *(const bf16x8*)(qp + 64 * x + 8);
+    }
+  }
+  const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
+  const int32_t top = min(phi, cap - 1);  // last token any row sees
+
+  struct Tokens {
+    uint4 k[2][KX];
+    VT v[8];
+    float ks[2], vs[2];
+    int32_t j0;
+    bool held[2];  // each half of 16 tokens lies in a page and has a token that is seen
+  };
+  auto load = [&](int32_t s, Tokens& x) __attribute__((always_inline)) {
+    x.j0 = s < steps.sinks ? 32 * s : steps.win0 + 32 * (s - steps.sinks);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int32_t j = x.j0 + 16 * half;
+      const int32_t found = j <= top ? cache_page(table, a.d.table_width, a.d.num_pages, ps, j) : -1;
+      const int32_t page = max(found, 0);
+      const int64_t at = (int64_t)page * a.d.heads_kv + g;
+      x.ks[half] = a.c.k_scale[at];
+      x.vs[half] = a.c.v_scale[at];
+      x.held[half] = found >= 0;
+      if (found < 0) x.ks[half] = x.vs[half] = 0.f;
+      const int64_t row = at * ps + (j & (ps - 1));
+      const uint8_t* kp = a.c.k_codes + (row + l16) * D + 16 * grp;
+#pragma unroll
+      for (int y = 0; y < KX; ++y) x.k[half][y] = *(const uint4*)(kp + 64 * y);
+      const uint8_t* vp = a.c.v_codes + (row + 4 * grp) * D + CB * l16;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x.v[4 * half + y] = *(const VT*)(vp + y * D);
+    }
+  };
+
+  float m_run[MT], l_run[MT];
+  f32x4 o[MT][CB];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m_run[mt] = NEG_INF;
+    l_run[mt] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) o[mt][c] = f32x4{};
+  }
+
+  auto compute = [&](const Tokens& x, int32_t s) __attribute__((always_inline)) {
+    // K operand: eight codes of a token per product
+    bf16x8 kf[2][2 * KX];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int y = 0; y < KX; ++y) {
+        const uint32_t c[4] = {x.k[half][y].x, x.k[half][y].y, x.k[half][y].z, x.k[half][y].w};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          bf16x2 p0, p1, p2, p3;
+          decode4(c[2 * e], p0, p1);
+          decode4(c[2 * e + 1], p2, p3);
+          kf[half][2 * y + e] = bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+        }
+      }
+    const int32_t jl = x.j0 + 31;
+    // tokens that the sink steps show belong to them alone; a window step's may be sinks too
+    const int32_t sinks = s < steps.sinks ? min(a.sinks, steps.win0) : a.sinks;
+    const int32_t near = s < steps.sinks ? 0 : a.window;
+    bf16x8 pf[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      f32x4 sc[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int kk = 0; kk < 2 * KX; ++kk) sc[half] = mfma16(kf[half][kk], qf[mt][kk], sc[half]);
+      const bool all = x.held[0] && x.held[1] && jl <= pos[mt] && (pos[mt] - x.j0 < near || jl < sinks);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) sc[half] *= x.ks[half] * a.scale_log2;
+      if (__builtin_amdgcn_ballot_w64(!all) != 0) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int32_t j = x.j0 + 16 * half + 4 * grp + e;
+            const bool see = j <= pos[mt] && (pos[mt] - j < near || j < sinks) && x.held[half];
+            if (!see) sc[half][e] = NEG_INF;
+          }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      // a row's tokens lie on four lanes; its maximum is joined only when some lane's rose by more than the slack
+      if (__builtin_amdgcn_ballot_w64(mx > m_run[mt] + RESCALE_SLACK) != 0) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m_run[mt], mx);
+        const float alpha = m_run[mt] == NEG_INF ? 0.f : fast_exp2(m_run[mt] - m_new);
+        l_run[mt] *= alpha;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[mt][c] *= alpha;
+        m_run[mt] = m_new;
+      }
+      const float m_use = m_run[mt] == NEG_INF ? 0.f : m_run[mt];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = fast_exp2(sc[half][e] - m_use);
+          l_run[mt] += p;
+          pf[mt][4 * half + e] = (__bf16)(p * x.vs[half]);
+        }
+    }
+    // V operand: rows d = CB l16 + c, the lane's eight tokens
+    VT v[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) v[y] = x.v[y];
+    if (jl > top || !x.held[0] || !x.held[1]) {  // what lies behind the last token is whatever the page held before
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        if (x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3) > top || !x.held[y >> 2]) v[y] = VT{};
+    }
+#pragma unroll
+    for (int c4 = 0; c4 < CB / 4; ++c4) {
+      bf16x2 turned[4][4];  // [column][token pair]
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t u0, u1;
+        if constexpr (D == 128) {
+          u0 = c4 ? v[2 * y].y : v[2 * y].x;
+          u1 = c4 ? v[2 * y + 1].y : v[2 * y + 1].x;
+        } else {
+          u0 = v[2 * y];
+          u1 = v[2 * y + 1];
+        }
+        // bytes (u0.0, u1.0, u0.1, u1.1) and (u0.2, u1.2, u0.3, u1.3): v_perm selects 0..3 from its second operand
+        const uint32_t lo = __builtin_amdgcn_perm(u1, u0, 0x05010400u), hi = __builtin_amdgcn_perm(u1, u0, 0x07030602u);
+        decode4(lo, turned[0][y], turned[1][y]);
+        decode4(hi, turned[2][y], turned[3][y]);
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bf16x8 vf{turned[c][0][0], turned[c][0][1], turned[c][1][0], turned[c][1][1],
+                        turned[c][2][0], turned[c][2][1], turned[c][3][0], turned[c][3][1]};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) o[mt][4 * c4 + c] = mfma16(vf, pf[mt], o[mt][4 * c4 + c]);
+      }
+    }
+  };
+
+  int32_t s = s_begin + w;
+  if (s < s_end) {
+    Tokens x, y;
+    load(s, x);
+    for (;;) {
+      const bool more = s + 4 < s_end;
+      if (more) load(s + 4, y);
+      compute(x, s);
+      if (!more) break;
+      s += 4;
+      x = y;
+    }
+  }
+
+  // join the four waves: 2 and 3 hand theirs to 0 and 1, then 1 to 0
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    l_run[mt] += __shfl_xor(l_run[mt], 16);
+    l_run[mt] += __shfl_xor(l_run[mt], 32);
+  }
+#pragma unroll
+  for (int turn = 0; turn < 2; ++turn) {
+    const int half = turn == 0 ? 2 : 1;
+    if (w >= half && w < 2 * half) {
+      float* out = join + (w - half) * SLOT + lane;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        out[(mt * (CB * 4 + 2)) * 64] = m_run[mt];
+        out[(mt * (CB * 4 + 2) + 1) * 64] = l_run[mt];
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[(mt * (CB * 4 + 2) + 2 + 4 * c + e) * 64] = o[mt][c][e];
+      }
+    }
+    __syncthreads();
+    if (w < half) {
+      const float* in = join + w * SLOT + lane;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const float m2 = in[(mt * (CB * 4 + 2)) * 64], l2 = in[(mt * (CB * 4 + 2) + 1) * 64];
+        const float m = fmaxf(m_run[mt], m2), m_use = m == NEG_INF ? 0.f : m;
+        const float f1 = fast_exp2(m_run[mt] - m_use), f2 = fast_exp2(m2 - m_use);
+        l_run[mt] = l_run[mt] * f1 + l2 * f2;
+        m_run[mt] = m;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[mt][c][e] = o[mt][c][e] * f1 + in[(mt * (CB * 4 + 2) + 2 + 4 * c + e) * 64] * f2;
+      }
+    }
+    __syncthreads();
+  }
+  if (w != 0) return;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int32_t r = rt.row0 + 16 * mt + l16;
+    if (r >= nrows) continue;
+    const int32_t t = r / a.group;
+    const int64_t tok = rt.t0 + t;
+    const int h = g * a.group + (r - t * a.group);
+    const float inv = l_run[mt] > 0.f ? 1.f / l_run[mt] : 0.f;
+    const float lse2 = l_run[mt] > 0.f ? m_run[mt] + __log2f(l_run[mt]) : NEG_INF;
+    const int64_t row = tok * a.heads_q + h;
+    if (a.splits == 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __bf16* op = a.o + row * D + CB * (4 * grp + e);
+#pragma unroll
+        for (int c = 0; c < CB; c += 4)
+          *(bf16x4*)(op + c) = bf16x4{(__bf16)(o[mt][c][e] * inv), (__bf16)(o[mt][c + 1][e] * inv),
+                                      (__bf16)(o[mt][c + 2][e] * inv), (__bf16)(o[mt][c + 3][e] * inv)};
+      }
+      if (grp == 0 && a.lse) a.lse[(int64_t)h * a.total_q + tok] = lse2 * 0.69314718055994530942f;
+    } else {
+      const int64_t at = (int64_t)split * a.total_q * a.heads_q + row;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float* op = a.part_o + at * D + CB * (4 * grp + e);
+#pragma unroll
+        for (int c = 0; c < CB; c += 4)
+          *(f32x4*)(op + c) = f32x4{o[mt][c][e] * inv, o[mt][c + 1][e] * inv, o[mt][c + 2][e] * inv, o[mt][c + 3][e] * inv};
+      }
+      if (grp == 0) a.part_lse[at] = lse2;
+    }
+  }
+}
+
+// Joins the splits of every row: one wave per row, D / 64 values per lane.  The number of splits with work follows
+// from the row's tile, as in the kernel above.
+template <int D>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a, int rows_per_tile) {
+  constexpr int E = D / 64;
+  constexpr float NEG_INF = -__builtin_inff();
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t rows = a.total_q * a.heads_q;
+  if (row >= rows) return;
+  const int64_t tok = row / a.heads_q;
+  const int h = (int)(row - tok * a.heads_q);
+  int32_t seq, t0, count;
+  if (a.cu) {
+    int32_t l = 0, r = a.d.num_seqs;
+    if (tok >= a.cu[r]) return;
+    while (r - l > 1) {
+      const int32_t mid = (l + r) >> 1;
+      if (a.cu[mid] <= tok) l = mid;
+      else r = mid;
+    }
+    seq = l;
+    t0 = a.cu[l];
+    count = (int32_t)min((int64_t)a.cu[l + 1], a.total_q) - t0;
+  } else {
+    seq = t0 = (int32_t)tok;
+    count = 1;
+  }
+  const int32_t len = max(0, a.c.seq_lens[seq]), pos0 = len - count;
+  const int32_t r = (int32_t)(tok - t0) * a.group + h % a.group;
+  const int32_t row0 = r / rows_per_tile * rows_per_tile, last = min(row0 + rows_per_tile, count * a.group) - 1;
+  const Steps steps = cache_steps(pos0 + row0 / a.group, pos0 + last / a.group, a.d.table_width * a.d.page_size, a.window, a.sinks);
+  const int32_t per = steps_per_split(steps.total, a.splits);
+  const int32_t live = per > 0 ? (steps.total + per - 1) / per : 1;
+  float m = NEG_INF, sum = 0.f, acc[E] = {};
+  for (int32_t s = 0; s < live; ++s) {
+    const int64_t at = (int64_t)s * rows + row;
+    const float l = a.part_lse[at];
+    if (l == NEG_INF) continue;
+    const float m_new = fmaxf(m, l), f1 = fast_exp2(m - m_new), f2 = fast_exp2(l - m_new);
+    sum = sum * f1 + f2;
+    m = m_new;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = acc[e] * f1 + a.part_o[at * D + E * lane + e] * f2;
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) a.o[row * D + E * lane + e] = (__bf16)(acc[e] * inv);
+  if (lane == 0 && a.lse) a.lse[(int64_t)h * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
+}
+
+// How a call is cut: row tiles of 16 mt rows, and splits of a tile's tokens so that the grid fills the chip, each of
+// at least 256 tokens.
+struct CacheCut {
+  int mt;
+  int64_t tiles;
+  int32_t splits;
+};
+
+static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
+  CacheCut c;
+  const int64_t group = heads_q / d.heads_kv;
+  const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
+  c.mt = rows > 32 ? 4 : rows > 16 ? 2 : 1;
+  c.tiles = one_each ? (int64_t)d.num_seqs * ((group + 16 * c.mt - 1) / (16 * c.mt))
+                     : item_base(total_q, group, 16 * c.mt, 1, d.num_seqs);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, tokens / 256));
+  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, 1024 / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+  return c;
+}
+
+static int64_t cache_workspace(const CacheCut& c, int32_t heads_q, int64_t total_q, int head_dim) {
+  return c.splits == 1 ? 0 : (int64_t)c.splits * total_q * heads_q * (head_dim + 1) * 4;
+}
+
+template <int D, int MT>
+static void launch_cache_attn(const CacheAttnArgs& a, int64_t blocks, hipStream_t s) {
+  hipLaunchKernelGGL((cache_attn_kernel<D, MT>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+}
+
+}  // namespace hsap
+
+using namespace hsap;
+
+extern "C" int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
+  clear_error();
+  if (!desc || heads_q < 1 || total_q < 0 || desc->heads_kv < 1 || heads_q % desc->heads_kv || desc->num_seqs < 0 ||
+      desc->table_width < 1 || (desc->head_dim != 64 && desc->head_dim != 128) || desc->page_size < 1) {
+    set_error("bad cache or head counts");
+    return -1;
+  }
+  const CacheCut c = cache_cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
+  return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
+}
+
+extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
+                                       int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
+                                       int64_t total_q, void* o_out, float* lse_out, void* workspace, int64_t workspace_bytes,
+                                       void* hip_stream) {
+  clear_error();
+  hsap_status st = check_cache(desc, cache);
+  if (st != HSAP_OK) return st;
+  const int d = desc->head_dim;
+  if (heads_q < 1 || heads_q % desc->heads_kv)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "heads_q=%d must be a positive multiple of heads_kv=%d", heads_q, desc->heads_kv);
+  if (!(softmax_scale > 0.f) || softmax_scale > 1e30f) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (window < 1) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "window %d < 1 (a query always sees itself)", window);
+  if (sinks < 0) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "sinks %d < 0", sinks);
+  if (total_q < 0 || total_q * heads_q > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_q %lld", (long long)total_q);
+  if (!cu_new && total_q != desc->num_seqs)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "without cu_new every sequence has one row: total_q %lld, num_seqs %d", (long long)total_q,
+              desc->num_seqs);
+  if (total_q == 0 || desc->num_seqs == 0) return HSAP_OK;
+  if (!q || !o_out || !workspace) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
+  if (((uintptr_t)q | (uintptr_t)o_out | (uintptr_t)workspace) & 15)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "q, o_out and workspace must be 16-byte aligned");
+  if (q_stride % 8 || q_stride < (int64_t)heads_q * d)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "q_stride %lld must be a multiple of 8 and at least %lld", (long long)q_stride,
+              (long long)heads_q * d);
+  const CacheCut c = cache_cut(*desc, heads_q, total_q, !cu_new, (int64_t)desc->table_width * desc->page_size);
+  const int64_t need = cache_workspace(c, heads_q, total_q, d);
+  if (workspace_bytes < need)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+  CacheAttnArgs a{};
+  a.d = *desc;
+  a.c = *cache;
+  a.q = (const __bf16*)q;
+  a.q_stride = q_stride;
+  a.cu = cu_new;
+  a.total_q = total_q;
+  a.o = (__bf16*)o_out;
+  a.lse = lse_out;
+  a.part_o = (float*)workspace;
+  a.part_lse = a.part_o + (int64_t)c.splits * total_q * heads_q * d;
+  a.heads_q = heads_q;
+  a.group = heads_q / desc->heads_kv;
+  a.window = window;
+  a.sinks = sinks;
+  a.tiles = (int32_t)c.tiles;
+  a.splits = c.splits;
+  a.scale_log2 = softmax_scale * 1.44269504088896340736f;
+  const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
+  if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (d == 128) c.mt == 1 ? launch_cache_attn<128, 1>(a, blocks, s) : c.mt == 2 ? launch_cache_attn<128, 2>(a, blocks, s)
+                                                                                 : launch_cache_attn<128, 4>(a, blocks, s);
+  else c.mt == 1 ? launch_cache_attn<64, 1>(a, blocks, s) : c.mt == 2 ? launch_cache_attn<64, 2>(a, blocks, s)
+                                                                       : launch_cache_attn<64, 4>(a, blocks, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
+  if (c.splits > 1) {
+    const dim3 grid((unsigned)((total_q * heads_q + 3) / 4));
+    if (d == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, grid, dim3(256), 0, s, a, 16 * c.mt);
+    else hipLaunchKernelGGL(cache_merge_kernel<64>, grid, dim3(256), 0, s, a, 16 * c.mt);
+    e = hipGetLastError();
+    if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn merge launch: %s", hipGetErrorString(e));
+  }
+  return HSAP_OK;
+}

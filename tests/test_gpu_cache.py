@@ -1,0 +1,350 @@
+"""The paged 8-bit cache on the GPU: appends bit for bit against the fp32 model of the oracle (and within the bounds of
+64 bits), attention over it within the oracle's derived bounds; ragged and idle sequences, pages of every size, bad and
+handed-back pages, garbage in unused places, windows, many rows, split contexts, replays, and the run of prompt and
+tokens as a server makes it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import cache as C
+from paper_2606_30460_amd import _lib as L
+
+pytestmark = pytest.mark.gpu
+
+
+def _bits(t):
+    return t.cpu().numpy()
+
+
+class Pages:
+    """A cache with room for `lens` (total tokens per sequence), pages in random order; unused places hold NaN."""
+
+    def __init__(self, lens, size, hkv, d, seed=0, spare=3, width=None):
+        rng = np.random.default_rng(seed)
+        per = [-(-int(n) // size) for n in lens]
+        pages = sum(per) + spare
+        order = rng.permutation(pages)
+        self.table = np.full((len(lens), width or max(1, max(per, default=1))), -1, dtype=np.int32)
+        at = 0
+        for s, n in enumerate(per):
+            self.table[s, :n] = order[at:at + n]
+            at += n
+        self.size, self.hkv, self.d, self.lens = size, hkv, d, np.asarray(lens)
+        shape = (pages, hkv, size, d)
+        self.codes = {x: np.full(shape, 0x7F, dtype=np.uint8) for x in "kv"}
+        self.scales = {x: np.full(shape[:2], np.nan, dtype=np.float32) for x in "kv"}
+
+    def fill(self, upto, seed=1, spread=1.0):
+        """The first upto[s] tokens of each sequence: normal values."""
+        rng = np.random.default_rng(seed)
+        for x in "kv":
+            for s, n in enumerate(upto):
+                n = max(0, int(n))
+                if n:
+                    val = (rng.standard_normal((n, self.hkv, self.d)) * np.exp(spread * rng.standard_normal((n, 1, 1))) * 0.7)
+                    C.append(self.codes[x], self.scales[x], self.table, [(s, p) for p in range(n)], val.astype(np.float32))
+        return self
+
+    def device(self, lens=None):
+        t = {x + "_codes": torch.from_numpy(self.codes[x].copy()).cuda() for x in "kv"}
+        t |= {x + "_scale": torch.from_numpy(self.scales[x].copy()).cuda() for x in "kv"}
+        lens = torch.from_numpy(np.asarray(self.lens if lens is None else lens).astype(np.int32)).cuda()
+        return L.KVCache(t["k_codes"], t["v_codes"], t["k_scale"], t["v_scale"], torch.from_numpy(self.table).cuda(), lens)
+
+
+def _cos_sin(rows, rot):
+    f = 100.0 ** (-np.arange(rot // 2) * 2.0 / max(rot, 1))
+    a = np.arange(rows)[:, None] * f
+    return torch.from_numpy(np.concatenate([np.cos(a), np.sin(a)], 1).astype(np.float32)).cuda()
+
+
+def _check_append(held, new, size, hkv, d, rot, interleaved=False, hq=0, k_out=False, one=False, rows=None, seed=0, width=None,
+                  pad=0, spread=1.0, break_page=None):
+    held, new = np.asarray(held), np.asarray(new)
+    total = held + new
+    p = Pages(np.maximum(total, 0), size, hkv, d, seed, width=width).fill(held, seed + 1)
+    if break_page is not None:
+        p.table[break_page] = 10 ** 6
+    n = int(new.sum())
+    g = torch.Generator().manual_seed(seed)
+    fused = torch.randn(n + pad, hq + 2 * hkv, d, generator=g) * torch.exp(spread * torch.randn(n + pad, 1, 1, generator=g))
+    fused = fused.to(torch.bfloat16).cuda()
+    q, k, v = fused[:, :hq], fused[:, hq:hq + hkv], fused[:, hq + hkv:]
+    rows = int(total.max(initial=1)) + 1 if rows is None else rows
+    cs = _cos_sin(rows, rot) if rot else None
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    cache = p.device(total)
+    q_out = torch.full((n + pad, hq, d), 7.0, dtype=torch.bfloat16, device="cuda") if hq else None
+    ko = torch.full((n + pad, hkv, d), 7.0, dtype=torch.bfloat16, device="cuda") if k_out else None
+    L.cache_append(cache, k, v, None if one else torch.from_numpy(cu).cuda(), cos_sin=cs, interleaved=interleaved, k_out=ko,
+                   q=q if hq else None, q_out=q_out)
+    torch.cuda.synchronize()
+    seq = np.repeat(np.arange(len(new)), new)
+    pos = np.concatenate([np.arange(a, a + b) for a, b in zip(held, new)] + [np.zeros(0)]).astype(np.int64)
+    live = (pos >= 0) & ((pos < rows) if rot else True)
+    row_of = _bits(cs)[np.clip(pos, 0, rows - 1)][:, None] if rot else np.zeros((n, 1, 0), np.float32)
+    host = {x: t.float().cpu().numpy()[:n] for x, t in (("q", q), ("k", k), ("v", v))}
+    turned = {x: C.rotate(host[x], row_of, interleaved, np.float32) for x in "qk"}
+    turned["v"] = host["v"]
+    for x in "kv":
+        C.append(p.codes[x], p.scales[x], p.table, [(s, int(a)) if ok else (s, -1) for s, a, ok in zip(seq, pos, live)], turned[x])
+    for x, codes, scale in (("k", cache.k_codes, cache.k_scale), ("v", cache.v_codes, cache.v_scale)):
+        assert np.array_equal(_bits(scale), p.scales[x], equal_nan=True), x
+        assert np.array_equal(_bits(codes), p.codes[x]), x
+    for t, x in ((q_out, "q"), (ko, "k")):
+        if t is None:
+            continue
+        want = torch.from_numpy(turned[x]).to(torch.bfloat16).float().numpy()
+        want[~live] = 7.0
+        assert np.array_equal(t.float().cpu().numpy()[:n], want), x
+        assert bool((t[n:] == 7.0).all())
+        wide = C.rotate(host[x], row_of, interleaved)          # 64 bits: half a bf16 step and the fp32 operations
+        assert (np.abs(want - wide) <= 2.0 ** -8 * np.abs(wide) + 2.0 ** -20 * np.abs(host[x]).max(-1, keepdims=True))[live].all()
+    return p, cache
+
+
+@pytest.mark.parametrize("d,rot,interleaved", [(64, 0, False), (64, 64, False), (128, 128, True), (128, 64, False), (64, 16, True)])
+@pytest.mark.parametrize("size", [16, 32, 64, 128])
+def test_append_ragged(size, d, rot, interleaved):
+    print(size, d, rot, interleaved, flush=True)
+    _check_append([0, 5, 16, 31, 100, 0, 127], [1, 11, 130, 0, 17, 300, 2], size, 3, d, rot, interleaved, hq=6, k_out=True,
+                  seed=size, pad=5)
+
+
+@pytest.mark.parametrize("d,rot", [(64, 64), (128, 32), (128, 0)])
+@pytest.mark.parametrize("seqs", [1, 7, 70])
+def test_append_one_token_each(seqs, d, rot):
+    print(seqs, d, rot, flush=True)
+    held = np.random.default_rng(seqs).integers(0, 90, seqs)
+    held[0] = 64                                  # a page begun anew
+    if seqs > 2:
+        held[2] = -1                              # an idle slot: length 0
+    new = np.ones(seqs, dtype=int)
+    _check_append(held, new, 64, 2, d, rot, hq=5, k_out=True, one=True, seed=seqs, spread=2.0)
+    _check_append(held, new, 64, 2, d, rot, hq=5, one=False, seed=seqs + 1, spread=2.0)
+
+
+def test_append_beyond_the_rotation_rows_the_table_and_the_pages():
+    _check_append([3, 10, 0], [20, 30, 5], 16, 2, 64, 64, hq=2, k_out=True, rows=25)          # positions 25.. are skipped
+    _check_append([3, 30], [60, 1], 16, 2, 64, 64, hq=2, k_out=True, width=4)                 # all fits
+    _check_append([3, 30], [20, 30], 16, 2, 64, 32, hq=2, k_out=True, break_page=(1, 2))      # no page: not cached
+    _check_append([30, 3], [1, 1], 16, 2, 64, 32, hq=2, k_out=True, break_page=(0, 1), one=True)
+    p = Pages([64, 40], 16, 2, 64, width=4).fill([10, 40])
+    cache = p.device([100, 41])                                                               # longer than the table
+    k = torch.randn(91, 2, 64, device="cuda").to(torch.bfloat16)
+    L.cache_append(cache, k, k, torch.tensor([0, 90, 91], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for x in "kv":
+        C.append(p.codes[x], p.scales[x], p.table, [(0, 10 + t) for t in range(54)], k[:54].float().cpu().numpy())
+        C.append(p.codes[x], p.scales[x], p.table, [(1, 40)], k[90:].float().cpu().numpy())
+    assert np.array_equal(_bits(cache.k_codes), p.codes["k"]) and np.array_equal(_bits(cache.v_codes), p.codes["v"])
+
+
+def test_append_of_extreme_values():
+    vals = torch.tensor([0.0, 3.0e38, -3.0e38, 1e-38, 2.0 ** -133, float("inf"), -float("inf"), float("nan"), 448.0, 449.0, 1.0, -0.0])
+    for i in range(len(vals)):
+        p = Pages([20], 16, 1, 64)
+        k = torch.zeros(20, 1, 64)
+        k[3, 0, :12] = vals.roll(i)
+        k[7, 0, 5] = vals[i]
+        k = k.to(torch.bfloat16).cuda()
+        cache = p.device()
+        L.cache_append(cache, k, k[:, :, torch.randperm(64)].contiguous(), torch.tensor([0, 20], dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        C.append(p.codes["k"], p.scales["k"], p.table, [(0, t) for t in range(20)], k.float().cpu().numpy())
+        got, want = (oracle.decode_fp8(c[p.table[0]]) for c in (_bits(cache.k_codes), p.codes["k"]))
+        assert np.array_equal(got, want, equal_nan=True), i
+        assert np.array_equal(_bits(cache.k_scale), p.scales["k"], equal_nan=True)
+    zero = Pages([16], 16, 1, 64)
+    cache = zero.device()
+    z = torch.zeros(16, 1, 64, dtype=torch.bfloat16, device="cuda")
+    L.cache_append(cache, z, z, torch.tensor([0, 16], dtype=torch.int32, device="cuda"))
+    assert float(cache.k_scale[zero.table[0, 0], 0]) == 2.0 ** -100 and bool((cache.k_codes[zero.table[0, 0]] == 0).all())
+
+
+def test_token_by_token_equals_the_model():
+    p = Pages([50, 50], 16, 2, 64, seed=3)
+    cache = p.device([0, 0])
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randn(50, 2, 2, 64, generator=g) * torch.exp(torch.randn(50, 2, 1, 1, generator=g) * 2)).to(torch.bfloat16)
+    for t in range(50):
+        cache.seq_lens.fill_(t + 1)
+        L.cache_append(cache, x[t].cuda(), (2 * x[t]).cuda(), None)
+        C.append(p.codes["k"], p.scales["k"], p.table, [(0, t), (1, t)], x[t].float().numpy())
+        C.append(p.codes["v"], p.scales["v"], p.table, [(0, t), (1, t)], 2 * x[t].float().numpy())
+    torch.cuda.synchronize()
+    assert np.array_equal(_bits(cache.k_codes), p.codes["k"]) and np.array_equal(_bits(cache.v_codes), p.codes["v"])
+    assert np.array_equal(_bits(cache.k_scale), p.scales["k"], equal_nan=True)
+
+
+def _check_attn(lens, new, size, hq, hkv, d, window=L.MAX_WINDOW, sinks=0, seed=0, one=False, pad=0, width=None, pages=None,
+                scale=None, strided=False, lse=True):
+    lens, new = np.asarray(lens), np.asarray(new)
+    p = pages or Pages(np.maximum(lens, 0), size, hkv, d, seed, width=width).fill(np.maximum(lens, 0), seed + 1)
+    n = int(new.sum())
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randn(n + pad, hq + (3 if strided else 0), d, generator=g).to(torch.bfloat16).cuda()
+    q = q[:, 1:1 + hq] if strided else q
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    cache = p.device(lens)
+    o = torch.full((n + pad, hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ls = torch.full((hq, n + pad), 7.0, device="cuda") if lse else None
+    ws = torch.full((L.cache_attn_workspace(cache, hq, n + pad),), 0xFF, dtype=torch.uint8, device="cuda")
+    scale = scale or 1 / math.sqrt(d)
+    L.cache_attn(cache, hq, scale, q, None if one else torch.from_numpy(cu).cuda(), o, ls, ws, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    want, tol, want_l, tol_l = C.attention(q[:n].float().double().cpu().numpy(), p.codes["k"], p.scales["k"], p.codes["v"],
+                                           p.scales["v"], p.table, lens, cu, window, sinks, scale)
+    err = np.abs(o[:n].float().cpu().numpy() - want)
+    assert (err <= tol + 1e-9).all(), float((err / (tol + 1e-9)).max())
+    assert bool((o[n:] == 7.0).all())
+    if lse:
+        got = ls.cpu().numpy()
+        none = np.isinf(want_l)
+        assert np.array_equal(got[:, :n][none], want_l[none])
+        assert (np.abs(got[:, :n] - np.where(none, 0, want_l))[~none] <= tol_l[~none]).all()
+        assert (got[:, n:] == 7.0).all()
+    return o
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [16, 32, 64, 128])
+def test_one_row_each(size, d):
+    print(size, d, flush=True)
+    _check_attn([1, 2, 15, 16, 17, 31, 32, 33, 63, 100, 129, 0, 600], np.ones(13, int), size, 8, 2, d, one=True, seed=size)
+    _check_attn([1, 2, 15, 16, 17, 31, 32, 33, 63, 100, 129, 0, 600], np.ones(13, int), size, 3, 3, d, pad=2, strided=True, lse=False)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 1), (16, 1), (17, 1), (40, 1), (80, 1), (24, 8), (6, 3)])
+def test_groups(hq, hkv):
+    print(hq, hkv, flush=True)
+    _check_attn([70, 300], [1, 1], 32, hq, hkv, 128, one=True, seed=hq)
+    _check_attn([70, 300], [3, 7], 32, hq, hkv, 64, seed=hq)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (33, 40), (100, 0), (1000, 5), (50, 1000)])
+def test_windows_and_sinks(window, sinks):
+    print(window, sinks, flush=True)
+    _check_attn([1, 40, 130, 333, 700], np.ones(5, int), 16, 4, 1, 64, window, sinks, one=True)
+    _check_attn([10, 40, 130, 333, 700], [10, 1, 0, 50, 129], 64, 4, 2, 128, window, sinks, pad=1)
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 8, 1), (128, 2, 2)])
+def test_many_rows(d, hq, hkv):
+    print(d, hq, hkv, flush=True)
+    _check_attn([200, 37, 128], [200, 5, 64], 32, hq, hkv, d, seed=7)       # a whole prompt, a few, a chunk
+    _check_attn([5, 3], [9, 3], 16, hq, hkv, d, seed=8)                     # more rows than tokens: the first see nothing
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_split_contexts(d):
+    print(d, flush=True)
+    _check_attn([5000], [1], 64, 4, 2, d, one=True, seed=1)
+    _check_attn([4097, 1, 300], [1, 1, 1], 16, 8, 2, d, one=True, seed=2)   # idle splits of short sequences
+    _check_attn([3000], [5], 128, 4, 1, d, window=700, sinks=4, seed=3, width=100)
+
+
+def test_large_scores_and_scales():
+    p = Pages([90], 16, 1, 64, seed=5).fill([90], spread=4.0)
+    _check_attn([90], [3], 16, 4, 1, 64, pages=p, seed=5)
+    _check_attn([90], [3], 16, 4, 1, 64, seed=6, scale=1.5)
+
+
+def test_bad_and_handed_back_pages():
+    # pages outside the window: entries of any value, never looked at
+    p = Pages([300, 200], 16, 2, 64, seed=9).fill([300, 200])
+    p.table[0, 2:15] = [2 ** 31 - 1, -2 ** 31, -5, 10 ** 6] * 3 + [-1]
+    _check_attn([300, 200], [1, 1], 16, 4, 2, 64, window=50, sinks=20, pages=p, one=True)
+    # an entry that is no page among those in use: its tokens are not seen
+    p.table[1, 4] = 10 ** 6
+    p.table[1, 5] = -1
+    _check_attn([300, 200], [1, 1], 16, 4, 2, 64, window=50, sinks=20, pages=p, one=True)
+    _check_attn([300, 200], [0, 60], 16, 4, 2, 64, pages=p)
+    # longer than the table
+    p = Pages([64], 16, 1, 64, seed=2).fill([64])
+    _check_attn([90], [30], 16, 2, 1, 64, pages=p)
+
+
+def test_shared_pages():
+    p = Pages([64, 64], 16, 1, 64, seed=4).fill([64, 0])
+    p.table[1, :4] = p.table[0, :4]
+    o = _check_attn([64, 64], [1, 1], 16, 2, 1, 64, pages=p, one=True)
+    assert o.shape[0] == 2
+
+
+def test_replayed_steps_follow_the_lengths():
+    hq, hkv, d, seqs = 8, 2, 128, 3
+    p = Pages([700, 90, 400], 32, hkv, d, seed=11, spare=0).fill([650, 40, 350])
+    cache, eager = p.device([650, 40, 350]), p.device([650, 40, 350])
+    cs = _cos_sin(800, d)
+    qkv = torch.zeros(seqs, hq + 2 * hkv, d, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(L.cache_attn_workspace(cache, hq, seqs), dtype=torch.uint8, device="cuda")
+
+    def step(c):
+        q = torch.empty(seqs, hq, d, dtype=torch.bfloat16, device="cuda")
+        o, ls = torch.empty_like(q), torch.empty(hq, seqs, device="cuda")
+        L.cache_append(c, qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], None, cos_sin=cs, q=qkv[:, :hq], q_out=q)
+        L.cache_attn(c, hq, 0.1, q, None, o, ls, ws, window=300, sinks=4)
+        return o, ls
+
+    step(p.device([650, 40, 350]))                   # loaded before the capture
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(cache)
+    for turn in range(4):
+        qkv.copy_(torch.randn(qkv.shape, generator=torch.Generator().manual_seed(turn)).to(torch.bfloat16))
+        for c in (cache, eager):
+            c.seq_lens.add_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        got_now = [x.clone() for x in got]
+        want = step(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(got_now, want):
+            assert torch.equal(a, b), turn
+        for a, b in zip(cache.tensors, eager.tensors):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), turn
+
+
+def test_serving_run():
+    """Prompts (window attention over the packed rows, K rotated by the append), then tokens one by one."""
+    hq, hkv, d, window, sinks = 4, 2, 64, 48, 3
+    prompts, steps = [37, 100, 1], 6
+    total = [n + steps for n in prompts]
+    p = Pages(total, 16, hkv, d, seed=21)
+    cache = p.device(prompts)
+    cs, scale = _cos_sin(200, d), 1 / math.sqrt(d)
+    cu = np.concatenate([[0], np.cumsum(prompts)]).astype(np.int32)
+    n = int(cu[-1])
+    g = torch.Generator().manual_seed(4)
+    qkv = torch.randn(n, hq + 2 * hkv, d, generator=g).to(torch.bfloat16).cuda()
+    q, k = torch.empty(n, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(n, hkv, d, dtype=torch.bfloat16, device="cuda")
+    v = qkv[:, hq + hkv:].contiguous()
+    cu_dev = torch.from_numpy(cu).cuda()
+    L.cache_append(cache, qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], cu_dev, cos_sin=cs, k_out=k, q=qkv[:, :hq], q_out=q)
+    desc = L.attn_desc(L.shard_desc(n, 1, "contiguous", 0, 1, 1), hq, hkv, d, scale)
+    o, lse = torch.empty_like(q), torch.empty(hq, n, device="cuda")
+    L.window_attn_fwd(desc, window, sinks, q, k, v, cu_dev, o, lse)
+    oc, lsec = torch.empty_like(q), torch.empty(hq, n, device="cuda")
+    ws = torch.empty(max(L.cache_attn_workspace(cache, hq, m) for m in (n, 3)), dtype=torch.uint8, device="cuda")
+    L.cache_attn(cache, hq, scale, q, cu_dev, oc, lsec, ws, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    ref = oracle.window_attention(q.float().cpu().numpy(), k.float().cpu().numpy(), v.float().cpu().numpy(), cu, np.arange(n),
+                                  window, sinks, scale)
+    assert (np.abs(o.float().cpu().numpy() - ref["o"]) <= ref["o_tol"]).all()
+    for step in range(steps):
+        x = torch.randn(3, hq + 2 * hkv, d, generator=g).to(torch.bfloat16).cuda()
+        cache.seq_lens.add_(1)
+        q1 = torch.empty(3, hq, d, dtype=torch.bfloat16, device="cuda")
+        L.cache_append(cache, x[:, hq:hq + hkv], x[:, hq + hkv:], None, cos_sin=cs, q=x[:, :hq], q_out=q1)
+        o1, l1 = torch.empty_like(q1), torch.empty(hq, 3, device="cuda")
+        L.cache_attn(cache, hq, scale, q1, None, o1, l1, ws, window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        codes = [_bits(t) for t in cache.tensors[:4]]
+        lens = np.asarray(prompts) + step + 1
+        want, tol, _, _ = C.attention(q1.float().double().cpu().numpy(), codes[0], codes[2], codes[1], codes[3], p.table, lens,
+                                      [0, 1, 2, 3], window, sinks, scale)
+        assert (np.abs(o1.float().cpu().numpy() - want) <= tol + 1e-9).all(), step
