@@ -10,7 +10,7 @@ namespace hsap {
 #if defined(__HIPCC__)
 
 // Queries of one chunk's sink pass (see window_bwd.hip).
-constexpr int32_t kSinkChunk = 1024;
+constexpr int32_t kSinkChunk = 256;
 // Most sink tokens per document that the backward takes: one workgroup holds them all (4 waves x 32 keys).
 constexpr int32_t kMaxBwdSinks = 128;
 
@@ -80,12 +80,13 @@ __device__ __forceinline__ DocSpan doc_span(const int32_t* cu, int32_t nd, int32
   return d;
 }
 
-// Transfers of a [64][D] bf16 tile from global memory to a swizzled LDS tile (mfma.h), WAVES waves, 64 16-byte chunks
+// Transfers of a [R][D] bf16 tile (R = 64 by default) from global memory to a swizzled LDS tile (mfma.h), WAVES waves, 64 16-byte chunks
 // per instruction.  Issued from asm and ordered by the kernels' own vmcnt waits (vm_wait_barrier): the compiler would
 // wait for every transfer before any later LDS read.
-template <int D, int WAVES>
+template <int D, int WAVES, int R = 64>
 struct TileStage {
-  static constexpr int CPR = D / 8, WCH = 64 * CPR / WAVES, U = WCH / 64;
+  static constexpr int CPR = D / 8, WCH = R * CPR / WAVES, U = WCH / 64;
+  static_assert(WCH % 64 == 0, "a wave moves whole instructions");
   uint32_t off[U];  // byte offset of this lane's chunk of instruction u from the tile's first row
   uint32_t lds0;    // the wave's first chunk within a tile, in bytes
   int first;        // this lane's chunk of instruction 0
@@ -99,7 +100,7 @@ struct TileStage {
       off[u] = (uint32_t)(row * row_bytes + swz_chunk<CPR>(row, p % CPR) * 16);
     }
   }
-  // 64 readable rows at src, row_bytes apart; src and dst uniform over the wave
+  // R readable rows at src, row_bytes apart; src and dst uniform over the wave
   __device__ __forceinline__ void rows(const void* src, const __bf16* dst) const {
     typedef __attribute__((address_space(3))) void* lds_void;
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void)dst + lds0;

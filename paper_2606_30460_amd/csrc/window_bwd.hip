@@ -6,9 +6,9 @@
 //
 // Every gradient row has one owner, which forms it whole in registers and stores it once: no atomics, the same bits
 // each time.  Four launches:
-//   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; also delta
+//   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; delta first
 //   sinks    a document's sinks are seen by all its later queries, far more than a window's worth.  The shard's rows
-//            are cut into chunks of 1024 queries; one workgroup per (chunk, K/V head) forms what the chunk's queries
+//            are cut into chunks of 256 queries; one workgroup per (chunk, K/V head) forms what the chunk's queries
 //            give to the sinks of the document that reaches into it from before (outside their windows): fp32 partials
 //   sum      the chunks of one document are added up, in order, into the first one's partial
 //   dK, dV   one workgroup per (128 consecutive keys, K/V head), over the queries whose window holds one of them --
@@ -99,7 +99,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
   }
   delta = pair_sum(delta);
   const float lse2 = a.lse[(int64_t)h * n + qrow] * kLog2e;
-  if (hi == 0 && valid) a.delta[(int64_t)h * n + qrow] = delta;
   const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
   if (tid == 0) tile_start = doc.start;
   __syncthreads();
@@ -114,6 +113,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
   const int64_t rstride = (int64_t)a.hkv * D;
   const __bf16* kbase = a.k + (int64_t)g * D;
   const __bf16* vbase = a.v + (int64_t)g * D;
+  // delta from O carries O's rounding, which dS = P (dP - delta) feels where a row has few keys (one key: dS is 0, but
+  // for that rounding).  Rows of fewer than 32 keys take delta = sum_j P_ij dP_ij instead, over the 64 positions up
+  // to the wave's last row and the sinks of its first row's document, read straight from global memory.
+  const bool few = valid && gq - wlo + 1 + slen < 32;
+  if (__builtin_amdgcn_ballot_w64(few) != 0) {
+    const int32_t g0 = __builtin_amdgcn_readlane(gq, 0), far = __builtin_amdgcn_readlane(doc.start, 0);
+    const bool sinks = __builtin_amdgcn_ballot_w64(few && slen > 0 && doc.start < g0 - 32) != 0;
+    float sum = 0.f;
+    for (int b = 0; b < (sinks ? 3 : 2); ++b) {
+      const int32_t j0 = b == 2 ? far : g0 - 32 + 32 * b;
+      const int32_t j = max(0, min(j0 + l32, i1));  // this lane's key row
+      const int64_t at = ((int64_t)(j + key_span(a.geom, j).delta) * a.hkv + g) * D + 8 * hi;
+      f32x16 sc = f32x16{}, dp = f32x16{};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(a.k + at + 16 * kk), qf[kk], sc);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) dp = mfma32(*(const bf16x8*)(a.v + at + 16 * kk), df[kk], dp);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int32_t x = j0 + c_row(e, hi);
+        const bool in = x >= wlo && x <= gq, sink = x >= doc.start && x < doc.start + slen;
+        // (the sinks of the third block: those before the other two)
+        const bool see = b == 2 ? sink && x < g0 - 32 : in || sink;
+        sum += see ? fast_exp2(__builtin_fmaf(sc[e], a.scale_log2, -lse2)) * dp[e] : 0.f;
+      }
+    }
+    sum = pair_sum(sum);
+    if (few) delta = sum;
+  }
+  if (hi == 0 && valid) a.delta[(int64_t)h * n + qrow] = delta;
+
   TileStage<D, WAVES> st;
   st.init(w, lane, rstride * 2);
   KeySpan span{0, 0, 0};
@@ -210,9 +240,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
 // before it; the queries those of the chunk outside the window.
 // ---------------------------------------------------------------------------
 template <int D, bool SINKS>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(WindowBwdArgs a) {
-  constexpr int WAVES = 4, QB = 64, CPR = D / 8, TILE = QB * D, BN = 32 * WAVES;
+__global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
+  constexpr int WAVES = 4, BN = 32 * WAVES, CPR = D / 8;
+  constexpr bool VLDS = D == 128;       // V in LDS: its fragments, K's and the two sums do not fit the registers together
+  constexpr int QB = VLDS ? 32 : 64, TILE = QB * D;
   constexpr float NEG_INF = -__builtin_inff();
+  __shared__ __attribute__((aligned(16))) __bf16 vtile[VLDS ? BN * D : 8];
   __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // Q slots 0, 1, then dO slots 0, 1
   __shared__ __attribute__((aligned(16))) float rows_s[2][2][QB];   // [slot][LSE in log2 units, -delta]
   __shared__ int32_t last_s[WAVES][2];
@@ -309,17 +342,19 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
   for (int mb = 0; mb < D / 32; ++mb) dk[mb] = dv[mb] = f32x16{};
 
   if (total > 0) {
-    bf16x8 kf[D / 16], vf[D / 16];
+    bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
     {
       const int64_t at = (krow * a.hkv + g) * D + 8 * hi;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         kf[kk] = *(const bf16x8*)(a.k + at + 16 * kk);
-        vf[kk] = *(const bf16x8*)(a.v + at + 16 * kk);
+        const bf16x8 x = *(const bf16x8*)(a.v + at + 16 * kk);
+        if constexpr (VLDS) *(bf16x8*)(vtile + 32 * w * D + swz<CPR>(l32, 16 * kk + 8 * hi)) = x;  // read by this wave alone
+        else vf[kk] = x;
       }
     }
     const int64_t rstride = (int64_t)a.hq * D;
-    TileStage<D, WAVES> st;
+    TileStage<D, WAVES, QB> st;
     st.init(w, lane, rstride * 2);
     // step i: segment x, head hh of the group, 64 queries from position pos; segment by segment, head by head
     struct Step {
@@ -332,7 +367,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
       p.hh = 0;
       ++p.x;
     };
-    float row_next = 0.f;  // the next step's LSE (wave 0) or delta (wave 1) of row `lane`
+    float row_next = 0.f;  // the next step's LSE (threads 0 .. QB - 1) or delta (the next QB) of a row
     auto stage = [&](const Step& p, int slot) {
       const int32_t lo = p.x ? seg_lo[1] : seg_lo[0], top = p.x ? seg_hi[1] : seg_hi[0];
       const int32_t pos = lo + QB * p.s;
@@ -349,10 +384,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
         st.gather([&](int r) { return qb + min(r, most) * rstride; }, ring + slot * TILE);
         st.gather([&](int r) { return ob + min(r, most) * rstride; }, ring + (2 + slot) * TILE);
       }
-      if (w < 2) row_next = (w == 0 ? a.lse : a.delta)[(int64_t)h * n + r0 + min(lane, most)];
+      if (tid < 2 * QB) row_next = (tid < QB ? a.lse : a.delta)[(int64_t)h * n + r0 + min(tid % QB, most)];
     };
     auto store_rows = [&](int slot) {
-      if (w < 2) rows_s[slot][w][lane] = w == 0 ? row_next * kLog2e : -row_next;
+      if (tid < 2 * QB) rows_s[slot][tid / QB][tid % QB] = tid < QB ? row_next * kLog2e : -row_next;
     };
     const int tr_row = 4 * hi + ((lane & 15) >> 2);
     const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -387,7 +422,12 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(Q + 32 * nb * D + rowoff[kk]), kf[kk], sc);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) dp = mfma32(*(const bf16x8*)(O + 32 * nb * D + rowoff[kk]), vf[kk], dp);
+        for (int kk = 0; kk < D / 16; ++kk) {
+          bf16x8 vx;
+          if constexpr (VLDS) vx = *(const bf16x8*)(vtile + 32 * w * D + rowoff[kk]);
+          else vx = vf[kk];
+          dp = mfma32(*(const bf16x8*)(O + 32 * nb * D + rowoff[kk]), vx, dp);
+        }
         if (__builtin_amdgcn_ballot_w64(!all) != 0) {
           const int32_t r4 = r + 4 * hi;
 #pragma unroll
@@ -425,7 +465,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
   }
 
   if constexpr (SINKS) {
-    // every sink of the document, those without a query here as zeros
+    // every sink of the document; those at or behind the chunk's first position are zeros
     const int32_t s = 32 * w + l32;
     if (s >= a.sinks) return;
     float* out = a.partial + (((int64_t)tile * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
@@ -435,6 +475,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void window_dkv_kernel(Windo
       for (int q = 0; q < 4; ++q) {
         f32x4 x{dk[mb][4 * q], dk[mb][4 * q + 1], dk[mb][4 * q + 2], dk[mb][4 * q + 3]};
         f32x4 y{dv[mb][4 * q], dv[mb][4 * q + 1], dv[mb][4 * q + 2], dv[mb][4 * q + 3]};
+        if (!key_ok) x = y = f32x4{};  // (a lane without a key repeats the last one's, unmasked)
         *(f32x4*)(out + 32 * mb + 8 * q) = x;
         *(f32x4*)(out + D + 32 * mb + 8 * q) = y;
       }
@@ -500,7 +541,15 @@ __global__ __launch_bounds__(256) void window_sink_sum_kernel(WindowBwdArgs a, i
   float* p = a.partial + ((int64_t)tile * a.hkv + g) * elems;
   for (int e = 4 * threadIdx.x; e < elems; e += 4 * 256) {
     f32x4 sum = *(const f32x4*)(p + e);
-    for (int x = 1; x <= more; ++x) sum += *(const f32x4*)(p + x * step + e);
+    int x = 1;
+    for (; x + 7 <= more; x += 8) {  // eight loads in flight
+      f32x4 part[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) part[y] = *(const f32x4*)(p + (x + y) * step + e);
+#pragma unroll
+      for (int y = 0; y < 8; ++y) sum += part[y];
+    }
+    for (; x <= more; ++x) sum += *(const f32x4*)(p + x * step + e);
     *(f32x4*)(p + e) = sum;
   }
 }
