@@ -7,8 +7,8 @@
 // raises it and the page's older codes are encoded anew -- by a power of two, so exactly, but for what falls under
 // e4m3's smallest normal number.
 //
-// A row of one head is D / 16 units of 16 values: eight pairs where it is rotated (values u.. and rot / 2 + u.. for
-// halves, 16 u .. for interleaved pairs), 16 values in place behind the rotation.  A thread holds a unit.
+// A row of one head is D / 16 units, each two runs of eight values D / 2 apart or, where halves are rotated, rot / 2 apart
+// (eight pairs), so that the lanes of a row read and write it in whole lines.  A thread holds a unit.
 #include <algorithm>
 
 #include "cache.h"
@@ -36,69 +36,64 @@ struct AppendArgs {
   int32_t kv_blocks;  // workgroups of the cache's part; the others rotate Q
 };
 
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 struct Unit {
-  float x[16];
+  f32x8 a, b;  // the two runs
 };
 
-// Unit u of a row: its two runs of eight values start at at[0] and at[1].
+// Unit u of a row: the first values of its two runs of eight.
+template <int D>
 __device__ __forceinline__ void unit_at(const AppendArgs& a, int u, bool turn, int (&at)[2]) {
-  if (turn && 16 * u < a.rot && !a.interleaved) {
-    at[0] = 8 * u;
-    at[1] = a.rot / 2 + 8 * u;
-  } else {
-    at[0] = 16 * u;
-    at[1] = 16 * u + 8;
-  }
+  const int rot = turn && !a.interleaved ? a.rot : 0;
+  const int base = 16 * u < rot ? 0 : rot, width = 16 * u < rot ? rot : D - rot;
+  at[0] = base + 8 * (u - base / 16);
+  at[1] = at[0] + width / 2;
 }
 
-__device__ __forceinline__ Unit load_unit(const AppendArgs& a, const __bf16* row, int u, bool turn, int64_t pos) {
-#pragma clang fp contract(off)
+template <int D>
+__device__ __forceinline__ Unit load_unit(const AppendArgs& a, const __bf16* row, int u, bool turn) {
   int at[2];
-  unit_at(a, u, turn, at);
-  const bf16x8 lo = *(const bf16x8*)(row + at[0]), hi = *(const bf16x8*)(row + at[1]);
-  Unit r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    r.x[e] = (float)lo[e];
-    r.x[8 + e] = (float)hi[e];
-  }
-  if (turn && 16 * u < a.rot) {
-    const float* cs = a.cos_sin + pos * a.rot + 8 * u;
-    float c[8], s[8];
-#pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      *(f32x4*)(c + e) = *(const f32x4*)(cs + e);
-      *(f32x4*)(s + e) = *(const f32x4*)(cs + a.rot / 2 + e);
-    }
-    if (a.interleaved) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = r.x[2 * e], y = r.x[2 * e + 1];
-        r.x[2 * e] = x * c[e] - y * s[e];
-        r.x[2 * e + 1] = y * c[e] + x * s[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = r.x[e], y = r.x[8 + e];
-        r.x[e] = x * c[e] - y * s[e];
-        r.x[8 + e] = y * c[e] + x * s[e];
-      }
-    }
+  unit_at<D>(a, u, turn, at);
+  return Unit{__builtin_convertvector(*(const bf16x8*)(row + at[0]), f32x8),
+              __builtin_convertvector(*(const bf16x8*)(row + at[1]), f32x8)};
+}
+
+__device__ __forceinline__ f32x8 load8(const float* p) {  // (16-byte aligned)
+  const f32x4 x = *(const f32x4*)p, y = *(const f32x4*)(p + 4);
+  return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+
+// four interleaved pairs by the cosines and sines at c and s
+__device__ __forceinline__ f32x8 turn_pairs(const f32x8& v, const float* cos, const float* sin) {
+#pragma clang fp contract(off)
+  const f32x4 c = *(const f32x4*)cos, s = *(const f32x4*)sin;
+  return f32x8{v[0] * c[0] - v[1] * s[0], v[1] * c[0] + v[0] * s[0], v[2] * c[1] - v[3] * s[1], v[3] * c[1] + v[2] * s[1],
+               v[4] * c[2] - v[5] * s[2], v[5] * c[2] + v[4] * s[2], v[6] * c[3] - v[7] * s[3], v[7] * c[3] + v[6] * s[3]};
+}
+
+template <int D>
+__device__ __forceinline__ Unit turn_unit(const AppendArgs& a, int u, int64_t pos, Unit r) {
+#pragma clang fp contract(off)
+  const float* cs = a.cos_sin + pos * a.rot;
+  if (a.interleaved) {
+    const int first = 4 * u, second = first + D / 4;  // first pairs of the runs
+    if (first < a.rot / 2) r.a = turn_pairs(r.a, cs + first, cs + a.rot / 2 + first);
+    if (second < a.rot / 2) r.b = turn_pairs(r.b, cs + second, cs + a.rot / 2 + second);
+  } else if (16 * u < a.rot) {
+    const f32x8 c = load8(cs + 8 * u), s = load8(cs + a.rot / 2 + 8 * u);
+    const f32x8 x = r.a, y = r.b;
+    r.a = x * c - y * s;
+    r.b = y * c + x * s;
   }
   return r;
 }
 
+template <int D>
 __device__ __forceinline__ void store_bf16(const AppendArgs& a, __bf16* row, int u, bool turn, const Unit& r) {
   int at[2];
-  unit_at(a, u, turn, at);
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    bf16x8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = (__bf16)r.x[8 * p + e];
-    *(bf16x8*)(row + at[p]) = o;
-  }
+  unit_at<D>(a, u, turn, at);
+  *(bf16x8*)(row + at[0]) = __builtin_convertvector(r.a, bf16x8);
+  *(bf16x8*)(row + at[1]) = __builtin_convertvector(r.b, bf16x8);
 }
 
 // e4m3 of x (nearest even, saturating at 448; NaN stays NaN)
@@ -112,38 +107,38 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
   return (uint32_t)w;
 }
 
+__device__ __forceinline__ uint2 encode8(const f32x8& x) {
+  return make_uint2(encode4(x[0], x[1], x[2], x[3]), encode4(x[4], x[5], x[6], x[7]));
+}
+
+template <int D>
 __device__ __forceinline__ void store_codes(const AppendArgs& a, uint8_t* row, int u, bool turn, const Unit& r, float inv) {
   int at[2];
-  unit_at(a, u, turn, at);
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const float* x = r.x + 8 * p;
-    *(uint2*)(row + at[p]) = make_uint2(encode4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
-                                        encode4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
-  }
+  unit_at<D>(a, u, turn, at);
+  *(uint2*)(row + at[0]) = encode8(r.a * inv);
+  *(uint2*)(row + at[1]) = encode8(r.b * inv);
 }
 
 // largest finite magnitude of a unit
 __device__ __forceinline__ float unit_max(const Unit& r) {
   float m = 0.f;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float x = fabsf(r.x[e]);
-    m = fmaxf(m, x < __builtin_inff() ? x : 0.f);
+  for (int e = 0; e < 8; ++e) {
+    const float x = fabsf(r.a[e]), y = fabsf(r.b[e]);
+    m = fmaxf(m, fmaxf(x < __builtin_inff() ? x : 0.f, y < __builtin_inff() ? y : 0.f));
   }
   return m;
 }
 
+__device__ __forceinline__ uint32_t recode4(uint32_t x, float ratio) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+  return encode4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
+}
+
 // 16 codes at p, encoded anew for a scale 1 / ratio times as large
 __device__ __forceinline__ void recode16(uint8_t* p, float ratio) {
-  uint4 w = *(const uint4*)p;
-  uint32_t* x = (uint32_t*)&w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i], true);
-    x[i] = encode4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
-  }
-  *(uint4*)p = w;
+  const uint4 w = *(const uint4*)p;
+  *(uint4*)p = make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
 }
 
 // The page's new scale; `kept` tokens before the new ones stay.  Sets inv to its reciprocal and ratio to what their codes
@@ -173,6 +168,7 @@ __device__ __forceinline__ void rotate_q(const AppendArgs& a, int64_t item) {
   const int64_t t = row / a.heads_q;
   const int h = (int)(row - t * a.heads_q);
   if (t >= a.total_new) return;
+  Unit x = load_unit<D>(a, a.q + t * a.q_stride + (int64_t)h * D, u, true);  // (under way while the position is looked up)
   int64_t pos;
   if (a.cu) {
     int32_t l = 0, r = a.d.num_seqs;  // cu[l] <= t < cu[r]
@@ -187,8 +183,8 @@ __device__ __forceinline__ void rotate_q(const AppendArgs& a, int64_t item) {
     pos = (int64_t)a.c.seq_lens[t] - 1;
   }
   if (pos < 0 || (a.rot && pos >= a.rows)) return;
-  const Unit x = load_unit(a, a.q + t * a.q_stride + (int64_t)h * D, u, true, pos);
-  store_bf16(a, a.q_out + (t * a.heads_q + h) * D, u, true, x);
+  if (a.rot) x = turn_unit<D>(a, u, pos, x);
+  store_bf16<D>(a, a.q_out + (t * a.heads_q + h) * D, u, true, x);
 }
 
 // One new token per sequence: D / 16 lanes per (sequence, head, K or V).
@@ -206,11 +202,12 @@ __global__ __launch_bounds__(256) void cache_append_one_kernel(AppendArgs a) {
   const int64_t s = (row >> 1) / a.d.heads_kv;
   const int h = (int)((row >> 1) - s * a.d.heads_kv);
   if (s >= a.d.num_seqs) return;
+  const __bf16* src = is_v ? a.v + s * a.v_stride : a.k + s * a.k_stride;
+  Unit x = load_unit<D>(a, src + (int64_t)h * D, u, !is_v);
   const int32_t pos = a.c.seq_lens[s] - 1;
   if (pos < 0 || (a.rot && pos >= a.rows)) return;
-  const __bf16* src = is_v ? a.v + s * a.v_stride : a.k + s * a.k_stride;
-  const Unit x = load_unit(a, src + (int64_t)h * D, u, !is_v, pos);
-  if (!is_v && a.k_out) store_bf16(a, a.k_out + (s * a.d.heads_kv + h) * D, u, true, x);
+  if (!is_v && a.rot) x = turn_unit<D>(a, u, pos, x);
+  if (!is_v && a.k_out) store_bf16<D>(a, a.k_out + (s * a.d.heads_kv + h) * D, u, true, x);
   const int32_t page = cache_page(a.c.page_table + s * a.d.table_width, a.d.table_width, a.d.num_pages, a.d.page_size, pos);
   if (page < 0) return;
   const int32_t slot = pos & (a.d.page_size - 1);
@@ -224,15 +221,16 @@ __global__ __launch_bounds__(256) void cache_append_one_kernel(AppendArgs a) {
   const float now = page_scale(amax, slot > 0, old, inv, ratio);
   if (ratio != 1.f)
     for (int32_t t = 0; t < slot; ++t) recode16(codes + t * D + 16 * u, ratio);
-  store_codes(a, codes + slot * D, u, !is_v, x, inv);
+  store_codes<D>(a, codes + slot * D, u, !is_v, x, inv);
   if (u == 0) *scale = now;
 }
 
 // Any number of new tokens: one workgroup per (page that a sequence's new tokens reach, head, K or V); the page's new
 // values are held in registers between the reduction of their maximum and their encoding.
-template <int D>
+// PER: units of a page per thread.
+template <int D, int PER>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
-  constexpr int UNITS = D / 16, PER = 128 * UNITS / 256;  // units per thread of a page of 128 tokens
+  constexpr int UNITS = D / 16;
   if ((int)blockIdx.x >= a.kv_blocks) {
     rotate_q<D>(a, (int64_t)(blockIdx.x - a.kv_blocks) * 256 + threadIdx.x);
     return;
@@ -265,16 +263,18 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   const int32_t slot0 = (int32_t)(lo - at * ps), units = (int32_t)(end - lo) * UNITS;
   const __bf16* src = (is_v ? a.v : a.k) + (int64_t)h * D;
   const int64_t stride = is_v ? a.v_stride : a.k_stride;
-  Unit x[PER];
+  Unit x[PER] = {};
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int unit = tid + 256 * i;
-    if (unit >= units) break;
-    const int64_t pos = lo + unit / UNITS, t = t0 + (pos - pos0);
-    x[i] = load_unit(a, src + t * stride, unit % UNITS, !is_v, pos);
-    amax = fmaxf(amax, unit_max(x[i]));
-    if (!is_v && a.k_out) store_bf16(a, a.k_out + (t * a.d.heads_kv + h) * D, unit % UNITS, true, x[i]);
+    if (unit < units) {
+      const int64_t pos = lo + unit / UNITS, t = t0 + (pos - pos0);
+      x[i] = load_unit<D>(a, src + t * stride, unit % UNITS, !is_v);
+      if (!is_v && a.rot) x[i] = turn_unit<D>(a, unit % UNITS, pos, x[i]);
+      amax = fmaxf(amax, unit_max(x[i]));
+      if (!is_v && a.k_out) store_bf16<D>(a, a.k_out + (t * a.d.heads_kv + h) * D, unit % UNITS, true, x[i]);
+    }
   }
   if (page < 0) return;
   float* scale = (is_v ? a.c.v_scale : a.c.k_scale) + (int64_t)page * a.d.heads_kv + h;
@@ -292,8 +292,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int unit = tid + 256 * i;
-    if (unit >= units) break;
-    store_codes(a, codes + (slot0 + unit / UNITS) * D, unit % UNITS, !is_v, x[i], inv);
+    if (unit < units) store_codes<D>(a, codes + (slot0 + unit / UNITS) * D, unit % UNITS, !is_v, x[i], inv);
   }
   if (tid == 0) *scale = now;
 }
@@ -381,8 +380,15 @@ extern "C" hsap_status hsap_cache_append(const hsap_cache_desc* desc, const hsap
   hipStream_t s = (hipStream_t)hip_stream;
   const dim3 grid((unsigned)blocks), block(256);
   if (cu_new) {
-    if (d == 128) hipLaunchKernelGGL(cache_append_kernel<128>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(cache_append_kernel<64>, grid, block, 0, s, a);
+    const int per = desc->page_size * (d / 16) / 256;
+    if (d == 128) {
+      if (per <= 1) hipLaunchKernelGGL((cache_append_kernel<128, 1>), grid, block, 0, s, a);
+      else if (per == 2) hipLaunchKernelGGL((cache_append_kernel<128, 2>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((cache_append_kernel<128, 4>), grid, block, 0, s, a);
+    } else {
+      if (per <= 1) hipLaunchKernelGGL((cache_append_kernel<64, 1>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((cache_append_kernel<64, 2>), grid, block, 0, s, a);
+    }
   } else {
     if (d == 128) hipLaunchKernelGGL(cache_append_one_kernel<128>, grid, block, 0, s, a);
     else hipLaunchKernelGGL(cache_append_one_kernel<64>, grid, block, 0, s, a);

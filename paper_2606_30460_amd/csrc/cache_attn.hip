@@ -62,7 +62,7 @@ __device__ __forceinline__ Steps cache_steps(int32_t plo, int32_t phi, int32_t c
   return Steps{ns, win0, ns + (phi >= win0 ? (phi - win0) / 32 + 1 : 0)};
 }
 
-// Splits that have work, of `total` steps dealt to at most `splits`, and the steps of each.
+// Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
 __device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -129,7 +129,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
   const Steps steps = cache_steps(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
   const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
-  if (s_begin >= s_end && split > 0) return;  // (split 0 writes the rows of a tile that sees nothing)
+  if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
+    const int32_t r = rt.row0 + tid, t = r / a.group;
+    if (tid < ROWS && r < nrows)
+      a.part_lse[((int64_t)split * a.total_q + rt.t0 + t) * a.heads_q + g * a.group + (r - t * a.group)] = NEG_INF;
+    return;
+  }
 
   // this lane's query of each 16-row block: row, position, Q fragments
   int32_t pos[MT];
@@ -217,8 +222,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
 #pragma unroll
         for (int kk = 0; kk < 2 * KX; ++kk) sc[half] = mfma16(kf[half][kk], qf[mt][kk], sc[half]);
       const bool all = x.held[0] && x.held[1] && jl <= pos[mt] && (pos[mt] - x.j0 < near || jl < sinks);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) sc[half] *= x.ks[half] * a.scale_log2;
+      const float sl[2] = {fmaxf(x.ks[0] * a.scale_log2, 1.17549435e-38f), fmaxf(x.ks[1] * a.scale_log2, 1.17549435e-38f)};
       if (__builtin_amdgcn_ballot_w64(!all) != 0) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -229,8 +233,9 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
             if (!see) sc[half][e] = NEG_INF;
           }
       }
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      // (scales are positive; at least the smallest normal number, so that -inf stays -inf)
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])) * sl[0],
+                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])) * sl[1]);
       // a row's tokens lie on four lanes; its maximum is joined only when some lane's rose by more than the slack
       if (__builtin_amdgcn_ballot_w64(mx > m_run[mt] + RESCALE_SLACK) != 0) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -247,7 +252,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = fast_exp2(sc[half][e] - m_use);
+          const float p = fast_exp2(__builtin_fmaf(sc[half][e], sl[half], -m_use));
           l_run[mt] += p;
           pf[mt][4 * half + e] = (__bf16)(p * x.vs[half]);
         }
@@ -377,55 +382,84 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
   }
 }
 
-// Joins the splits of every row: one wave per row, D / 64 values per lane.  The number of splits with work follows
-// from the row's tile, as in the kernel above.
+// Joins the splits of every row by their LSE.  Up to eight: D / 4 lanes per row, four values each, every load of a row
+// in flight together.
 template <int D>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a, int rows_per_tile) {
-  constexpr int E = D / 64;
+__global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a) {
   constexpr float NEG_INF = -__builtin_inff();
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int LANES = D / 4, MOST = 8;
   const int64_t rows = a.total_q * a.heads_q;
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+  const int x = threadIdx.x % LANES;
   if (row >= rows) return;
   const int64_t tok = row / a.heads_q;
-  const int h = (int)(row - tok * a.heads_q);
-  int32_t seq, t0, count;
-  if (a.cu) {
-    int32_t l = 0, r = a.d.num_seqs;
-    if (tok >= a.cu[r]) return;
-    while (r - l > 1) {
-      const int32_t mid = (l + r) >> 1;
-      if (a.cu[mid] <= tok) l = mid;
-      else r = mid;
-    }
-    seq = l;
-    t0 = a.cu[l];
-    count = (int32_t)min((int64_t)a.cu[l + 1], a.total_q) - t0;
-  } else {
-    seq = t0 = (int32_t)tok;
-    count = 1;
-  }
-  const int32_t len = max(0, a.c.seq_lens[seq]), pos0 = len - count;
-  const int32_t r = (int32_t)(tok - t0) * a.group + h % a.group;
-  const int32_t row0 = r / rows_per_tile * rows_per_tile, last = min(row0 + rows_per_tile, count * a.group) - 1;
-  const Steps steps = cache_steps(pos0 + row0 / a.group, pos0 + last / a.group, a.d.table_width * a.d.page_size, a.window, a.sinks);
-  const int32_t per = steps_per_split(steps.total, a.splits);
-  const int32_t live = per > 0 ? (steps.total + per - 1) / per : 1;
-  float m = NEG_INF, sum = 0.f, acc[E] = {};
-  for (int32_t s = 0; s < live; ++s) {
-    const int64_t at = (int64_t)s * rows + row;
-    const float l = a.part_lse[at];
-    if (l == NEG_INF) continue;
-    const float m_new = fmaxf(m, l), f1 = fast_exp2(m - m_new), f2 = fast_exp2(l - m_new);
-    sum = sum * f1 + f2;
-    m = m_new;
+  if (a.cu && tok >= a.cu[a.d.num_seqs]) return;  // a row of no sequence
+  float l[MOST], m = NEG_INF, sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] * f1 + a.part_o[at * D + E * lane + e] * f2;
+  for (int s = 0; s < MOST; ++s) {
+    l[s] = s < a.splits ? a.part_lse[s * rows + row] : NEG_INF;
+    m = fmaxf(m, l[s]);
+  }
+  f32x4 acc = f32x4{};
+#pragma unroll
+  for (int s = 0; s < MOST; ++s) {
+    const float f = l[s] == NEG_INF ? 0.f : fast_exp2(l[s] - m);
+    sum += f;
+    if (f > 0.f) acc += f * *(const f32x4*)(a.part_o + (s * rows + row) * D + 4 * x);
   }
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  *(bf16x4*)(a.o + row * D + 4 * x) = bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv),
+                                             (__bf16)(acc[3] * inv)};
+  if (x == 0 && a.lse)
+    a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
+}
+
+// More splits: a workgroup per row.  Every wave forms the weights of all splits (up to 256, four to a lane); the
+// 256 / (D / 4) groups of lanes then take every so manieth split and are added up in LDS.
+constexpr int kMaxSplits = 256;
+template <int D>
+__global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
+  constexpr float NEG_INF = -__builtin_inff();
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+  __shared__ float weight[kMaxSplits];
+  __shared__ f32x4 part[GROUPS][LANES];
+  const int64_t rows = a.total_q * a.heads_q, row = blockIdx.x;
+  const int64_t tok = row / a.heads_q;
+  if (a.cu && tok >= a.cu[a.d.num_seqs]) return;
+  const int tid = threadIdx.x, lane = tid & 63, x = tid % LANES, grp = tid / LANES;
+  float l[kMaxSplits / 64], m = NEG_INF, sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) a.o[row * D + E * lane + e] = (__bf16)(acc[e] * inv);
-  if (lane == 0 && a.lse) a.lse[(int64_t)h * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
+  for (int y = 0; y < kMaxSplits / 64; ++y) {
+    const int s = 64 * y + lane;
+    l[y] = s < a.splits ? a.part_lse[s * rows + row] : NEG_INF;
+    m = fmaxf(m, l[y]);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+#pragma unroll
+  for (int y = 0; y < kMaxSplits / 64; ++y) {
+    const float f = l[y] == NEG_INF ? 0.f : fast_exp2(l[y] - m);
+    sum += f;
+    if (tid < 64) weight[64 * y + lane] = f;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+  __syncthreads();
+  f32x4 acc = f32x4{};
+#pragma unroll 4
+  for (int s = grp; s < a.splits; s += GROUPS) {
+    const float f = weight[s];
+    if (f > 0.f) acc += f * *(const f32x4*)(a.part_o + (s * rows + row) * D + 4 * x);
+  }
+  part[grp][x] = acc;
+  __syncthreads();
+  if (grp > 0) return;
+  for (int y = 1; y < GROUPS; ++y) acc += part[y][x];
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  *(bf16x4*)(a.o + row * D + 4 * x) = bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv),
+                                             (__bf16)(acc[3] * inv)};
+  if (x == 0 && a.lse)
+    a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
 }
 
 // How a call is cut: row tiles of 16 mt rows, and splits of a tile's tokens so that the grid fills the chip, each of
@@ -436,6 +470,8 @@ struct CacheCut {
   int32_t splits;
 };
 
+constexpr int64_t kCacheGrid = 1024;  // workgroups to aim at
+
 static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
   const int64_t group = heads_q / d.heads_kv;
@@ -443,8 +479,8 @@ static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tot
   c.mt = rows > 32 ? 4 : rows > 16 ? 2 : 1;
   c.tiles = one_each ? (int64_t)d.num_seqs * ((group + 16 * c.mt - 1) / (16 * c.mt))
                      : item_base(total_q, group, 16 * c.mt, 1, d.num_seqs);
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, tokens / 256));
-  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, 1024 / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
+  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
   return c;
 }
 
@@ -528,11 +564,17 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
   if (c.splits > 1) {
-    const dim3 grid((unsigned)((total_q * heads_q + 3) / 4));
-    if (d == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, grid, dim3(256), 0, s, a, 16 * c.mt);
-    else hipLaunchKernelGGL(cache_merge_kernel<64>, grid, dim3(256), 0, s, a, 16 * c.mt);
+    const int64_t rows = total_q * heads_q;
+    const dim3 few((unsigned)((rows * (d / 4) + 255) / 256)), many((unsigned)rows), block(256);
+    if (c.splits <= 8) {
+      if (d == 128) hipLaunchKernelGGL(cache_join_few_kernel<128>, few, block, 0, s, a);
+      else hipLaunchKernelGGL(cache_join_few_kernel<64>, few, block, 0, s, a);
+    } else {
+      if (d == 128) hipLaunchKernelGGL(cache_join_many_kernel<128>, many, block, 0, s, a);
+      else hipLaunchKernelGGL(cache_join_many_kernel<64>, many, block, 0, s, a);
+    }
     e = hipGetLastError();
-    if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn merge launch: %s", hipGetErrorString(e));
+    if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn join launch: %s", hipGetErrorString(e));
   }
   return HSAP_OK;
 }
