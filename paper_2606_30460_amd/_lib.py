@@ -687,12 +687,23 @@ def convert_f32_bf16(src, dst, stream=None) -> None:
 MAX_WINDOW = 2 ** 31 - 1  # a window that ends nothing
 
 
-def _one_device(*tensors) -> None:
-    """Every tensor on the current device (the stream and the launch are that device's)."""
-    here = _torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError("tensor on cuda:%d, but cuda:%d is the current device" % (t.device.index, here))
+def _here() -> int:
+    """The current device (the stream and the launch are that device's); -1 without a GPU, where no tensor passes."""
+    torch = _torch or _load_torch()
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+
+
+def _arg(t, dtype_name: str, what: str, numel: Optional[int], here: int) -> int:
+    """Address of a contiguous device tensor of that type and size on the current device; refuses any other.  (One pass
+    over the attributes, since these calls are made for single tokens too.)"""
+    try:
+        if (t.dtype is _dtypes[dtype_name] and t.get_device() == here >= 0 and t.is_contiguous()
+                and (numel is None or t.numel() == numel)):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, dtype_name, what, numel)
+    raise ValueError("%s is on %s, but cuda:%d is the current device" % (what, t.device, here))
 
 
 def _extent(value: int, what: str) -> int:
@@ -702,24 +713,26 @@ def _extent(value: int, what: str) -> int:
     return value
 
 
+def _window_sizes(desc: AttnDesc):
+    """Rows of the shard and elements of q and of k."""
+    s, d = desc.shard, desc.head_dim
+    n = s.rows
+    return n, n * desc.heads_q * d, s.sp_degree * n * desc.heads_kv * d
+
+
 def window_attn_fwd(desc: AttnDesc, window: int, sinks: int, q, k, v, cu_seqlens_dev, o_out, lse_out,
                     stream=None) -> None:
     """hsap_window_attn_fwd: q bf16 [n, Hq, d] against k / v bf16 [P, n, Hkv, d] through a window of ``window`` tokens
     and the first ``sinks`` tokens of each document (cu_seqlens_dev int32 [num_docs + 1] on the device) -> o_out bf16
     [n, Hq, d], lse_out fp32 [Hq, n]."""
-    s = desc.shard
-    n = s.rows
-    hq, hkv, d, P = desc.heads_q, desc.heads_kv, desc.head_dim, s.sp_degree
-    _dev(q, "bfloat16", "q", n * hq * d)
-    _dev(k, "bfloat16", "k", P * n * hkv * d)
-    _dev(v, "bfloat16", "v", P * n * hkv * d)
-    _dev(cu_seqlens_dev, "int32", "cu_seqlens")
-    _dev(o_out, "bfloat16", "o_out", n * hq * d)
-    _dev(lse_out, "float32", "lse_out", hq * n)
-    _one_device(q, k, v, cu_seqlens_dev, o_out, lse_out)
-    _check(lib().hsap_window_attn_fwd(ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q),
-                                      _ptr(k), _ptr(v), _ptr(cu_seqlens_dev), cu_seqlens_dev.numel() - 1, _ptr(o_out),
-                                      _ptr(lse_out), _stream(stream)))
+    here = _here()
+    n, nq, nkv = _window_sizes(desc)
+    _check(lib().hsap_window_attn_fwd(
+        ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _arg(q, "bfloat16", "q", nq, here),
+        _arg(k, "bfloat16", "k", nkv, here), _arg(v, "bfloat16", "v", nkv, here),
+        _arg(cu_seqlens_dev, "int32", "cu_seqlens", None, here), cu_seqlens_dev.numel() - 1,
+        _arg(o_out, "bfloat16", "o_out", nq, here), _arg(lse_out, "float32", "lse_out", desc.heads_q * n, here),
+        _stream(stream)))
 
 
 def window_attn_bwd_workspace(desc: AttnDesc, window: int, sinks: int) -> int:
@@ -734,24 +747,16 @@ def window_attn_bwd(desc: AttnDesc, window: int, sinks: int, q, k, v, d_o, o, ls
                     stream=None) -> None:
     """hsap_window_attn_bwd: gradients of window_attn_fwd (o, lse: its outputs) into dq bf16 [n, Hq, d] and dk / dv
     [P, n, Hkv, d], both bf16 or both fp32; workspace: uint8, window_attn_bwd_workspace bytes."""
-    s = desc.shard
-    n = s.rows
-    hq, hkv, d, P = desc.heads_q, desc.heads_kv, desc.head_dim, s.sp_degree
-    for t, name in ((q, "q"), (d_o, "d_o"), (o, "o"), (dq, "dq")):
-        _dev(t, "bfloat16", name, n * hq * d)
-    for t, name in ((k, "k"), (v, "v")):
-        _dev(t, "bfloat16", name, P * n * hkv * d)
-    _dev(lse, "float32", "lse", hq * n)
-    _dev(cu_seqlens_dev, "int32", "cu_seqlens")
-    wide = getattr(dk, "dtype", None) is _dtypes["float32"]
-    for t, name in ((dk, "dk"), (dv, "dv")):
-        _dev(t, "float32" if wide else "bfloat16", name, P * n * hkv * d)
-    _dev(workspace, "uint8", "workspace")
-    _one_device(q, k, v, d_o, o, lse, cu_seqlens_dev, dq, dk, dv, workspace)
-    _check(lib().hsap_window_attn_bwd(ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q),
-                                      _ptr(k), _ptr(v), _ptr(d_o), _ptr(o), _ptr(lse), _ptr(cu_seqlens_dev),
-                                      cu_seqlens_dev.numel() - 1, _ptr(dq), _ptr(dk), _ptr(dv), int(wide), _ptr(workspace),
-                                      workspace.numel(), _stream(stream)))
+    here = _here()
+    n, nq, nkv = _window_sizes(desc)
+    grads = "float32" if getattr(dk, "dtype", None) is _dtypes["float32"] else "bfloat16"
+    _check(lib().hsap_window_attn_bwd(
+        ctypes.byref(desc), _extent(window, "window"), _extent(sinks, "sinks"), _arg(q, "bfloat16", "q", nq, here),
+        _arg(k, "bfloat16", "k", nkv, here), _arg(v, "bfloat16", "v", nkv, here), _arg(d_o, "bfloat16", "d_o", nq, here),
+        _arg(o, "bfloat16", "o", nq, here), _arg(lse, "float32", "lse", desc.heads_q * n, here),
+        _arg(cu_seqlens_dev, "int32", "cu_seqlens", None, here), cu_seqlens_dev.numel() - 1,
+        _arg(dq, "bfloat16", "dq", nq, here), _arg(dk, grads, "dk", nkv, here), _arg(dv, grads, "dv", nkv, here),
+        int(grads == "float32"), _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
@@ -781,21 +786,32 @@ class KVCache:
             raise ValueError("the cache's tensors are on several devices")
         self.desc = CacheDesc(pages, size, hkv, d, seqs, width)
         self.buffers = CacheBuffers(*[_ptr(t) for t in self.tensors])
+        self.device_index = k_codes.get_device()
+        self._refs = (ctypes.byref(self.desc), ctypes.byref(self.buffers))
 
 
-def _token_rows(t, what: str, rows: int, heads: int, d: int) -> int:
-    """Row stride (elements) of a bf16 tensor [rows, heads, d] whose rows are contiguous."""
+def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int):
+    """Address and row stride (elements) of a bf16 tensor [rows, heads, d] on the current device, its rows contiguous."""
     torch = _torch or _load_torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a device tensor" % what)
     if t.dtype is not _dtypes["bfloat16"]:
         raise TypeError("%s must be bfloat16, got %s" % (what, t.dtype))
-    if tuple(t.shape) != (rows, heads, d):
+    if t.shape != (rows, heads, d):
         raise ValueError("%s is %s, expected [%d, %d, %d]" % (what, list(t.shape), rows, heads, d))
+    if t.get_device() != here:
+        raise ValueError("%s is on %s, but cuda:%d is the current device" % (what, t.device, here))
     row, head, one = t.stride()
     if (one != 1 or (head != d and heads > 1)) and rows:
         raise ValueError("%s must have contiguous rows [heads, head_dim]" % what)
-    return row if rows > 1 else heads * d
+    return t.data_ptr(), (row if rows > 1 else heads * d)
+
+
+def _cache_here(cache: KVCache) -> int:
+    here = _here()
+    if cache.device_index != here:
+        raise ValueError("the cache is on cuda:%d, but cuda:%d is the current device" % (cache.device_index, here))
+    return here
 
 
 def cache_append(cache: KVCache, k, v, cu_new, cos_sin=None, interleaved: bool = False, k_out=None, q=None, q_out=None,
@@ -803,31 +819,28 @@ def cache_append(cache: KVCache, k, v, cu_new, cos_sin=None, interleaved: bool =
     """hsap_cache_append: new tokens' k / v bf16 [total_new, Hkv, d] (rows may be strided) into the cache, K (and q bf16
     [total_new, Hq, d] -> q_out) rotated by the rows of cos_sin fp32 [positions, rot_dim] (None: not rotated); k_out
     takes the rotated K.  cu_new int32 [num_seqs + 1], or None for one token per sequence."""
-    c = cache.desc
+    here, c = _cache_here(cache), cache.desc
+    hkv, d = c.heads_kv, c.head_dim
     total = k.shape[0]
-    ks = _token_rows(k, "k", total, c.heads_kv, c.head_dim)
-    vs = _token_rows(v, "v", total, c.heads_kv, c.head_dim)
-    if cu_new is not None:
-        _dev(cu_new, "int32", "cu_new", c.num_seqs + 1)
-    rows = rot = 0
+    kp, ks = _token_rows(k, "k", total, hkv, d, here)
+    vp, vs = _token_rows(v, "v", total, hkv, d, here)
+    cu = 0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here)
+    table = rows = rot = 0
     if cos_sin is not None:
-        _dev(cos_sin, "float32", "cos_sin")
+        table = _arg(cos_sin, "float32", "cos_sin", None, here)
         if cos_sin.dim() != 2:
             raise ValueError("cos_sin must be [positions, rot_dim]")
         rows, rot = cos_sin.shape
-    if k_out is not None:
-        _dev(k_out, "bfloat16", "k_out", total * c.heads_kv * c.head_dim)
-    heads = qs = 0
+    ko = 0 if k_out is None else _arg(k_out, "bfloat16", "k_out", total * hkv * d, here)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out come together")
+    heads = qp = qs = qo = 0
     if q is not None:
         heads = q.shape[1]
-        qs = _token_rows(q, "q", total, heads, c.head_dim)
-        _dev(q_out, "bfloat16", "q_out", total * heads * c.head_dim)
-    _one_device(k, v, cu_new, cos_sin, k_out, q, q_out, cache.tensors[0])
-    _check(lib().hsap_cache_append(ctypes.byref(c), ctypes.byref(cache.buffers), _ptr(k), ks, _ptr(v), vs, _ptr(cu_new), total,
-                                   _ptr(cos_sin), rows, rot, int(bool(interleaved)), _ptr(k_out), _ptr(q), qs, heads,
-                                   _ptr(q_out), _stream(stream)))
+        qp, qs = _token_rows(q, "q", total, heads, d, here)
+        qo = _arg(q_out, "bfloat16", "q_out", total * heads * d, here)
+    _check(lib().hsap_cache_append(*cache._refs, kp, ks, vp, vs, cu, total, table, rows, rot, 1 if interleaved else 0, ko, qp,
+                                   qs, heads, qo, _stream(stream)))
 
 
 def cache_attn_workspace(cache: KVCache, heads_q: int, total_q: int, one_each: Optional[bool] = None) -> int:
@@ -845,19 +858,15 @@ def cache_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_new, o_
                window: int = MAX_WINDOW, sinks: int = 0, stream=None) -> None:
     """hsap_cache_attn: q bf16 [total_q, Hq, d] (rows may be strided; the sequences' newest tokens) over the cache ->
     o_out bf16 [total_q, Hq, d], lse_out fp32 [Hq, total_q] or None; workspace: uint8, cache_attn_workspace bytes."""
-    c = cache.desc
+    here, c = _cache_here(cache), cache.desc
     total = q.shape[0]
-    qs = _token_rows(q, "q", total, int(heads_q), c.head_dim)
-    if cu_new is not None:
-        _dev(cu_new, "int32", "cu_new", c.num_seqs + 1)
-    _dev(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim)
-    if lse_out is not None:
-        _dev(lse_out, "float32", "lse_out", total * heads_q)
-    _dev(workspace, "uint8", "workspace")
-    _one_device(q, cu_new, o_out, lse_out, workspace, cache.tensors[0])
-    _check(lib().hsap_cache_attn(ctypes.byref(c), ctypes.byref(cache.buffers), int(heads_q), float(softmax_scale),
-                                 _extent(window, "window"), _extent(sinks, "sinks"), _ptr(q), qs, _ptr(cu_new), total,
-                                 _ptr(o_out), _ptr(lse_out), _ptr(workspace), workspace.numel(), _stream(stream)))
+    qp, qs = _token_rows(q, "q", total, heads_q, c.head_dim, here)
+    _check(lib().hsap_cache_attn(
+        *cache._refs, heads_q, softmax_scale, _extent(window, "window"), _extent(sinks, "sinks"), qp, qs,
+        0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here), total,
+        _arg(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim, here),
+        0 if lse_out is None else _arg(lse_out, "float32", "lse_out", total * heads_q, here),
+        _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------

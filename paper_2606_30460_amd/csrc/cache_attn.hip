@@ -446,10 +446,18 @@ __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
   for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
   __syncthreads();
   f32x4 acc = f32x4{};
-#pragma unroll 4
-  for (int s = grp; s < a.splits; s += GROUPS) {
-    const float f = weight[s];
-    if (f > 0.f) acc += f * *(const f32x4*)(a.part_o + (s * rows + row) * D + 4 * x);
+  for (int s0 = grp; s0 < a.splits; s0 += 8 * GROUPS) {  // eight loads in flight
+    f32x4 o[8];
+    float f[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const int s = min(s0 + y * GROUPS, a.splits - 1);
+      f[y] = s0 + y * GROUPS < a.splits ? weight[s] : 0.f;
+      o[y] = *(const f32x4*)(a.part_o + (s * rows + row) * D + 4 * x);
+    }
+#pragma unroll
+    for (int y = 0; y < 8; ++y)
+      if (f[y] > 0.f) acc += f[y] * o[y];  // (the rows of an idle split are not written)
   }
   part[grp][x] = acc;
   __syncthreads();
