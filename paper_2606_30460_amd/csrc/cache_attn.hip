@@ -38,6 +38,7 @@ struct CacheAttnArgs {
   float* part_lse; // [splits, total_q, Hq], log2 units
   int32_t heads_q;
   int32_t group;
+  int32_t page_shift;  // log2 of the page size
   int32_t window;
   int32_t sinks;
   int32_t tiles;   // row tiles, all sequences
@@ -104,8 +105,18 @@ __device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, i
   return t.count > 0 && row0 < (int64_t)t.count * a.group;
 }
 
-template <int D, int MT>
-__global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) void cache_attn_kernel(CacheAttnArgs a) {
+template <typename T, bool ONCE>
+__device__ __forceinline__ T read_codes(const uint8_t* p) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+  if constexpr (ONCE) return __builtin_bit_cast(T, __builtin_nontemporal_load((const words*)p));
+  else return *(const T*)p;
+}
+
+// ONCE: every code is read by one workgroup of the call alone and the cache is larger than the 256 MB behind the L2s: the
+// loads are marked as streaming (64 sequences of 8k tokens, 8 heads of 128: 128 -> 119 us; with several row tiles per
+// sequence 46 -> 49 us, with 67 MB of codes, which the next call finds there again, 21.8 -> 22.5 us).
+template <int D, int MT, bool ONCE>
+__global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_kernel(CacheAttnArgs a) {
   constexpr int KX = D / 64, CB = D / 16, ROWS = 16 * MT;  // 16-byte loads per K row and lane; d values per lane of V
   constexpr float NEG_INF = -__builtin_inff();
   constexpr float RESCALE_SLACK = 8.f;
@@ -161,25 +172,40 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
     int32_t j0;
     bool held[2];  // each half of 16 tokens lies in a page and has a token that is seen
   };
-  auto load = [&](int32_t s, Tokens& x) __attribute__((always_inline)) {
-    x.j0 = s < steps.sinks ? 32 * s : steps.win0 + 32 * (s - steps.sinks);
+  // Pages of a step's halves (-1: none), looked up a step before its codes are asked for, those a step before their use.
+  struct Where {
+    int32_t page[2];
+  };
+  auto first_token = [&](int32_t s) { return s < steps.sinks ? 32 * s : steps.win0 + 32 * (s - steps.sinks); };
+  auto look_up = [&](int32_t s) __attribute__((always_inline)) {
+    Where x{{-1, -1}};
+    if (s < s_end) {
+      const int32_t j0 = first_token(s);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int32_t at = (j0 + 16 * half) >> a.page_shift;
+        if (j0 + 16 * half <= top) x.page[half] = table[at];  // (top is below the table's capacity)
+      }
+    }
+    return x;
+  };
+  auto load = [&](int32_t s, const Where& where, Tokens& x) __attribute__((always_inline)) {
+    x.j0 = first_token(s);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int32_t j = x.j0 + 16 * half;
-      const int32_t found = j <= top ? cache_page(table, a.d.table_width, a.d.num_pages, ps, j) : -1;
-      const int32_t page = max(found, 0);
+      x.held[half] = (uint32_t)where.page[half] < (uint32_t)a.d.num_pages;
+      const int32_t page = x.held[half] ? where.page[half] : 0;
       const int64_t at = (int64_t)page * a.d.heads_kv + g;
-      x.ks[half] = a.c.k_scale[at];
-      x.vs[half] = a.c.v_scale[at];
-      x.held[half] = found >= 0;
-      if (found < 0) x.ks[half] = x.vs[half] = 0.f;
-      const int64_t row = at * ps + (j & (ps - 1));
+      x.ks[half] = x.held[half] ? a.c.k_scale[at] : 0.f;
+      x.vs[half] = x.held[half] ? a.c.v_scale[at] : 0.f;
+      const int64_t row = (at << a.page_shift) + (j & (ps - 1));
       const uint8_t* kp = a.c.k_codes + (row + l16) * D + 16 * grp;
 #pragma unroll
-      for (int y = 0; y < KX; ++y) x.k[half][y] = *(const uint4*)(kp + 64 * y);
+      for (int y = 0; y < KX; ++y) x.k[half][y] = read_codes<uint4, ONCE>(kp + 64 * y);
       const uint8_t* vp = a.c.v_codes + (row + 4 * grp) * D + CB * l16;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) x.v[4 * half + y] = *(const VT*)(vp + y * D);
+      for (int y = 0; y < 4; ++y) x.v[4 * half + y] = read_codes<VT, ONCE>(vp + y * D);
     }
   };
 
@@ -297,10 +323,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : MT == 4 && D == 128 ? 1 : 2) voi
   int32_t s = s_begin + w;
   if (s < s_end) {
     Tokens x, y;
-    load(s, x);
+    load(s, look_up(s), x);
+    Where next = look_up(s + 4);
     for (;;) {
       const bool more = s + 4 < s_end;
-      if (more) load(s + 4, y);
+      if (more) load(s + 4, next, y);
+      next = look_up(s + 8);
       compute(x, s);
       if (!more) break;
       s += 4;
@@ -414,9 +442,9 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a) {
     a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
 }
 
-// More splits: a workgroup per row.  Every wave forms the weights of all splits (up to 256, four to a lane); the
+// More splits: a workgroup per row.  Every wave forms the weights of all splits (up to 128, two to a lane); the
 // 256 / (D / 4) groups of lanes then take every so manieth split and are added up in LDS.
-constexpr int kMaxSplits = 256;
+constexpr int kMaxSplits = 128;
 template <int D>
 __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
   constexpr float NEG_INF = -__builtin_inff();
@@ -471,7 +499,8 @@ __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
 }
 
 // How a call is cut: row tiles of 16 mt rows, and splits of a tile's tokens so that the grid fills the chip, each of
-// at least 256 tokens.
+// at least 256 tokens, at most 128 (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits 24.5, 128 19.4,
+// 256 22.0: more partials to join).
 struct CacheCut {
   int mt;
   int64_t tiles;
@@ -496,9 +525,14 @@ static int64_t cache_workspace(const CacheCut& c, int32_t heads_q, int64_t total
   return c.splits == 1 ? 0 : (int64_t)c.splits * total_q * heads_q * (head_dim + 1) * 4;
 }
 
-template <int D, int MT>
-static void launch_cache_attn(const CacheAttnArgs& a, int64_t blocks, hipStream_t s) {
-  hipLaunchKernelGGL((cache_attn_kernel<D, MT>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+template <int D>
+static void launch_cache_attn(const CacheAttnArgs& a, int mt, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(256);
+  const int64_t bytes = 2 * (int64_t)a.d.num_seqs * a.d.table_width * a.d.page_size * a.d.heads_kv * D;
+  if (mt == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 4, false>), grid, block, 0, s, a);
+  else if (mt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
+  else if (!a.cu && bytes > (int64_t(256) << 20)) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false>), grid, block, 0, s, a);
 }
 
 }  // namespace hsap
@@ -557,6 +591,7 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   a.part_lse = a.part_o + (int64_t)c.splits * total_q * heads_q * d;
   a.heads_q = heads_q;
   a.group = heads_q / desc->heads_kv;
+  a.page_shift = __builtin_ctz((unsigned)desc->page_size);
   a.window = window;
   a.sinks = sinks;
   a.tiles = (int32_t)c.tiles;
@@ -565,10 +600,8 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
   if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
-  if (d == 128) c.mt == 1 ? launch_cache_attn<128, 1>(a, blocks, s) : c.mt == 2 ? launch_cache_attn<128, 2>(a, blocks, s)
-                                                                                 : launch_cache_attn<128, 4>(a, blocks, s);
-  else c.mt == 1 ? launch_cache_attn<64, 1>(a, blocks, s) : c.mt == 2 ? launch_cache_attn<64, 2>(a, blocks, s)
-                                                                       : launch_cache_attn<64, 4>(a, blocks, s);
+  if (d == 128) launch_cache_attn<128>(a, c.mt, blocks, s);
+  else launch_cache_attn<64>(a, c.mt, blocks, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
   if (c.splits > 1) {
