@@ -68,10 +68,10 @@ __device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// four e4m3 codes to bf16 (exact)
-__device__ __forceinline__ void decode4(uint32_t w, bf16x2& lo, bf16x2& hi) {
-  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true);
+// four e4m3 codes times a power of two to bf16 (exact within bf16's range)
+__device__ __forceinline__ void decode4(uint32_t w, float pow2, bf16x2& lo, bf16x2& hi) {
+  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, false);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, true);
 }
 
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_k
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           bf16x2 p0, p1, p2, p3;
-          decode4(c[2 * e], p0, p1);
-          decode4(c[2 * e + 1], p2, p3);
+          decode4(c[2 * e], 1.f, p0, p1);
+          decode4(c[2 * e + 1], 1.f, p2, p3);
           kf[half][2 * y + e] = bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
         }
       }
@@ -239,6 +239,17 @@ __global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_k
     // tokens that the sink steps show belong to them alone; a window step's may be sinks too
     const int32_t sinks = s < steps.sinks ? min(a.sinks, steps.win0) : a.sinks;
     const int32_t near = s < steps.sinks ? 0 : a.window;
+    // every row of the tile sees every token of the step
+    const bool all = x.held[0] && x.held[1] && jl <= plo && (phi - x.j0 < near || jl < sinks);
+    // V's scale: its power of two goes into the conversion of the codes, what is left of it (1 for the scales that an
+    // append makes) into P
+    float vpow[2], vrest[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      vpow[half] = __uint_as_float(__float_as_uint(x.vs[half]) & 0x7F800000u);
+      vrest[half] = __uint_as_float((__float_as_uint(x.vs[half]) & 0x007FFFFFu) | 0x3F800000u);
+    }
+    const bool rest = vrest[0] != 1.f || vrest[1] != 1.f;
     bf16x8 pf[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -247,9 +258,8 @@ __global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_k
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int kk = 0; kk < 2 * KX; ++kk) sc[half] = mfma16(kf[half][kk], qf[mt][kk], sc[half]);
-      const bool all = x.held[0] && x.held[1] && jl <= pos[mt] && (pos[mt] - x.j0 < near || jl < sinks);
       const float sl[2] = {fmaxf(x.ks[0] * a.scale_log2, 1.17549435e-38f), fmaxf(x.ks[1] * a.scale_log2, 1.17549435e-38f)};
-      if (__builtin_amdgcn_ballot_w64(!all) != 0) {
+      if (!all) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -274,14 +284,21 @@ __global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_k
         m_run[mt] = m_new;
       }
       const float m_use = m_run[mt] == NEG_INF ? 0.f : m_run[mt];
+      float pr[8];
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float p = fast_exp2(__builtin_fmaf(sc[half][e], sl[half], -m_use));
           l_run[mt] += p;
-          pf[mt][4 * half + e] = (__bf16)(p * x.vs[half]);
+          pr[4 * half + e] = p;
         }
+      if (rest) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] *= vrest[e >> 2];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[mt][e] = (__bf16)pr[e];
     }
     // V operand: rows d = CB l16 + c, the lane's eight tokens
     VT v[8];
@@ -307,8 +324,8 @@ __global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_k
         }
         // bytes (u0.0, u1.0, u0.1, u1.1) and (u0.2, u1.2, u0.3, u1.3): v_perm selects 0..3 from its second operand
         const uint32_t lo = __builtin_amdgcn_perm(u1, u0, 0x05010400u), hi = __builtin_amdgcn_perm(u1, u0, 0x07030602u);
-        decode4(lo, turned[0][y], turned[1][y]);
-        decode4(hi, turned[2][y], turned[3][y]);
+        decode4(lo, vpow[y >> 1], turned[0][y], turned[1][y]);
+        decode4(hi, vpow[y >> 1], turned[2][y], turned[3][y]);
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -507,7 +524,10 @@ struct CacheCut {
   int32_t splits;
 };
 
-constexpr int64_t kCacheGrid = 1024;  // workgroups to aim at
+// Workgroups to aim at: what the chip holds at once, and twice that where a workgroup is short of work for the time that its
+// loads take (one 16-row block: 64 sequences of 8k tokens 129 us with 512, 128 with 1024, 127 with 2048; four blocks:
+// 3 x 700 rows 44 us with 512, 46 with 1024, 68 with 2048, where the fp32 partials weigh more).
+constexpr int64_t kCacheGrid = 512;
 
 static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
@@ -517,7 +537,7 @@ static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tot
   c.tiles = one_each ? (int64_t)d.num_seqs * ((group + 16 * c.mt - 1) / (16 * c.mt))
                      : item_base(total_q, group, 16 * c.mt, 1, d.num_seqs);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
-  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, (c.mt == 1 ? 2 : 1) * kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
   return c;
 }
 

@@ -348,3 +348,13 @@ def test_serving_run():
         want, tol, _, _ = C.attention(q1.float().double().cpu().numpy(), codes[0], codes[2], codes[1], codes[3], p.table, lens,
                                       [0, 1, 2, 3], window, sinks, scale)
         assert (np.abs(o1.float().cpu().numpy() - want) <= tol + 1e-9).all(), step
+
+
+def test_scales_that_are_no_powers_of_two():
+    # a cache filled by other means: any positive scale
+    p = Pages([200, 77], 32, 2, 128, seed=15).fill([200, 77])
+    rng = np.random.default_rng(1)
+    for x in "kv":
+        p.scales[x] *= rng.uniform(0.3, 3.0, p.scales[x].shape).astype(np.float32)
+    _check_attn([200, 77], [1, 1], 32, 4, 2, 128, pages=p, one=True, seed=15)
+    _check_attn([200, 77], [40, 9], 32, 4, 2, 128, pages=p, seed=16)
