@@ -26,6 +26,26 @@ __device__ __forceinline__ int32_t segment_start(const Geom& g, int32_t x, int32
   return (int32_t)global_pos(g, x, (int64_t)sg * g.m);
 }
 
+// 32-row blocks of a workgroup's four waves: four, or fewer, each then taken by several waves that share its steps as
+// streams, so that a small grid has more and shorter workgroups.  `tiles`: workgroups that four blocks would give.  A split
+// pays as long as all its workgroups are resident at once: one per CU at head_dim 128, two at 64 (their LDS).
+// Measured on one document, us, four blocks -> two -> one:
+//   forward, d 64, window 300:   64 tiles 14.0 -> 9.2, 256 tiles 14.8 -> 11.7, 282 tiles 17.6 -> 18.9
+//   forward, d 128, window 300:  128 tiles 17.9 -> 13.6, 256 tiles 19.2 -> 24.8
+//   whole backward by dK/dV's choice, d 64:   64 tiles 72 -> 49 -> 39, 128 tiles 72 -> 50 -> 45, 256 tiles 94 -> 77 -> 85,
+//     512 tiles 130 -> 132 -> 151
+//   d 128:  64 tiles 112 -> 73 -> 62, 128 tiles 119 -> 80 -> 96, 256 tiles 157 -> 164 -> 195
+inline int window_row_blocks(int64_t tiles, int head_dim) {
+  const int64_t resident = kComputeUnits * (head_dim == 64 ? 2 : 1);
+  return 4 * tiles <= resident ? 1 : 2 * tiles <= resident ? 2 : 4;
+}
+inline int64_t window_q_tiles(const Geom& g, int heads_q) { return g.n / g.m * ((g.m + 127) / 128) * heads_q; }
+// (of the chunks' keys, those that the shard's windows reach)
+inline int64_t window_key_tiles(const Geom& g, int heads_kv, int64_t window) {
+  const int64_t keys = g.n / g.m * (g.m + window);
+  return (keys < g.N ? keys : g.N) / 128 * heads_kv;
+}
+
 // Storage of keys in sharded order as runs of consecutive positions: [lo, hi) are the positions whose row is
 // position + delta.  One chunk of a contiguous layout of one shard holds everything.
 struct KeySpan {

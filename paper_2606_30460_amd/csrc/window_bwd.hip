@@ -52,20 +52,44 @@ struct WindowBwdArgs {
   float scale_log2;
 };
 
+// Adds the streams' sums onto stream 0's, in stream order, through LDS (register by register: no bank conflict).
+template <int N, int WAVES, int KS>
+__device__ __forceinline__ void join_streams(f32x16 (&sum)[N], float* res, int w, int ks, int lane) {
+  if (ks > 0) {
+    float* const mine = res + ((ks - 1) * WAVES + w) * N * 16 * 64 + lane;
+#pragma unroll
+    for (int mb = 0; mb < N; ++mb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mine[(16 * mb + j) * 64] = sum[mb][j];
+  }
+  hsap_lds_barrier();
+  if (ks == 0) {
+    for (int x = 1; x < KS; ++x) {
+      const float* const other = res + ((x - 1) * WAVES + w) * N * 16 * 64 + lane;
+#pragma unroll
+      for (int mb = 0; mb < N; ++mb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[mb][j] += other[(16 * mb + j) * 64];
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // dQ: the forward's ranges, three products per 64-key step (S, dP and dS K).  dP - delta is formed by the matrix
 // product itself, whose accumulator starts at -delta.
 // ---------------------------------------------------------------------------
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs a) {
+template <int D, int WAVES, int KS>
+__global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_dq_kernel(WindowBwdArgs a) {
   constexpr int KB = 64, CPR = D / 8, TILE = KB * D, BM = 32 * WAVES;
   constexpr float NEG_INF = -__builtin_inff();
-  __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // K slots 0, 1, then V slots 0, 1
+  __shared__ __attribute__((aligned(16))) __bf16 rings[KS * 4 * TILE];  // per stream: K slots 0, 1, then V slots 0, 1
   __shared__ int32_t tile_start;
+  static_assert(KS == 1 || KS * 4 * TILE * 2 >= (KS - 1) * WAVES * (D / 2) * 256, "room for the streams' results");
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int w = uniform(tid >> 6);
+  const int w = uniform(tid >> 6) % WAVES, ks = uniform(tid >> 6) / WAVES;  // 32-row slice, key stream
+  __bf16* const ring = rings + ks * 4 * TILE;
   auto Ks = [&](int slot) { return ring + slot * TILE; };
   auto Vs = [&](int slot) { return ring + (2 + slot) * TILE; };
   int t, h;
@@ -106,7 +130,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
   const int32_t win_lo = max(start0, i0 - (a.window - 1));
   const int32_t sink_hi = start0 + min(a.sinks, win_lo - start0);
   const int32_t sink_steps = (sink_hi - start0 + KB - 1) / KB;
-  const int32_t total = sink_steps + (i1 - win_lo + KB) / KB;
+  const int32_t steps = sink_steps + (i1 - win_lo + KB) / KB;
+  const int32_t total = KS == 1 ? steps : (steps - ks + KS - 1) / KS;  // this stream's: ks, ks + KS, ...
   const int32_t wlo = max(doc.start, gq - (a.window - 1));
   const int32_t slen = min(a.sinks, wlo - doc.start);
 
@@ -142,12 +167,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
     sum = pair_sum(sum);
     if (few) delta = sum;
   }
-  if (hi == 0 && valid) a.delta[(int64_t)h * n + qrow] = delta;
+  if (hi == 0 && valid && ks == 0) a.delta[(int64_t)h * n + qrow] = delta;
 
   TileStage<D, WAVES> st;
   st.init(w, lane, rstride * 2);
   KeySpan span{0, 0, 0};
-  auto stage = [&](int s, int slot) {
+  auto stage = [&](int i, int slot) {
+    const int s = KS * i + ks;
     const int32_t j0 = s < sink_steps ? start0 + KB * s : win_lo + KB * (s - sink_steps);
     const int32_t jmax = s < sink_steps ? sink_hi - 1 : i1;
     stage_keys<D, WAVES>(st, a.geom, span, j0, jmax, kbase, rstride, Ks(slot));
@@ -170,11 +196,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
 #pragma unroll
   for (int j = 0; j < 16; ++j) minus_delta[j] = -delta;
 
-  stage(0, 0);
+  if (KS == 1 || total > 0) stage(0, 0);
   vm_wait_barrier<0>();
-  auto step = [&](int s, auto par) __attribute__((always_inline)) {
+  auto step = [&](int i, auto par) __attribute__((always_inline)) {
     constexpr int S0 = decltype(par)::value, S1 = S0 ^ 1;
-    if (s + 1 < total) stage(s + 1, S1);
+    if (i + 1 < total) stage(i + 1, S1);
+    const int s = KS * i + ks;
     const bool sink_step = s < sink_steps;
     const int32_t j0 = sink_step ? start0 + KB * s : win_lo + KB * (s - sink_steps);
     const uint32_t wlen = sink_step || !valid ? 0u : (uint32_t)(gq - wlo + 1);
@@ -212,10 +239,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
     }
     vm_wait_barrier<0>();
   };
-  for (int s = 0; s < total; s += 2) {
-    step(s, std::integral_constant<int, 0>{});
-    if (s + 1 < total) step(s + 1, std::integral_constant<int, 1>{});
+  // every stream takes part in the barriers of the longest one (the first)
+  const int most = KS == 1 ? total : (steps + KS - 1) / KS;
+  for (int s = 0; s < most; s += 2) {
+    if (KS == 1 || s < total) step(s, std::integral_constant<int, 0>{});
+    else vm_wait_barrier<0>();
+    if (s + 1 < most) {
+      if (KS == 1 || s + 1 < total) step(s + 1, std::integral_constant<int, 1>{});
+      else vm_wait_barrier<0>();
+    }
   }
+  if constexpr (KS > 1) join_streams<D / 32, WAVES, KS>(dq, (float*)rings, w, ks, lane);
+  if (KS > 1 && ks > 0) return;
 
   if (!valid) return;
   __bf16* op = a.dq + (qrow * a.hq + h) * D + 4 * hi;
@@ -239,20 +274,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_dq_kernel(WindowBwdArgs 
 // SINKS: the keys are the sinks, up to the chunk's first position, of the document that holds that position and began
 // before it; the queries those of the chunk outside the window.
 // ---------------------------------------------------------------------------
-template <int D, bool SINKS>
-__global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
-  constexpr int WAVES = 4, BN = 32 * WAVES, CPR = D / 8;
+template <int D, bool SINKS, int WAVES, int KS>
+__global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) void window_dkv_kernel(WindowBwdArgs a) {
+  constexpr int BN = 32 * WAVES, CPR = D / 8;
   constexpr bool VLDS = D == 128;       // V in LDS: its fragments, K's and the two sums do not fit the registers together
-  constexpr int QB = VLDS ? 32 : 64, TILE = QB * D;
+  constexpr int QB = VLDS || WAVES == 1 ? 32 : 64, TILE = QB * D;
   constexpr float NEG_INF = -__builtin_inff();
+  static_assert(KS == 1 || KS * 4 * TILE * 2 >= (KS - 1) * WAVES * (D / 2) * 256, "room for the streams' results");
   __shared__ __attribute__((aligned(16))) __bf16 vtile[VLDS ? BN * D : 8];
-  __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // Q slots 0, 1, then dO slots 0, 1
-  __shared__ __attribute__((aligned(16))) float rows_s[2][2][QB];   // [slot][LSE in log2 units, -delta]
+  __shared__ __attribute__((aligned(16))) __bf16 rings[KS * 4 * TILE];  // per stream: Q slots 0, 1, then dO slots 0, 1
+  __shared__ __attribute__((aligned(16))) float rows_all[KS][2][2][QB];   // [slot][LSE in log2 units, -delta]
   __shared__ int32_t last_s[WAVES][2];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int w = uniform(tid >> 6);
+  const int w = uniform(tid >> 6) % WAVES, ks = uniform(tid >> 6) / WAVES;  // 32 keys, stream of query steps
+  const int sid = tid - 64 * WAVES * ks;                                    // thread of the stream
+  __bf16* const ring = rings + ks * 4 * TILE;
+  auto& rows_s = rows_all[ks];
   const int grp = a.hq / a.hkv;
   const int g = blockIdx.x % a.hkv;
   const int32_t tile = blockIdx.x / a.hkv;
@@ -321,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
       int32_t e = key + len[x];
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o));
-      if (lane == 0) last_s[w][x] = e;
+      if (lane == 0 && ks == 0) last_s[w][x] = e;
     }
     __syncthreads();
 #pragma unroll
@@ -335,13 +374,14 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
   }
   const int32_t cnt0 = max(0, (seg_hi[0] - seg_lo[0] + QB - 1) / QB);
   const int32_t cnt1 = SINKS ? 0 : max(0, (seg_hi[1] - seg_lo[1] + QB - 1) / QB);
-  const int32_t total = (cnt0 + cnt1) * grp;
+  const int32_t steps = (cnt0 + cnt1) * grp;
+  const int32_t total = KS == 1 ? steps : (steps - ks + KS - 1) / KS;  // this stream's: ks, ks + KS, ...
 
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int mb = 0; mb < D / 32; ++mb) dk[mb] = dv[mb] = f32x16{};
 
-  if (total > 0) {
+  if (steps > 0) {
     bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
     {
       const int64_t at = (krow * a.hkv + g) * D + 8 * hi;
@@ -349,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
       for (int kk = 0; kk < D / 16; ++kk) {
         kf[kk] = *(const bf16x8*)(a.k + at + 16 * kk);
         const bf16x8 x = *(const bf16x8*)(a.v + at + 16 * kk);
-        if constexpr (VLDS) *(bf16x8*)(vtile + 32 * w * D + swz<CPR>(l32, 16 * kk + 8 * hi)) = x;  // read by this wave alone
+        if constexpr (VLDS) *(bf16x8*)(vtile + 32 * w * D + swz<CPR>(l32, 16 * kk + 8 * hi)) = x;  // (the streams' are the same)
         else vf[kk] = x;
       }
     }
@@ -360,14 +400,16 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
     struct Step {
       int32_t x, hh, s;
     };
-    auto advance = [&](Step& p) {
-      if (++p.s < (p.x ? cnt1 : cnt0)) return;
-      p.s = 0;
-      if (++p.hh < grp) return;
-      p.hh = 0;
-      ++p.x;
+    auto advance = [&](Step& p, int by) {
+      for (int y = 0; y < by; ++y) {
+        if (++p.s < (p.x ? cnt1 : cnt0)) continue;
+        p.s = 0;
+        if (++p.hh < grp) continue;
+        p.hh = 0;
+        ++p.x;
+      }
     };
-    float row_next = 0.f;  // the next step's LSE (threads 0 .. QB - 1) or delta (the next QB) of a row
+    float row_next = 0.f;  // the next step's LSE (the stream's threads 0 .. QB - 1) or delta (the next QB) of a row
     auto stage = [&](const Step& p, int slot) {
       const int32_t lo = p.x ? seg_lo[1] : seg_lo[0], top = p.x ? seg_hi[1] : seg_hi[0];
       const int32_t pos = lo + QB * p.s;
@@ -384,10 +426,10 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
         st.gather([&](int r) { return qb + min(r, most) * rstride; }, ring + slot * TILE);
         st.gather([&](int r) { return ob + min(r, most) * rstride; }, ring + (2 + slot) * TILE);
       }
-      if (tid < 2 * QB) row_next = (tid < QB ? a.lse : a.delta)[(int64_t)h * n + r0 + min(tid % QB, most)];
+      if (sid < 2 * QB) row_next = (sid < QB ? a.lse : a.delta)[(int64_t)h * n + r0 + min(sid % QB, most)];
     };
     auto store_rows = [&](int slot) {
-      if (tid < 2 * QB) rows_s[slot][tid / QB][tid % QB] = tid < QB ? row_next * kLog2e : -row_next;
+      if (sid < 2 * QB) rows_s[slot][sid / QB][sid % QB] = sid < QB ? row_next * kLog2e : -row_next;
     };
     const int tr_row = 4 * hi + ((lane & 15) >> 2);
     const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -399,11 +441,15 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) troff[mb][k] = swz<CPR>(8 * k + tr_row, 32 * mb + tr_col) - 8 * k * D;
 
-    Step cur{cnt0 > 0 ? 0 : 1, 0, 0}, nxt = cur;
-    stage(cur, 0);
-    store_rows(0);
+    Step cur{cnt0 > 0 ? 0 : 1, 0, 0};
+    if (KS == 1 || total > 0) {
+      advance(cur, ks);
+      stage(cur, 0);
+      store_rows(0);
+    }
     vm_wait_barrier<0>();
-    advance(nxt);
+    Step nxt = cur;
+    if (total > 1) advance(nxt, KS);
     auto step = [&](int i, auto par) __attribute__((always_inline)) {
       constexpr int S0 = decltype(par)::value, S1 = S0 ^ 1;
       if (i + 1 < total) stage(nxt, S1);
@@ -456,13 +502,25 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowBwdArgs a) {
       if (i + 1 < total) store_rows(S1);
       vm_wait_barrier<0>();
       cur = nxt;
-      if (i + 2 < total) advance(nxt);
+      if (i + 2 < total) advance(nxt, KS);
     };
-    for (int i = 0; i < total; i += 2) {
-      step(i, std::integral_constant<int, 0>{});
-      if (i + 1 < total) step(i + 1, std::integral_constant<int, 1>{});
+    // every stream takes part in the barriers of the longest one (the first)
+    const int most = KS == 1 ? total : (steps + KS - 1) / KS;
+    for (int i = 0; i < most; i += 2) {
+      if (KS == 1 || i < total) step(i, std::integral_constant<int, 0>{});
+      else vm_wait_barrier<0>();
+      if (i + 1 < most) {
+        if (KS == 1 || i + 1 < total) step(i + 1, std::integral_constant<int, 1>{});
+        else vm_wait_barrier<0>();
+      }
+    }
+    if constexpr (KS > 1) {
+      join_streams<D / 32, WAVES, KS>(dk, (float*)rings, w, ks, lane);
+      hsap_lds_barrier();
+      join_streams<D / 32, WAVES, KS>(dv, (float*)rings, w, ks, lane);
     }
   }
+  if (KS > 1 && ks > 0) return;
 
   if constexpr (SINKS) {
     // every sink of the document; those at or behind the chunk's first position are zeros
@@ -571,30 +629,47 @@ static int64_t bwd_workspace(const hsap_attn_desc* d, const Geom& g, int32_t win
   return delta_bytes(d, g) + g.n / g.m * sink_chunks(g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
 }
 
+template <int D, int WAVES, int KS>
+static hsap_status launch_dq(WindowBwdArgs& a, hipStream_t s) {
+  a.tiles = (int32_t)((a.geom.m + 32 * WAVES - 1) / (32 * WAVES));
+  const int64_t blocks = a.geom.n / a.geom.m * a.tiles * a.hq;
+  if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
+  hipLaunchKernelGGL((window_dq_kernel<D, WAVES, KS>), dim3((unsigned)blocks), dim3(64 * WAVES * KS), 0, s, a);
+  return check_launch_window("window_attn_bwd dQ");
+}
+
+template <int D, bool SINKS, int WAVES, int KS>
+static hsap_status launch_dkv(WindowBwdArgs& a, hipStream_t s) {
+  const int64_t segs = a.geom.n / a.geom.m;
+  a.tiles = (int32_t)((a.geom.m + 32 * WAVES - 1) / (32 * WAVES));
+  const int64_t blocks = (SINKS ? segs * a.chunks : segs * a.geom.P * a.tiles) * a.hkv;
+  if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
+  hipLaunchKernelGGL((window_dkv_kernel<D, SINKS, WAVES, KS>), dim3((unsigned)blocks), dim3(64 * WAVES * KS), 0, s, a);
+  return check_launch_window(SINKS ? "window_attn_bwd sinks" : "window_attn_bwd dK/dV");
+}
+
 template <int D>
 static hsap_status launch_window_bwd(WindowBwdArgs& a, hipStream_t s) {
-  const Geom& g = a.geom;
-  const int64_t segs = g.n / g.m;
-  a.tiles = (int32_t)((g.m + 127) / 128);
-  const int64_t q_blocks = segs * a.tiles * a.hq, k_blocks = segs * g.P * a.tiles * a.hkv, s_blocks = segs * a.chunks * a.hkv;
-  if (q_blocks > INT32_MAX || k_blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
-  hipLaunchKernelGGL((window_dq_kernel<D, 4>), dim3((unsigned)q_blocks), dim3(256), 0, s, a);
-  hsap_status st = check_launch_window("window_attn_bwd dQ");
+  hsap_status st = window_row_blocks(window_q_tiles(a.geom, a.hq), D) < 4 ? launch_dq<D, 2, 2>(a, s) : launch_dq<D, 4, 1>(a, s);
   if (st != HSAP_OK) return st;
-  if (s_blocks) {
-    hipLaunchKernelGGL((window_dkv_kernel<D, true>), dim3((unsigned)s_blocks), dim3(256), 0, s, a);
-    st = check_launch_window("window_attn_bwd sinks");
+  if (a.chunks) {
+    // as many key blocks as there are sinks; the other waves are streams over the queries
+    st = a.sinks <= 32 ? launch_dkv<D, true, 1, 4>(a, s) : a.sinks <= 64 ? launch_dkv<D, true, 2, 2>(a, s) : launch_dkv<D, true, 4, 1>(a, s);
     if (st != HSAP_OK) return st;
     if (a.chunks > 1) {
-      hipLaunchKernelGGL(window_sink_sum_kernel, dim3((unsigned)s_blocks), dim3(256), 0, s, a, a.sinks * 2 * D);
+      const int64_t blocks = a.geom.n / a.geom.m * a.chunks * a.hkv;
+      hipLaunchKernelGGL(window_sink_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, a.sinks * 2 * D);
       st = check_launch_window("window_attn_bwd sink sum");
       if (st != HSAP_OK) return st;
     }
   } else {
     a.partial = nullptr;
   }
-  hipLaunchKernelGGL((window_dkv_kernel<D, false>), dim3((unsigned)k_blocks), dim3(256), 0, s, a);
-  return check_launch_window("window_attn_bwd dK/dV");
+  switch (window_row_blocks(window_key_tiles(a.geom, a.hkv, a.window), D)) {
+    case 1: return launch_dkv<D, false, 1, 4>(a, s);
+    case 2: return launch_dkv<D, false, 2, 2>(a, s);
+    default: return launch_dkv<D, false, 4, 1>(a, s);
+  }
 }
 
 }  // namespace hsap

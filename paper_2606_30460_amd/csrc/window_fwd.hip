@@ -38,17 +38,19 @@ struct WindowFwdArgs {
   float scale_log2;
 };
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel(WindowFwdArgs a) {
+template <int D, int WAVES, int KS>
+__global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : D == 64 && KS == 1 ? 3 : 2) void window_fwd_kernel(WindowFwdArgs a) {
   constexpr int KB = 64, CPR = D / 8, TILE = KB * D, BM = 32 * WAVES;
   constexpr float NEG_INF = -__builtin_inff();
   constexpr float RESCALE_SLACK = 8.f;  // log2 units a row maximum may rise before O is rescaled
-  __shared__ __attribute__((aligned(16))) __bf16 ring[4 * TILE];  // K slots 0, 1, then V slots 0, 1
+  __shared__ __attribute__((aligned(16))) __bf16 rings[KS * 4 * TILE];  // per stream: K slots 0, 1, then V slots 0, 1
   __shared__ int32_t tile_start;
+  static_assert(KS == 1 || KS * 4 * TILE * 2 >= (KS - 1) * WAVES * (D / 2 + 2) * 256, "room for the streams' results");
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int w = uniform(tid >> 6);
+  const int w = uniform(tid >> 6) % WAVES, ks = uniform(tid >> 6) / WAVES;  // 32-row slice, key stream
+  __bf16* const ring = rings + ks * 4 * TILE;
   auto Ks = [&](int slot) { return ring + slot * TILE; };
   auto Vs = [&](int slot) { return ring + (2 + slot) * TILE; };
   int t, h;
@@ -83,7 +85,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel
   const int32_t win_lo = max(start0, i0 - (a.window - 1));
   const int32_t sink_hi = start0 + min(a.sinks, win_lo - start0);
   const int32_t sink_steps = (sink_hi - start0 + KB - 1) / KB;
-  const int32_t total = sink_steps + (i1 - win_lo + KB) / KB;
+  const int32_t steps = sink_steps + (i1 - win_lo + KB) / KB;
+  const int32_t total = KS == 1 ? steps : (steps - ks + KS - 1) / KS;  // this stream's: ks, ks + KS, ...
   // this lane's keys: wlo .. gq, and start .. start + slen - 1 (its sinks before the window)
   const int32_t wlo = max(doc.start, gq - (a.window - 1));
   const int32_t slen = min(a.sinks, wlo - doc.start);
@@ -94,8 +97,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel
   TileStage<D, WAVES> st;
   st.init(w, lane, rstride * 2);
   KeySpan kspan{0, 0, 0}, vspan{0, 0, 0};
-  auto step_key = [&](int s) { return s < sink_steps ? start0 + KB * s : win_lo + KB * (s - sink_steps); };
-  auto step_max = [&](int s) { return s < sink_steps ? sink_hi - 1 : i1; };  // last key that exists for it
+  auto at = [&](int s) { return KS * s + ks; };  // of all steps
+  auto step_key = [&](int s) { return at(s) < sink_steps ? start0 + KB * at(s) : win_lo + KB * (at(s) - sink_steps); };
+  auto step_max = [&](int s) { return at(s) < sink_steps ? sink_hi - 1 : i1; };  // last key that exists for it
   auto stage_k = [&](int s, int slot) {
     stage_keys<D, WAVES>(st, a.geom, kspan, step_key(s), step_max(s), kbase, rstride, Ks(slot));
   };
@@ -128,8 +132,10 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel
 #pragma unroll
   for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
 
-  stage_k(0, 0);
-  stage_v(0, 0);
+  if (KS == 1 || total > 0) {
+    stage_k(0, 0);
+    stage_v(0, 0);
+  }
   if (total > 1) stage_k(1, 1);
   vm_wait_barrier<0>();
   f32x16 sc[KB / 32];
@@ -164,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel
 
     // A step that every query of the wave sees whole needs no per-key mask.  Keys of a sink step at or behind the first
     // window belong to the window steps.
-    const bool sink_step = s < sink_steps;
+    const bool sink_step = at(s) < sink_steps;
     const int32_t j0 = step_key(s);
     const uint32_t wlen = sink_step || !valid ? 0u : (uint32_t)(gq - wlo + 1);
     const uint32_t sl = !valid ? 0u : (uint32_t)(sink_step ? min(slen, max(sink_hi - doc.start, 0)) : slen);
@@ -223,7 +229,44 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) void window_fwd_kernel
     __builtin_amdgcn_s_setprio(0);
     vm_wait_barrier<0>();
   };
-  if constexpr (D == 64) {
+  if constexpr (KS > 1) {
+    // every stream takes part in the barriers of the longest one (the first)
+    const int most = (steps + KS - 1) / KS;
+    f32x16 sn[KB / 32];
+    for (int s = 0; s < most; s += 2) {
+      if (s < total) step(s, std::integral_constant<int, 0>{}, sc, sn);
+      else vm_wait_barrier<0>();
+      if (s + 1 < most) {
+        if (s + 1 < total) step(s + 1, std::integral_constant<int, 1>{}, sn, sc);
+        else vm_wait_barrier<0>();
+      }
+    }
+    // the streams' maxima, sums and O to LDS, register by register (no bank conflict), joined in stream order
+    float* const res = (float*)rings;
+    if (ks > 0) {
+      float* const mine = res + ((ks - 1) * WAVES + w) * (D / 2 + 2) * 64 + lane;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mine[(16 * mb + j) * 64] = o[mb][j];
+      mine[(D / 2) * 64] = m_run;
+      mine[(D / 2 + 1) * 64] = l_run;
+    }
+    hsap_lds_barrier();
+    if (ks > 0) return;
+    for (int x = 1; x < KS; ++x) {
+      const float* const other = res + ((x - 1) * WAVES + w) * (D / 2 + 2) * 64 + lane;
+      const float m2 = other[(D / 2) * 64], l2 = other[(D / 2 + 1) * 64];
+      const float m = fmaxf(m_run, m2), m_use = m == NEG_INF ? 0.f : m;
+      const float f1 = fast_exp2(m_run - m_use), f2 = fast_exp2(m2 - m_use);
+      l_run = l_run * f1 + l2 * f2;
+      m_run = m;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[mb][j] = o[mb][j] * f1 + other[(16 * mb + j) * 64] * f2;
+    }
+  } else if constexpr (D == 64) {
     // one score array: each 32-key half is replaced once its exponentials are formed
     for (int s = 0; s < total; s += 2) {
       step(s, std::integral_constant<int, 0>{}, sc, sc);
@@ -266,16 +309,23 @@ hsap_status check_window(const hsap_attn_desc* desc, int32_t window, int32_t sin
   return HSAP_OK;
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, int KS>
 static hsap_status launch_window_fwd(WindowFwdArgs& a, hipStream_t stream) {
   constexpr int BM = 32 * WAVES;
   a.tiles = (int32_t)((a.geom.m + BM - 1) / BM);
   const int64_t blocks = a.geom.n / a.geom.m * a.tiles * a.hq;
   if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
-  hipLaunchKernelGGL((window_fwd_kernel<D, WAVES>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, stream, a);
+  hipLaunchKernelGGL((window_fwd_kernel<D, WAVES, KS>), dim3((unsigned)blocks), dim3(64 * WAVES * KS), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "window_attn_fwd launch: %s", hipGetErrorString(e));
   return HSAP_OK;
+}
+
+template <int D>
+static hsap_status dispatch_window_fwd(WindowFwdArgs& a, hipStream_t stream) {
+  // (one block in four streams gains nothing over two in two)
+  if (window_row_blocks(window_q_tiles(a.geom, a.hq), D) < 4) return launch_window_fwd<D, 2, 2>(a, stream);
+  return launch_window_fwd<D, 4, 1>(a, stream);
 }
 
 }  // namespace hsap
@@ -307,5 +357,5 @@ extern "C" hsap_status hsap_window_attn_fwd(const hsap_attn_desc* desc, int32_t 
   a.sinks = (int32_t)std::min<int64_t>(sinks, a.geom.Ns);
   a.scale_log2 = desc->softmax_scale * kLog2e;
   hipStream_t s = (hipStream_t)hip_stream;
-  return desc->head_dim == 128 ? launch_window_fwd<128, 4>(a, s) : launch_window_fwd<64, 4>(a, s);
+  return desc->head_dim == 128 ? dispatch_window_fwd<128>(a, s) : dispatch_window_fwd<64>(a, s);
 }
