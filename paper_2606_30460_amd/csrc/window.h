@@ -9,8 +9,6 @@ namespace hsap {
 
 #if defined(__HIPCC__)
 
-// Queries of one chunk's sink pass (see window_bwd.hip).
-constexpr int32_t kSinkChunk = 256;
 // Most sink tokens per document that the backward takes: one workgroup holds them all (4 waves x 32 keys).
 constexpr int32_t kMaxBwdSinks = 128;
 

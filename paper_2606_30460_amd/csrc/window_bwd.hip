@@ -8,12 +8,12 @@
 // each time.  Four launches:
 //   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; delta first
 //   sinks    a document's sinks are seen by all its later queries, far more than a window's worth.  The shard's rows
-//            are cut into chunks of 256 queries; one workgroup per (chunk, K/V head) forms what the chunk's queries
+//            are cut into chunks (256 queries or more); one workgroup per (chunk, K/V head) forms what the chunk's queries
 //            give to the sinks of the document that reaches into it from before (outside their windows): fp32 partials
-//   sum      the chunks of one document are added up, in order, into the first one's partial
+//   sum      where a segment has many chunks: those of one document added up, in order, into the first one's partial
 //   dK, dV   one workgroup per (128 consecutive keys, K/V head), over the queries whose window holds one of them --
 //            and, for sinks, over the queries of their own chunk -- for every query head of the group; a sink's
-//            partial is added before the gradient is rounded
+//            partials are added before the gradient is rounded
 // The middle two run only where some query can be further than a window from a sink.
 #include <algorithm>
 #include <type_traits>
@@ -46,7 +46,9 @@ struct WindowBwdArgs {
   int32_t window;
   int32_t sinks;
   int32_t tiles;   // q-tiles (dQ) or key tiles (dK, dV) per segment
-  int32_t chunks;  // sink chunks per segment
+  int32_t chunk;   // queries of a sink chunk, a power of two
+  int32_t chunks;  // sink chunks per segment; 0: no sink pass
+  int32_t summed;  // a document's partials are summed up in its first chunk's
   int32_t dkv_f32;
   float scale;
   float scale_log2;
@@ -100,13 +102,13 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
   const int64_t n = a.geom.n;
   const int32_t m = (int32_t)a.geom.m;
   const int32_t p0 = uniform(segment_start(a.geom, a.shard, seg));
-  const int32_t cu_end = a.cu[a.num_docs];
   const int32_t i0 = p0 + qt * BM;
-  const int32_t i1 = min(min(i0 + BM - 1, p0 + m - 1), cu_end - 1);
+  const int32_t gq = min(i0 + 32 * w + l32, p0 + m - 1);
+  const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
+  const int32_t i1 = min(min(i0 + BM - 1, p0 + m - 1), a.cu[a.num_docs] - 1);
   if (i1 < i0) return;
-  const int32_t gq = min(i0 + 32 * w + l32, i1);
   const bool valid = i0 + 32 * w + l32 <= i1;
-  const int64_t qrow = (int64_t)seg * m + (gq - p0);
+  const int64_t qrow = (int64_t)seg * m + (min(gq, i1) - p0);
 
   bf16x8 qf[D / 16], df[D / 16];
   float delta = 0.f;
@@ -123,7 +125,6 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
   }
   delta = pair_sum(delta);
   const float lse2 = a.lse[(int64_t)h * n + qrow] * kLog2e;
-  const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
   if (tid == 0) tile_start = doc.start;
   __syncthreads();
   const int32_t start0 = uniform(tile_start);
@@ -298,7 +299,6 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   const int64_t n = a.geom.n;
   const int32_t m = (int32_t)a.geom.m;
   const int32_t per_seq = segments_per_sequence(a.geom);
-  const int32_t cu_end = a.cu[a.num_docs];
 
   // this lane's key: position, row, and its queries [qlo, qlo + len[x]) in the shard's segment x of the sequence
   int32_t key, qlo, first_seg;
@@ -310,9 +310,9 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   if constexpr (SINKS) {
     first_seg = tile / a.chunks;
     const int32_t a0 = uniform(segment_start(a.geom, a.shard, first_seg));
-    const int32_t c0 = a0 + (tile - first_seg * a.chunks) * kSinkChunk;
-    if (c0 >= cu_end) return;
+    const int32_t c0 = a0 + (tile - first_seg * a.chunks) * a.chunk;
     doc = doc_span(a.cu, a.num_docs, c0, lane);
+    if (c0 >= a.cu[a.num_docs]) return;
     t_doc = uniform(doc.start);
     const int32_t doc_end = uniform(doc.end);
     const int32_t count = min(a.sinks, c0 - t_doc);
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     key = t_doc + min(32 * w + l32, count - 1);
     krow = key + key_span(a.geom, key).delta;
     seg_lo[0] = c0;
-    seg_hi[0] = min(min(c0 + kSinkChunk, a0 + m), doc_end);
+    seg_hi[0] = min(min(c0 + a.chunk, a0 + m), doc_end);
     qlo = max(c0, (int32_t)min((int64_t)key + a.window, (int64_t)INT32_MAX));
     len[0] = key_ok ? max(seg_hi[0] - qlo, 0) : 0;
   } else {
@@ -331,12 +331,12 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     const int32_t chunk = run / runs, rseg = run - chunk * runs;
     const int32_t r0 = uniform(segment_start(a.geom, chunk, rseg));
     const int32_t j0 = r0 + at;
-    const int32_t jl = min(min(j0 + BN - 1, r0 + m - 1), cu_end - 1);
-    if (jl < j0) return;
-    key = min(j0 + 32 * w + l32, jl);
-    key_ok = j0 + 32 * w + l32 <= jl;
-    krow = (int64_t)chunk * n + (int64_t)rseg * m + (key - r0);
+    key = min(j0 + 32 * w + l32, r0 + m - 1);
     doc = doc_span(a.cu, a.num_docs, key, lane);
+    const int32_t jl = min(min(j0 + BN - 1, r0 + m - 1), a.cu[a.num_docs] - 1);
+    if (jl < j0) return;
+    key_ok = j0 + 32 * w + l32 <= jl;
+    krow = (int64_t)chunk * n + (int64_t)rseg * m + (min(key, jl) - r0);
     qlo = key;
     const int32_t b = rseg / per_seq;  // sequence of the batch
     first_seg = b * per_seq;
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
       const int32_t a0 = uniform(segment_start(a.geom, a.shard, first_seg + x)), b0 = a0 + m;
       int32_t end = near;
       if (key - doc.start < a.sinks && key >= a0 && key < b0)
-        end = max(end, min(doc.end, a0 + ((key - a0) / kSinkChunk + 1) * kSinkChunk));
+        end = max(end, a.chunks ? min(doc.end, a0 + ((key - a0) / a.chunk + 1) * a.chunk) : doc.end);
       len[x] = key_ok ? max(min(end, b0) - key, 0) : 0;
       seg_lo[x] = max(a0, j0);
       seg_hi[x] = b0;
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   if constexpr (!SINKS) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      int32_t e = key + len[x];
+      int32_t e = key_ok ? key + len[x] : 0;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o));
       if (lane == 0 && ks == 0) last_s[w][x] = e;
@@ -540,25 +540,26 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   } else {
     if (!key_ok) return;
     const int32_t s = key - doc.start;
-    if (s < a.sinks && a.partial) {
-      // the summed partials of the document's chunks in each of the shard's segments
+    if (s < a.sinks && a.chunks) {
+      // the partials of the document's chunks, or their sum, in each of the shard's segments
       for (int x = 0; x < per_seq; ++x) {
         const int32_t a0 = segment_start(a.geom, a.shard, first_seg + x);
-        const int32_t c = doc.start < a0 ? 0 : (doc.start - a0) / kSinkChunk + 1;  // first chunk that begins inside it
-        const int64_t c0 = (int64_t)a0 + (int64_t)c * kSinkChunk;
-        if (c0 >= min(doc.end, a0 + m)) continue;
-        const float* in = a.partial + ((((int64_t)(first_seg + x) * a.chunks + c) * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
+        const int32_t first = doc.start < a0 ? 0 : (doc.start - a0) / a.chunk + 1;  // first chunk that begins inside it
+        const int32_t end = (int32_t)((min((int64_t)doc.end, (int64_t)a0 + m) - a0 + a.chunk - 1) / a.chunk);
+        for (int32_t c = first; c < (a.summed ? min(end, first + 1) : end); ++c) {
+          const float* in = a.partial + ((((int64_t)(first_seg + x) * a.chunks + c) * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
 #pragma unroll
-        for (int mb = 0; mb < D / 32; ++mb)
+          for (int mb = 0; mb < D / 32; ++mb)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4 y = *(const f32x4*)(in + 32 * mb + 8 * q), z = *(const f32x4*)(in + D + 32 * mb + 8 * q);
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 y = *(const f32x4*)(in + 32 * mb + 8 * q), z = *(const f32x4*)(in + D + 32 * mb + 8 * q);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              dk[mb][4 * q + e] += y[e];
-              dv[mb][4 * q + e] += z[e];
+              for (int e = 0; e < 4; ++e) {
+                dk[mb][4 * q + e] += y[e];
+                dv[mb][4 * q + e] += z[e];
+              }
             }
-          }
+        }
       }
     }
     const int64_t at = (krow * a.hkv + g) * D + 4 * hi;
@@ -588,12 +589,12 @@ __global__ __launch_bounds__(256) void window_sink_sum_kernel(WindowBwdArgs a, i
   const int32_t tile = blockIdx.x / a.hkv;
   const int32_t seg = tile / a.chunks, c = tile - seg * a.chunks;
   const int32_t a0 = segment_start(a.geom, a.shard, seg);
-  const int64_t c0 = (int64_t)a0 + (int64_t)c * kSinkChunk;
+  const int64_t c0 = (int64_t)a0 + (int64_t)c * a.chunk;
   if (c0 >= a.cu[a.num_docs]) return;
   const DocSpan doc = doc_span(a.cu, a.num_docs, (int32_t)c0, lane);
-  if (doc.start >= c0 || (c > 0 && doc.start < c0 - kSinkChunk)) return;
+  if (doc.start >= c0 || (c > 0 && doc.start < c0 - a.chunk)) return;
   const int64_t end = min((int64_t)doc.end, a0 + a.geom.m);
-  const int32_t more = (int32_t)((end - 1 - c0) / kSinkChunk);  // chunks of the document behind this one
+  const int32_t more = (int32_t)((end - 1 - c0) / a.chunk);  // chunks of the document behind this one
   if (more == 0) return;
   const int64_t step = (int64_t)a.hkv * elems;
   float* p = a.partial + ((int64_t)tile * a.hkv + g) * elems;
@@ -618,15 +619,28 @@ static hsap_status check_launch_window(const char* what) {
   return HSAP_OK;
 }
 
-// Sink chunks per segment that the sink pass runs over; 0 where no query is further than a window from a sink.
-static int32_t sink_chunks(const Geom& g, int32_t window, int32_t sinks) {
-  return sinks > 0 && window < g.Ns ? (int32_t)((g.m + kSinkChunk - 1) / kSinkChunk) : 0;
+// Queries of a sink chunk: a workgroup per CU over all chunks and K/V heads, at least 256 (8192 rows x 8 heads: chunks of 256
+// 33 us, of 1024 177 us; 16384 rows x 16 heads: 256 58 us, 1024 26 us).
+static int32_t sink_chunk(const hsap_attn_desc* d, const Geom& g) {
+  int32_t c = 256;
+  while (c < 4096 && g.n * d->heads_kv > c * kComputeUnits) c *= 2;
+  return c;
 }
+
+// Sink chunks per segment; 0 where no chunk begins inside a document that has a sink further than a window from its queries.
+static int32_t sink_chunks(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
+  if (sinks == 0 || window >= g.Ns) return 0;
+  const int32_t c = sink_chunk(d, g), per = (int32_t)((g.m + c - 1) / c);
+  return per == 1 && g.P == 1 && g.layout == HSAP_LAYOUT_CONTIGUOUS ? 0 : per;
+}
+
+// Up to so many chunks per segment the dK/dV kernel adds a document's partials itself.
+constexpr int32_t kDirectChunks = 8;
 
 static int64_t delta_bytes(const hsap_attn_desc* d, const Geom& g) { return (4 * g.n * d->heads_q + 255) / 256 * 256; }
 
 static int64_t bwd_workspace(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
-  return delta_bytes(d, g) + g.n / g.m * sink_chunks(g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
+  return delta_bytes(d, g) + g.n / g.m * sink_chunks(d, g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
 }
 
 template <int D, int WAVES, int KS>
@@ -656,14 +670,12 @@ static hsap_status launch_window_bwd(WindowBwdArgs& a, hipStream_t s) {
     // as many key blocks as there are sinks; the other waves are streams over the queries
     st = a.sinks <= 32 ? launch_dkv<D, true, 1, 4>(a, s) : a.sinks <= 64 ? launch_dkv<D, true, 2, 2>(a, s) : launch_dkv<D, true, 4, 1>(a, s);
     if (st != HSAP_OK) return st;
-    if (a.chunks > 1) {
+    if (a.summed) {
       const int64_t blocks = a.geom.n / a.geom.m * a.chunks * a.hkv;
       hipLaunchKernelGGL(window_sink_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, a.sinks * 2 * D);
       st = check_launch_window("window_attn_bwd sink sum");
       if (st != HSAP_OK) return st;
     }
-  } else {
-    a.partial = nullptr;
   }
   switch (window_row_blocks(window_key_tiles(a.geom, a.hkv, a.window), D)) {
     case 1: return launch_dkv<D, false, 1, 4>(a, s);
@@ -695,7 +707,9 @@ extern "C" hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t 
   if (st != HSAP_OK) return st;
   a.window = (int32_t)std::min<int64_t>(window, a.geom.Ns);
   a.sinks = (int32_t)std::min<int64_t>(sinks, a.geom.Ns);
-  a.chunks = sink_chunks(a.geom, a.window, a.sinks);
+  a.chunks = sink_chunks(desc, a.geom, a.window, a.sinks);
+  a.chunk = sink_chunk(desc, a.geom);
+  a.summed = a.chunks > kDirectChunks;
   if (a.chunks && a.sinks > kMaxBwdSinks)
     HSAP_FAIL(HSAP_ERR_UNSUPPORTED, "sinks %d above %d in the backward", sinks, kMaxBwdSinks);
   if (!q || !k || !v || !d_o || !o || !lse || !dq || !dk || !dv || !workspace)

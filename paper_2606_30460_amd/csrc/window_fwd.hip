@@ -62,14 +62,14 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : D == 64 && KS =
   const int64_t n = a.geom.n;
   const int32_t m = (int32_t)a.geom.m;
   const int32_t p0 = uniform(segment_start(a.geom, a.shard, seg));  // the segment's first position
-  const int32_t cu_end = a.cu[a.num_docs];
-  // positions of the tile's rows that are queries: i0 .. i1; rows behind the last document are left alone
   const int32_t i0 = p0 + qt * BM;
-  const int32_t i1 = min(min(i0 + BM - 1, p0 + m - 1), cu_end - 1);
+  const int32_t gq = min(i0 + 32 * w + l32, p0 + m - 1);
+  const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
+  // positions of the tile's rows that are queries: i0 .. i1; rows behind the last document are left alone
+  const int32_t i1 = min(min(i0 + BM - 1, p0 + m - 1), a.cu[a.num_docs] - 1);
   if (i1 < i0) return;
-  const int32_t gq = min(i0 + 32 * w + l32, i1);
   const bool valid = i0 + 32 * w + l32 <= i1;
-  const int64_t qrow = (int64_t)seg * m + (gq - p0);
+  const int64_t qrow = (int64_t)seg * m + (min(gq, i1) - p0);
 
   bf16x8 qf[D / 16];
   {
@@ -77,7 +77,6 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : D == 64 && KS =
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
   }
-  const DocSpan doc = doc_span(a.cu, a.num_docs, gq, lane);
   if (tid == 0) tile_start = doc.start;
   __syncthreads();
   const int32_t start0 = uniform(tile_start);
