@@ -140,6 +140,31 @@ struct TileStage {
   }
 };
 
+// Operand addresses in a swizzled [rows][D] tile (mfma.h).  Row reads (row l32 of a 32-row block, chunk 2 kk + hi) and
+// transpose reads (rows 8 k + tr_row of a 16-row block, columns 32 mb + tr_col) of one lane differ by an exclusive or
+// in the chunk's bits alone, so a base each gives them all.  fresh() keeps the compiler from holding the sixteen
+// addresses in registers through a loop that has none to spare.
+template <int D>
+struct TileReads {
+  int row, tr0, tr1;  // elements
+
+  __device__ __forceinline__ void init(int lane) {
+    constexpr int CPR = D / 8;
+    const int l32 = lane & 31, hi = lane >> 5;
+    const int tr_row = 4 * hi + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    row = swz<CPR>(l32, 8 * hi);
+    tr0 = swz<CPR>(tr_row, tr_col);
+    tr1 = swz<CPR>(8 + tr_row, tr_col);
+  }
+  __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(tr0), "+v"(tr1)); }
+  // row l32 of the block at `tile`, sixteen columns kk
+  __device__ __forceinline__ bf16x8 rows(const __bf16* tile, int kk) const { return *(const bf16x8*)(tile + (row ^ (16 * kk))); }
+  // columns 32 mb .. +31 of the sixteen rows at `tile`, transposed
+  __device__ __forceinline__ bf16x8 turned(const __bf16* tile, int mb) const {
+    return cat4(ds_read_tr16(tile + (tr0 ^ (32 * mb))), ds_read_tr16(tile + (tr1 ^ (32 * mb))));
+  }
+};
+
 // Uniform copy of a value that is the same on every lane.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 

@@ -76,13 +76,18 @@ __device__ __forceinline__ void join_streams(f32x16 (&sum)[N], float* res, int w
   }
 }
 
+// The compiler, short of registers, reads an operand from LDS right before its product and waits for it.  The loops below
+// read a few products ahead instead and keep the order of reads and products (vector instructions may still move).
+constexpr int kAhead = 3;
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x406); }
+
 // ---------------------------------------------------------------------------
 // dQ: the forward's ranges, three products per 64-key step (S, dP and dS K).  dP - delta is formed by the matrix
 // product itself, whose accumulator starts at -delta.
 // ---------------------------------------------------------------------------
 template <int D, int WAVES, int KS>
 __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_dq_kernel(WindowBwdArgs a) {
-  constexpr int KB = 64, CPR = D / 8, TILE = KB * D, BM = 32 * WAVES;
+  constexpr int KB = 64, TILE = KB * D, BM = 32 * WAVES;
   constexpr float NEG_INF = -__builtin_inff();
   __shared__ __attribute__((aligned(16))) __bf16 rings[KS * 4 * TILE];  // per stream: K slots 0, 1, then V slots 0, 1
   __shared__ int32_t tile_start;
@@ -180,15 +185,8 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
     stage_keys<D, WAVES>(st, a.geom, span, j0, jmax, kbase, rstride, Ks(slot));
     stage_keys<D, WAVES>(st, a.geom, span, j0, jmax, vbase, rstride, Vs(slot));
   };
-  const int tr_row = 4 * hi + ((lane & 15) >> 2);
-  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  int rowoff[D / 16], troff[D / 32][2];
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) rowoff[kk] = swz<CPR>(l32, 16 * kk + 8 * hi);
-#pragma unroll
-  for (int mb = 0; mb < D / 32; ++mb)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) troff[mb][k] = swz<CPR>(8 * k + tr_row, 32 * mb + tr_col) - 8 * k * D;
+  TileReads<D> rd;
+  rd.init(lane);
 
   f32x16 dq[D / 32];
 #pragma unroll
@@ -198,6 +196,10 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
   for (int j = 0; j < 16; ++j) minus_delta[j] = -delta;
 
   if (KS == 1 || total > 0) stage(0, 0);
+  // (the compiler sees no wait inside asm: without this use it would wait for these rows at their first use in the
+  // loop, every time, and so for the transfers under way)
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) asm volatile("" ::"v"(qf[kk]), "v"(df[kk]));
   vm_wait_barrier<0>();
   auto step = [&](int i, auto par) __attribute__((always_inline)) {
     constexpr int S0 = decltype(par)::value, S1 = S0 ^ 1;
@@ -213,11 +215,22 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
     const __bf16 *K = Ks(S0), *V = Vs(S0);
 #pragma unroll
     for (int nb = 0; nb < KB / 32; ++nb) {
+      rd.fresh();
+      const __bf16 *Kb = K + 32 * nb * D, *Vb = V + 32 * nb * D;
       f32x16 sc = f32x16{}, dp = minus_delta;
+      bf16x8 fa[kAhead];
+      auto read = [&](int i) __attribute__((always_inline)) {
+        if (i < D / 8) fa[i % kAhead] = i < D / 16 ? rd.rows(Kb, i) : rd.rows(Vb, i - D / 16);
+      };
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(K + 32 * nb * D + rowoff[kk]), qf[kk], sc);
+      for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) dp = mfma32(*(const bf16x8*)(V + 32 * nb * D + rowoff[kk]), df[kk], dp);
+      for (int i = 0; i < D / 8; ++i) {
+        if (i < D / 16) sc = mfma32(fa[i % kAhead], qf[i], sc);
+        else dp = mfma32(fa[i % kAhead], df[i - D / 16], dp);
+        read(i + kAhead);
+        keep_order();
+      }
       if (masked) {
         const int32_t rw0 = rw + 4 * hi, rs0 = rs + 4 * hi;
 #pragma unroll
@@ -226,16 +239,20 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
           if ((uint32_t)(rw0 + c) >= wlen && (uint32_t)(rs0 + c) >= sl) sc[j] = NEG_INF;
         }
       }
-      bf16x8 ds[2];
+      bf16x8 ft[kAhead], ds[2];
+      auto read_turned = [&](int i) __attribute__((always_inline)) {
+        if (i < D / 16) ft[i % kAhead] = rd.turned(Kb + 16 * (i / (D / 32)) * D, i % (D / 32));
+      };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) read_turned(i);
+      keep_order();
 #pragma unroll
       for (int j = 0; j < 16; ++j) ds[j >> 3][j & 7] = (__bf16)(fast_exp2(__builtin_fmaf(sc[j], a.scale_log2, -lse2)) * dp[j]);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int rb = (32 * nb + 16 * half) * D;
-#pragma unroll
-        for (int mb = 0; mb < D / 32; ++mb)
-          dq[mb] = mfma32(cat4(ds_read_tr16(K + rb + troff[mb][0]), ds_read_tr16(K + rb + 8 * D + troff[mb][1])), ds[half],
-                          dq[mb]);
+      for (int i = 0; i < D / 16; ++i) {
+        dq[i % (D / 32)] = mfma32(ft[i % kAhead], ds[i / (D / 32)], dq[i % (D / 32)]);
+        read_turned(i + kAhead);
+        keep_order();
       }
     }
     vm_wait_barrier<0>();
@@ -286,6 +303,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   __shared__ __attribute__((aligned(16))) __bf16 rings[KS * 4 * TILE];  // per stream: Q slots 0, 1, then dO slots 0, 1
   __shared__ __attribute__((aligned(16))) float rows_all[KS][2][2][QB];   // [slot][LSE in log2 units, -delta]
   __shared__ int32_t last_s[WAVES][2];
+  __shared__ int32_t key_s[SINKS ? 1 : WAVES][4][32];  // what the end needs of the keys: row (-1: none), position, document
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
@@ -362,6 +380,12 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
       for (int o = 16; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o));
       if (lane == 0 && ks == 0) last_s[w][x] = e;
     }
+    if (hi == 0 && ks == 0) {  // (kept here: the loop has no registers to spare)
+      key_s[w][0][l32] = key_ok ? (int32_t)krow : -1;
+      key_s[w][1][l32] = key;
+      key_s[w][2][l32] = doc.start;
+      key_s[w][3][l32] = doc.end;
+    }
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -431,21 +455,20 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     auto store_rows = [&](int slot) {
       if (sid < 2 * QB) rows_s[slot][sid / QB][sid % QB] = sid < QB ? row_next * kLog2e : -row_next;
     };
-    const int tr_row = 4 * hi + ((lane & 15) >> 2);
-    const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    int rowoff[D / 16], troff[D / 32][2];
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) rowoff[kk] = swz<CPR>(l32, 16 * kk + 8 * hi);
-#pragma unroll
-    for (int mb = 0; mb < D / 32; ++mb)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) troff[mb][k] = swz<CPR>(8 * k + tr_row, 32 * mb + tr_col) - 8 * k * D;
+    TileReads<D> rd;
+    rd.init(lane);
 
     Step cur{cnt0 > 0 ? 0 : 1, 0, 0};
     if (KS == 1 || total > 0) {
       advance(cur, ks);
       stage(cur, 0);
       store_rows(0);
+    }
+    // (as in the dQ kernel: no wait for these rows inside the loop)
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      asm volatile("" ::"v"(kf[kk]));
+      if constexpr (!VLDS) asm volatile("" ::"v"(vf[kk]));
     }
     vm_wait_barrier<0>();
     Step nxt = cur;
@@ -462,17 +485,26 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
         const bool some = r < (int32_t)ln && r + 31 >= 0;
         const bool all = !key_ok || (r >= 0 && r + 32 <= (int32_t)ln);
         if (__builtin_amdgcn_ballot_w64(some) == 0) continue;
+        rd.fresh();
+        // S and dP: 2 D / 16 products, each operand read kAhead products before its use
+        const __bf16 *Qb = Q + 32 * nb * D, *Ob = O + 32 * nb * D;
         f32x16 sc = f32x16{}, dp;
 #pragma unroll
         for (int j = 0; j < 16; ++j) dp[j] = rows_s[S0][1][32 * nb + c_row(j, hi)];
+        bf16x8 fa[kAhead], fv[kAhead];
+        auto read = [&](int i) __attribute__((always_inline)) {
+          if (i >= D / 8) return;
+          fa[i % kAhead] = i < D / 16 ? rd.rows(Qb, i) : rd.rows(Ob, i - D / 16);
+          if (VLDS && i >= D / 16) fv[i % kAhead] = rd.rows(vtile + 32 * w * D, i - D / 16);
+        };
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(*(const bf16x8*)(Q + 32 * nb * D + rowoff[kk]), kf[kk], sc);
+        for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          bf16x8 vx;
-          if constexpr (VLDS) vx = *(const bf16x8*)(vtile + 32 * w * D + rowoff[kk]);
-          else vx = vf[kk];
-          dp = mfma32(*(const bf16x8*)(O + 32 * nb * D + rowoff[kk]), vx, dp);
+        for (int i = 0; i < D / 8; ++i) {
+          if (i < D / 16) sc = mfma32(fa[i % kAhead], kf[i], sc);
+          else dp = mfma32(fa[i % kAhead], VLDS ? fv[i % kAhead] : vf[VLDS ? 0 : i - D / 16], dp);
+          read(i + kAhead);
+          keep_order();
         }
         if (__builtin_amdgcn_ballot_w64(!all) != 0) {
           const int32_t r4 = r + 4 * hi;
@@ -480,23 +512,30 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
           for (int j = 0; j < 16; ++j)
             if ((uint32_t)(r4 + c_row(j, 0)) >= ln) sc[j] = NEG_INF;
         }
-        bf16x8 pb[2], ds[2];
+        // the sums' operands: per sixteen queries and 32 columns dO^T (for dV), then Q^T (for dK)
+        bf16x8 ft[kAhead], pb[2], ds[2];
+        auto read_turned = [&](int i) __attribute__((always_inline)) {
+          if (i < D / 8) ft[i % kAhead] = rd.turned((i & 1 ? Qb : Ob) + 16 * (i / (D / 16)) * D, i / 2 % (D / 32));
+        };
+        float lse2[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) lse2[j] = rows_s[S0][0][32 * nb + c_row(j, hi)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_turned(i);
+        keep_order();
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float p = fast_exp2(__builtin_fmaf(sc[j], a.scale_log2, -rows_s[S0][0][32 * nb + c_row(j, hi)]));
+          const float p = fast_exp2(__builtin_fmaf(sc[j], a.scale_log2, -lse2[j]));
           pb[j >> 3][j & 7] = (__bf16)p;
           ds[j >> 3][j & 7] = (__bf16)(p * dp[j]);
         }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int rb = (32 * nb + 16 * half) * D;
-#pragma unroll
-          for (int mb = 0; mb < D / 32; ++mb) {
-            dv[mb] = mfma32(cat4(ds_read_tr16(O + rb + troff[mb][0]), ds_read_tr16(O + rb + 8 * D + troff[mb][1])), pb[half],
-                            dv[mb]);
-            dk[mb] = mfma32(cat4(ds_read_tr16(Q + rb + troff[mb][0]), ds_read_tr16(Q + rb + 8 * D + troff[mb][1])), ds[half],
-                            dk[mb]);
-          }
+        for (int i = 0; i < D / 8; ++i) {
+          const int half = i / (D / 16), mb = i / 2 % (D / 32);
+          if (i & 1) dk[mb] = mfma32(ft[i % kAhead], ds[half], dk[mb]);
+          else dv[mb] = mfma32(ft[i % kAhead], pb[half], dv[mb]);
+          read_turned(i + kAhead);
+          keep_order();
         }
       }
       if (i + 1 < total) store_rows(S1);
@@ -538,14 +577,15 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
         *(f32x4*)(out + D + 32 * mb + 8 * q) = y;
       }
   } else {
-    if (!key_ok) return;
-    const int32_t s = key - doc.start;
+    const int32_t row = key_s[w][0][l32], start = key_s[w][2][l32], doc_end = key_s[w][3][l32];
+    if (row < 0) return;
+    const int32_t s = key_s[w][1][l32] - start;
     if (s < a.sinks && a.chunks) {
       // the partials of the document's chunks, or their sum, in each of the shard's segments
       for (int x = 0; x < per_seq; ++x) {
         const int32_t a0 = segment_start(a.geom, a.shard, first_seg + x);
-        const int32_t first = doc.start < a0 ? 0 : (doc.start - a0) / a.chunk + 1;  // first chunk that begins inside it
-        const int32_t end = (int32_t)((min((int64_t)doc.end, (int64_t)a0 + m) - a0 + a.chunk - 1) / a.chunk);
+        const int32_t first = start < a0 ? 0 : (start - a0) / a.chunk + 1;  // first chunk that begins inside it
+        const int32_t end = (int32_t)((min((int64_t)doc_end, (int64_t)a0 + m) - a0 + a.chunk - 1) / a.chunk);
         for (int32_t c = first; c < (a.summed ? min(end, first + 1) : end); ++c) {
           const float* in = a.partial + ((((int64_t)(first_seg + x) * a.chunks + c) * a.hkv + g) * a.sinks + s) * (2 * D) + 4 * hi;
 #pragma unroll
@@ -562,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
         }
       }
     }
-    const int64_t at = (krow * a.hkv + g) * D + 4 * hi;
+    const int64_t at = ((int64_t)row * a.hkv + g) * D + 4 * hi;
 #pragma unroll
     for (int mb = 0; mb < D / 32; ++mb)
 #pragma unroll
