@@ -215,7 +215,6 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
     const __bf16 *K = Ks(S0), *V = Vs(S0);
 #pragma unroll
     for (int nb = 0; nb < KB / 32; ++nb) {
-      rd.fresh();
       const __bf16 *Kb = K + 32 * nb * D, *Vb = V + 32 * nb * D;
       f32x16 sc = f32x16{}, dp = minus_delta;
       bf16x8 fa[kAhead];
