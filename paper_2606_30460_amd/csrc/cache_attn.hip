@@ -116,7 +116,7 @@ __device__ __forceinline__ T read_codes(const uint8_t* p) {
 // loads are marked as streaming (64 sequences of 8k tokens, 8 heads of 128: 128 -> 119 us; with several row tiles per
 // sequence 46 -> 49 us, with 67 MB of codes, which the next call finds there again, 21.8 -> 22.5 us).
 template <int D, int MT, bool ONCE>
-__global__ __launch_bounds__(256, MT == 4 && D == 128 ? 1 : 2) void cache_attn_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   constexpr int KX = D / 64, CB = D / 16, ROWS = 16 * MT;  // 16-byte loads per K row and lane; d values per lane of V
   constexpr float NEG_INF = -__builtin_inff();
   constexpr float RESCALE_SLACK = 8.f;
@@ -515,7 +515,8 @@ __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
     a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
 }
 
-// How a call is cut: row tiles of 16 mt rows, and splits of a tile's tokens so that the grid fills the chip, each of
+// How a call is cut: row tiles of 16 mt rows (two blocks where the sequences have more than 16 rows: 28 x 50 rows x 8 of 64
+// heads of 128 28 us, one block 34, four 48; 2048 rows over 30000 tokens, head_dim 64, 769, 1305 and 1012), and splits of a tile's tokens so that the grid fills the chip, each of
 // at least 256 tokens, at most 128 (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits 24.5, 128 19.4,
 // 256 22.0: more partials to join).
 struct CacheCut {
@@ -524,20 +525,19 @@ struct CacheCut {
   int32_t splits;
 };
 
-// Workgroups to aim at: what the chip holds at once, and twice that where a workgroup is short of work for the time that its
-// loads take (one 16-row block: 64 sequences of 8k tokens 129 us with 512, 128 with 1024, 127 with 2048; four blocks:
-// 3 x 700 rows 44 us with 512, 46 with 1024, 68 with 2048, where the fp32 partials weigh more).
-constexpr int64_t kCacheGrid = 512;
+// Workgroups to aim at: twice what the chip holds at once (64 sequences of 8k tokens: 129 us with 512, 128 with 1024, 127
+// with 2048; 3 x 700 rows: 49, 43 and 47 us, where the fp32 partials begin to weigh).
+constexpr int64_t kCacheGrid = 1024;
 
 static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
   const int64_t group = heads_q / d.heads_kv;
   const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
-  c.mt = rows > 32 ? 4 : rows > 16 ? 2 : 1;
+  c.mt = rows > 16 ? 2 : 1;
   c.tiles = one_each ? (int64_t)d.num_seqs * ((group + 16 * c.mt - 1) / (16 * c.mt))
                      : item_base(total_q, group, 16 * c.mt, 1, d.num_seqs);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
-  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, (c.mt == 1 ? 2 : 1) * kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
   return c;
 }
 
@@ -549,8 +549,7 @@ template <int D>
 static void launch_cache_attn(const CacheAttnArgs& a, int mt, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
   const int64_t bytes = 2 * (int64_t)a.d.num_seqs * a.d.table_width * a.d.page_size * a.d.heads_kv * D;
-  if (mt == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 4, false>), grid, block, 0, s, a);
-  else if (mt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
+  if (mt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
   else if (!a.cu && bytes > (int64_t(256) << 20)) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false>), grid, block, 0, s, a);
 }
