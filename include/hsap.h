@@ -742,7 +742,7 @@ int64_t hsap_window_attn_bwd_workspace(const hsap_attn_desc* desc, int32_t windo
  *               0 for a key that none of them sees.  Every row of the documents is written (not accumulated).
  *   workspace   device, 16-byte aligned, at least hsap_window_attn_bwd_workspace bytes (workspace_bytes: its size);
  *               contents on entry ignored.  Calls that overlap in time need workspaces of their own.
- * sinks <= 128 wherever window < N, else HSAP_ERR_UNSUPPORTED.  Two to four launches on `stream`; no atomics: the same
+ * sinks <= 128 wherever window < N, else HSAP_ERR_UNSUPPORTED.  Two to five launches on `stream`; no atomics: the same
  * inputs give the same bits.
  */
 hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const void* q,

@@ -5,7 +5,7 @@
 //   dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i   (dK, dV over the query heads of the K/V head)
 //
 // Every gradient row has one owner, which forms it whole in registers and stores it once: no atomics, the same bits
-// each time.  Four launches:
+// each time.  Up to five launches:
 //   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; delta first
 //   sinks    a document's sinks are seen by all its later queries, far more than a window's worth.  The shard's rows
 //            are cut into chunks (256 queries or more); one workgroup per (chunk, K/V head) forms what the chunk's queries
@@ -14,7 +14,9 @@
 //   dK, dV   one workgroup per (128 consecutive keys, K/V head), over the queries whose window holds one of them --
 //            and, for sinks, over the queries of their own chunk -- for every query head of the group; a sink's
 //            partials are added before the gradient is rounded
-// The middle two run only where some query can be further than a window from a sink.
+//   heads    where that grid is small and a group large, the group's heads are dealt to several workgroups, whose fp32
+//            gradients this one adds up in order
+// Sinks and sum run only where some query can be further than a window from a sink.
 #include <algorithm>
 #include <type_traits>
 
@@ -50,6 +52,8 @@ struct WindowBwdArgs {
   int32_t chunks;  // sink chunks per segment; 0: no sink pass
   int32_t summed;  // a document's partials are summed up in its first chunk's
   int32_t dkv_f32;
+  int32_t head_split;  // workgroups per key tile and K/V head, each with some of the group's heads
+  float* heads_part;   // [head_split, P * n, Hkv, 2, D], head_split > 1: dK (unscaled) and dV of each
   float scale;
   float scale_log2;
 };
@@ -312,7 +316,10 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   auto& rows_s = rows_all[ks];
   const int grp = a.hq / a.hkv;
   const int g = blockIdx.x % a.hkv;
-  const int32_t tile = blockIdx.x / a.hkv;
+  const int32_t rest = blockIdx.x / a.hkv;
+  const int hs = SINKS ? 0 : rest % a.head_split;
+  const int32_t tile = SINKS ? rest : rest / a.head_split;
+  const int h0 = SINKS ? 0 : hs * grp / a.head_split, h1 = SINKS ? grp : (hs + 1) * grp / a.head_split;  // heads of the group
   const int64_t n = a.geom.n;
   const int32_t m = (int32_t)a.geom.m;
   const int32_t per_seq = segments_per_sequence(a.geom);
@@ -397,7 +404,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
   }
   const int32_t cnt0 = max(0, (seg_hi[0] - seg_lo[0] + QB - 1) / QB);
   const int32_t cnt1 = SINKS ? 0 : max(0, (seg_hi[1] - seg_lo[1] + QB - 1) / QB);
-  const int32_t steps = (cnt0 + cnt1) * grp;
+  const int32_t steps = (cnt0 + cnt1) * (h1 - h0);
   const int32_t total = KS == 1 ? steps : (steps - ks + KS - 1) / KS;  // this stream's: ks, ks + KS, ...
 
   f32x16 dk[D / 32], dv[D / 32];
@@ -427,8 +434,8 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
       for (int y = 0; y < by; ++y) {
         if (++p.s < (p.x ? cnt1 : cnt0)) continue;
         p.s = 0;
-        if (++p.hh < grp) continue;
-        p.hh = 0;
+        if (++p.hh < h1) continue;
+        p.hh = h0;
         ++p.x;
       }
     };
@@ -457,7 +464,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     TileReads<D> rd;
     rd.init(lane);
 
-    Step cur{cnt0 > 0 ? 0 : 1, 0, 0};
+    Step cur{cnt0 > 0 ? 0 : 1, h0, 0};
     if (KS == 1 || total > 0) {
       advance(cur, ks);
       stage(cur, 0);
@@ -579,7 +586,7 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     const int32_t row = key_s[w][0][l32], start = key_s[w][2][l32], doc_end = key_s[w][3][l32];
     if (row < 0) return;
     const int32_t s = key_s[w][1][l32] - start;
-    if (s < a.sinks && a.chunks) {
+    if (s < a.sinks && a.chunks && hs == 0) {
       // the partials of the document's chunks, or their sum, in each of the shard's segments
       for (int x = 0; x < per_seq; ++x) {
         const int32_t a0 = segment_start(a.geom, a.shard, first_seg + x);
@@ -600,6 +607,17 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
             }
         }
       }
+    }
+    if (a.head_split > 1) {
+      float* out = a.heads_part + (((int64_t)hs * a.geom.P * n + row) * a.hkv + g) * (2 * D) + 4 * hi;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          *(f32x4*)(out + 32 * mb + 8 * q) = f32x4{dk[mb][4 * q], dk[mb][4 * q + 1], dk[mb][4 * q + 2], dk[mb][4 * q + 3]};
+          *(f32x4*)(out + D + 32 * mb + 8 * q) = f32x4{dv[mb][4 * q], dv[mb][4 * q + 1], dv[mb][4 * q + 2], dv[mb][4 * q + 3]};
+        }
+      return;
     }
     const int64_t at = ((int64_t)row * a.hkv + g) * D + 4 * hi;
 #pragma unroll
@@ -652,6 +670,33 @@ __global__ __launch_bounds__(256) void window_sink_sum_kernel(WindowBwdArgs a, i
   }
 }
 
+// dK and dV as the sum of the head splits' fp32 parts, in order: a thread per four values of each.
+__global__ __launch_bounds__(256) void window_heads_sum_kernel(WindowBwdArgs a, int d) {
+  const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t rows = (int64_t)a.geom.P * a.geom.n, per_row = (int64_t)a.hkv * (d / 4);
+  const int64_t row = item / per_row;
+  if (row >= rows) return;
+  const int32_t at = (int32_t)(item - row * per_row), g = at / (d / 4), e = 4 * (at - g * (d / 4));
+  const int32_t chunk = (int32_t)(row / a.geom.n);
+  if (global_pos(a.geom, chunk, row - (int64_t)chunk * a.geom.n) >= a.cu[a.num_docs]) return;  // padding
+  const float* p = a.heads_part + (row * a.hkv + g) * (2 * d) + e;
+  const int64_t step = rows * a.hkv * (2 * d);
+  f32x4 dk = *(const f32x4*)p, dv = *(const f32x4*)(p + d);
+  for (int x = 1; x < a.head_split; ++x) {
+    dk += *(const f32x4*)(p + x * step);
+    dv += *(const f32x4*)(p + x * step + d);
+  }
+  dk *= a.scale;
+  const int64_t out = (row * a.hkv + g) * d + e;
+  if (a.dkv_f32) {
+    *(f32x4*)((float*)a.dk + out) = dk;
+    *(f32x4*)((float*)a.dv + out) = dv;
+  } else {
+    *(bf16x4*)((__bf16*)a.dk + out) = bf16x4{(__bf16)dk[0], (__bf16)dk[1], (__bf16)dk[2], (__bf16)dk[3]};
+    *(bf16x4*)((__bf16*)a.dv + out) = bf16x4{(__bf16)dv[0], (__bf16)dv[1], (__bf16)dv[2], (__bf16)dv[3]};
+  }
+}
+
 static hsap_status check_launch_window(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
@@ -678,8 +723,30 @@ constexpr int32_t kDirectChunks = 8;
 
 static int64_t delta_bytes(const hsap_attn_desc* d, const Geom& g) { return (4 * g.n * d->heads_q + 255) / 256 * 256; }
 
+// Workgroups that share a key tile's heads: while all stay resident at once and each keeps at least eight steps, its parts
+// within 64 MiB.
+static int32_t head_split(const hsap_attn_desc* d, const Geom& g, int32_t window) {
+  const int grp = d->heads_q / d->heads_kv;
+  const int64_t tiles = window_key_tiles(g, d->heads_kv, window);
+  const int blocks = window_row_blocks(tiles, d->head_dim);
+  if (blocks == 4 || grp == 1) return 1;
+  const int64_t resident = kComputeUnits * (d->head_dim == 64 ? 2 : 1);
+  const int64_t per_head = (std::min<int64_t>(window, g.m) + 32 * blocks) / 32;  // 32-query steps of one head
+  const int64_t steps = per_head * grp * blocks / 4;                             // a stream's
+  const int64_t bytes = (int64_t)g.P * g.n * d->heads_kv * 2 * d->head_dim * 4;
+  const int64_t most = std::min<int64_t>(std::min<int64_t>(grp, steps / 8),
+                                         std::min(resident / std::max<int64_t>(1, tiles * 4 / blocks), (int64_t(64) << 20) / bytes));
+  return (int32_t)std::max<int64_t>(1, most);
+}
+
+static int64_t heads_bytes(const hsap_attn_desc* d, const Geom& g, int32_t window) {
+  const int64_t split = head_split(d, g, window);
+  return split > 1 ? split * g.P * g.n * d->heads_kv * 2 * d->head_dim * 4 : 0;
+}
+
 static int64_t bwd_workspace(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
-  return delta_bytes(d, g) + g.n / g.m * sink_chunks(d, g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
+  return delta_bytes(d, g) + heads_bytes(d, g, window) +
+         g.n / g.m * sink_chunks(d, g, window, sinks) * d->heads_kv * sinks * 2 * d->head_dim * 4;
 }
 
 template <int D, int WAVES, int KS>
@@ -695,7 +762,7 @@ template <int D, bool SINKS, int WAVES, int KS>
 static hsap_status launch_dkv(WindowBwdArgs& a, hipStream_t s) {
   const int64_t segs = a.geom.n / a.geom.m;
   a.tiles = (int32_t)((a.geom.m + 32 * WAVES - 1) / (32 * WAVES));
-  const int64_t blocks = (SINKS ? segs * a.chunks : segs * a.geom.P * a.tiles) * a.hkv;
+  const int64_t blocks = (SINKS ? segs * a.chunks : segs * a.geom.P * a.tiles * a.head_split) * a.hkv;
   if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipLaunchKernelGGL((window_dkv_kernel<D, SINKS, WAVES, KS>), dim3((unsigned)blocks), dim3(64 * WAVES * KS), 0, s, a);
   return check_launch_window(SINKS ? "window_attn_bwd sinks" : "window_attn_bwd dK/dV");
@@ -717,10 +784,14 @@ static hsap_status launch_window_bwd(WindowBwdArgs& a, hipStream_t s) {
     }
   }
   switch (window_row_blocks(window_key_tiles(a.geom, a.hkv, a.window), D)) {
-    case 1: return launch_dkv<D, false, 1, 4>(a, s);
-    case 2: return launch_dkv<D, false, 2, 2>(a, s);
+    case 1: st = launch_dkv<D, false, 1, 4>(a, s); break;
+    case 2: st = launch_dkv<D, false, 2, 2>(a, s); break;
     default: return launch_dkv<D, false, 4, 1>(a, s);
   }
+  if (st != HSAP_OK || a.head_split == 1) return st;
+  const int64_t blocks = ((int64_t)a.geom.P * a.geom.n * a.hkv * (D / 4) + 255) / 256;
+  hipLaunchKernelGGL(window_heads_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, D);
+  return check_launch_window("window_attn_bwd head sum");
 }
 
 }  // namespace hsap
@@ -733,7 +804,7 @@ extern "C" int64_t hsap_window_attn_bwd_workspace(const hsap_attn_desc* desc, in
   static const int32_t none = 0;
   if (check_window(desc, window, sinks, &none, 1, &g) != HSAP_OK) return -1;
   const int32_t s = (int32_t)std::min<int64_t>(sinks, g.Ns);
-  return bwd_workspace(desc, g, window, s);
+  return bwd_workspace(desc, g, (int32_t)std::min<int64_t>(window, g.Ns), s);
 }
 
 extern "C" hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int32_t sinks, const void* q,
@@ -767,7 +838,9 @@ extern "C" hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t 
   a.o = (const __bf16*)o;
   a.lse = lse;
   a.delta = (float*)workspace;
-  a.partial = (float*)((char*)workspace + delta_bytes(desc, a.geom));
+  a.head_split = head_split(desc, a.geom, a.window);
+  a.heads_part = (float*)((char*)workspace + delta_bytes(desc, a.geom));
+  a.partial = (float*)((char*)a.heads_part + heads_bytes(desc, a.geom, a.window));
   a.cu = cu_seqlens;
   a.dq = (__bf16*)dq;
   a.dk = dk;

@@ -170,6 +170,17 @@ def test_head_groups(hq, hkv):
     Problem(_cu([150, 40]), 190, 60, 2, hq=hq, hkv=hkv, d=64, seed=hq).check()
 
 
+@pytest.mark.parametrize("d,wide", [(128, False), (64, True)])
+def test_heads_of_a_group_in_several_workgroups(d, wide):
+    # few key tiles, many heads and a wide window: the heads are dealt out, their parts summed
+    for P, layout, shard in ((1, "contiguous", 0), (2, "zigzag", 1)):
+        print(P, layout, flush=True)
+        p = Problem(_cu([500, 0, 85]), 600, 300, 4, P=P, layout=layout, shard=shard, hq=40, hkv=2, d=d, seed=3, pad_nan=True,
+                    wide_grads=wide)
+        assert p.outputs()["workspace"].numel() > 2 * P * p.n * 2 * 2 * d * 4
+        p.check()
+
+
 def test_large_scores_and_wide_gradients():
     p = Problem(_cu([170, 30]), 200, 50, 4, hq=2, hkv=1, d=64, scale=2.0, wide_grads=True, seed=4)
     p.check()

@@ -66,7 +66,7 @@ def test_backward_workspace_and_sinks():
     lib, d = L.lib(), _desc()
     size = L.window_attn_bwd_workspace(d, 10, 4)
     assert size == (4 * 1001 * 4 + 255) // 256 * 256 + 4 * 2 * 4 * 2 * 128 * 4     # delta, four chunks' partials
-    assert L.window_attn_bwd_workspace(d, 1001, 4) == L.window_attn_bwd_workspace(d, 10, 0)   # nothing beyond the window
+    assert L.window_attn_bwd_workspace(d, 1001, 4) == L.window_attn_bwd_workspace(d, 1001, 0)   # nothing beyond the window
     assert _bwd(d, sinks=4, size=size - 1) == L.HSAP_ERR_INVALID_ARG
     assert str(size) in lib.hsap_last_error().decode()
     assert _bwd(d, sinks=129) == L.HSAP_ERR_UNSUPPORTED and "128" in lib.hsap_last_error().decode()
