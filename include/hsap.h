@@ -761,7 +761,7 @@ hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int
  *               page_table[s, p].  Entries of pages without a token that a call reads or writes are not looked at
  *               (a window lets a serving loop hand old pages back).  An entry outside [0, num_pages) is no page:
  *               nothing is written there and its tokens are not seen.  Several sequences may share pages they only
- *               read; a page that two sequences append to in one call holds either's codes.
+ *               read; the codes and scale of a page that two sequences append to in one call are undefined.
  *   seq_lens    device int32 [num_seqs]: tokens of each sequence, the new ones included.  0 (or less): an idle slot.
  *   cu_new      device int32 [num_seqs + 1], 0 = cu[0] <= ... <= cu[num_seqs] <= total_new: sequence s has the rows
  *               cu[s] .. cu[s + 1] - 1 of the new-token tensors, its last tokens, at positions seq_lens[s] - count ..

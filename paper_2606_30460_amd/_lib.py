@@ -732,7 +732,7 @@ def window_attn_fwd(desc: AttnDesc, window: int, sinks: int, q, k, v, cu_seqlens
         _arg(k, "bfloat16", "k", nkv, here), _arg(v, "bfloat16", "v", nkv, here),
         _arg(cu_seqlens_dev, "int32", "cu_seqlens", None, here), cu_seqlens_dev.numel() - 1,
         _arg(o_out, "bfloat16", "o_out", nq, here), _arg(lse_out, "float32", "lse_out", desc.heads_q * n, here),
-        _stream(stream)))
+        _stream_on(stream, here)))
 
 
 def window_attn_bwd_workspace(desc: AttnDesc, window: int, sinks: int) -> int:
@@ -756,7 +756,7 @@ def window_attn_bwd(desc: AttnDesc, window: int, sinks: int, q, k, v, d_o, o, ls
         _arg(o, "bfloat16", "o", nq, here), _arg(lse, "float32", "lse", desc.heads_q * n, here),
         _arg(cu_seqlens_dev, "int32", "cu_seqlens", None, here), cu_seqlens_dev.numel() - 1,
         _arg(dq, "bfloat16", "dq", nq, here), _arg(dk, grads, "dk", nkv, here), _arg(dv, grads, "dv", nkv, here),
-        int(grads == "float32"), _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream(stream)))
+        int(grads == "float32"), _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream_on(stream, here)))
 
 
 # ---------------------------------------------------------------------------
@@ -793,7 +793,7 @@ class KVCache:
 def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int):
     """Address and row stride (elements) of a bf16 tensor [rows, heads, d] on the current device, its rows contiguous."""
     torch = _torch or _load_torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
         raise TypeError("%s must be a device tensor" % what)
     if t.dtype is not _dtypes["bfloat16"]:
         raise TypeError("%s must be bfloat16, got %s" % (what, t.dtype))
@@ -805,6 +805,11 @@ def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int):
     if (one != 1 or (head != d and heads > 1)) and rows:
         raise ValueError("%s must have contiguous rows [heads, head_dim]" % what)
     return t.data_ptr(), (row if rows > 1 else heads * d)
+
+
+def _stream_on(stream, here: int) -> int:
+    """_stream for the current device, already known."""
+    return _torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
 
 
 def _cache_here(cache: KVCache) -> int:
@@ -840,7 +845,7 @@ def cache_append(cache: KVCache, k, v, cu_new, cos_sin=None, interleaved: bool =
         qp, qs = _token_rows(q, "q", total, heads, d, here)
         qo = _arg(q_out, "bfloat16", "q_out", total * heads * d, here)
     _check(lib().hsap_cache_append(*cache._refs, kp, ks, vp, vs, cu, total, table, rows, rot, 1 if interleaved else 0, ko, qp,
-                                   qs, heads, qo, _stream(stream)))
+                                   qs, heads, qo, _stream_on(stream, here)))
 
 
 def cache_attn_workspace(cache: KVCache, heads_q: int, total_q: int, one_each: Optional[bool] = None) -> int:
@@ -866,7 +871,7 @@ def cache_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_new, o_
         0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here), total,
         _arg(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim, here),
         0 if lse_out is None else _arg(lse_out, "float32", "lse_out", total * heads_q, here),
-        _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream(stream)))
+        _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream_on(stream, here)))
 
 
 # ---------------------------------------------------------------------------

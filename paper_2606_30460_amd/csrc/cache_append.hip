@@ -235,7 +235,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     rotate_q<D>(a, (int64_t)(blockIdx.x - a.kv_blocks) * 256 + threadIdx.x);
     return;
   }
-  __shared__ float wave_max[4];
+  __shared__ float wave_max[4], old_scale;
   const int tid = threadIdx.x;
   const bool is_v = blockIdx.x & 1;
   const int32_t pair = (int32_t)(blockIdx.x >> 1);
@@ -279,14 +279,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   if (page < 0) return;
   float* scale = (is_v ? a.c.v_scale : a.c.k_scale) + (int64_t)page * a.d.heads_kv + h;
   uint8_t* codes = (is_v ? a.c.v_codes : a.c.k_codes) + cache_row(page, a.d.heads_kv, h, ps, 0, D);
-  const float old = slot0 > 0 ? *scale : 0.f;
+  if (tid == 0) old_scale = slot0 > 0 ? *scale : 0.f;  // (read by the thread that writes it)
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
   if ((tid & 63) == 0) wave_max[tid >> 6] = amax;
   __syncthreads();
   amax = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
   float inv, ratio;
-  const float now = page_scale(amax, slot0 > 0, old, inv, ratio);
+  const float now = page_scale(amax, slot0 > 0, old_scale, inv, ratio);
   if (ratio != 1.f)
     for (int e = tid; e < slot0 * UNITS; e += 256) recode16(codes + 16 * e, ratio);
 #pragma unroll
