@@ -716,7 +716,7 @@ hsap_status hsap_convert_f32_bf16(const float* src, void* dst, int64_t count, vo
  *   cu_seqlens  DEVICE int32 [num_docs + 1], 0 = cu[0] <= cu[1] <= ... <= cu[num_docs] <= B * N, a boundary at every
  *               b * N (rules of hsap_plan; read by the kernels, so not checked).  Positions at or behind
  *               cu[num_docs] are padding: their q, k, v rows are not read, their rows of every output not written.
- *   q, k, v and d_o are finite in the rows of the documents.
+ *   q, d_o and the k, v rows that some query of the shard sees are finite.  No output overlaps an input.
  * --------------------------------------------------------------------- */
 
 /*
@@ -742,6 +742,7 @@ int64_t hsap_window_attn_bwd_workspace(const hsap_attn_desc* desc, int32_t windo
  *               0 for a key that none of them sees.  Every row of the documents is written (not accumulated).
  *   workspace   device, 16-byte aligned, at least hsap_window_attn_bwd_workspace bytes (workspace_bytes: its size);
  *               contents on entry ignored.  Calls that overlap in time need workspaces of their own.
+ * q, k, v, d_o, o 16-byte aligned, dq 8-byte, dk and dv 8-byte as bf16, 16-byte as fp32.
  * sinks <= 128 wherever window < N, else HSAP_ERR_UNSUPPORTED.  Two to five launches on `stream`; no atomics: the same
  * inputs give the same bits.
  */
@@ -799,6 +800,8 @@ typedef struct {
  *   rot_dim     a multiple of 16 up to d; 0: no rotation, cos_sin not read.
  *   k_out       device bf16 [total_new, Hkv, d] or NULL: K rotated (for the prompt's own attention).
  *   q, q_out    device bf16 [total_new, heads_q, d] (q with a row stride as k; q_out contiguous), both or neither.
+ * k_out and q_out are 16-byte aligned; k_out may be k and q_out q (rotated in place) where those rows are contiguous, else
+ * no output overlaps an input.
  * Scales are powers of two: the smallest 2^e, -100 <= e <= 120, with 448 * 2^e >= every value of the page and head, among
  * the tokens it holds (a token overwritten at its position still counts until the page is begun anew).  Codes are
  * e4m3 of value / scale, fp32 rounded to nearest even, once.  When a new token raises a page's scale, the codes of

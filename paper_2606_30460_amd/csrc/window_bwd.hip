@@ -415,10 +415,12 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 && D == 128 ? 1 : 2) 
     bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
     {
       const int64_t at = (krow * a.hkv + g) * D + 8 * hi;
+      // (the row of a key that no query of the shard sees may hold anything)
+      const bool seen = (len[0] > 0 && qlo + len[0] > seg_lo[0]) || (len[1] > 0 && qlo + len[1] > seg_lo[1]);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        kf[kk] = *(const bf16x8*)(a.k + at + 16 * kk);
-        const bf16x8 x = *(const bf16x8*)(a.v + at + 16 * kk);
+        kf[kk] = seen ? *(const bf16x8*)(a.k + at + 16 * kk) : bf16x8{};
+        const bf16x8 x = seen ? *(const bf16x8*)(a.v + at + 16 * kk) : bf16x8{};
         if constexpr (VLDS) *(bf16x8*)(vtile + 32 * w * D + swz<CPR>(l32, 16 * kk + 8 * hi)) = x;  // (the streams' are the same)
         else vf[kk] = x;
       }

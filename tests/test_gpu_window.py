@@ -158,6 +158,32 @@ def test_padding_rows_are_not_read_and_not_written():
         assert bool((out[x] == 7.0).all()), x
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("layout,P,shard", [("contiguous", 4, 2), ("zigzag", 3, 1)])
+@pytest.mark.parametrize("window,sinks", [(30, 3), (70, 0)])
+def test_rows_that_no_query_sees_may_hold_anything(layout, P, shard, window, sinks, d):
+    # the rows of other shards that were never fetched: NaN there gives the bits of finite values there, and gradient 0
+    print(layout, P, window, sinks, d, flush=True)
+    N, lengths = 240 * P, [100, 1, 240 * P - 160, 59]
+    p = Problem(_cu(lengths), N, window, sinks, P=P, layout=layout, shard=shard, hq=4, hkv=2, d=d, seed=P)
+    start = np.repeat(np.concatenate([[0], np.cumsum(lengths)[:-1]]), lengths)
+    i, j = p.pos[:, None], np.arange(N)[None]
+    seen = ((start[i] <= j) & (j <= i) & ((i - j < window) | (j - start[i] < sinks))).any(0)
+    assert seen[p.pos].all() and not seen.all()
+    finite, out = p.outputs(), p.outputs(fill=-3.0)
+    p.forward(finite)
+    p.backward(finite)
+    unseen = torch.from_numpy(~seen[p.order]).cuda()
+    for x in ("k", "v"):
+        p.dev[x].view(N, 2, d)[unseen] = float("nan")
+    p.forward(out)
+    p.backward(out)
+    torch.cuda.synchronize()
+    for x in ("o", "lse", "dq", "dk", "dv"):
+        assert torch.equal(finite[x], out[x]), x
+    assert not bool(out["dk"].view(N, 2, d)[unseen].any()) and not bool(out["dv"].view(N, 2, d)[unseen].any())
+
+
 def test_many_empty_documents():
     # more boundaries at one position than the kernels' window of boundaries holds
     cu = _cu([10] + [0] * 200 + [30] + [0] * 90 + [1] * 150 + [0] * 70)
