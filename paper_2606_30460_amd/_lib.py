@@ -766,7 +766,11 @@ def window_attn_bwd(desc: AttnDesc, window: int, sinks: int, q, k, v, d_o, o, ls
 class KVCache:
     """The tensors of a paged e4m3 K/V cache (hsap_cache): codes uint8 [num_pages, Hkv, page_size, d], scales fp32
     [num_pages, Hkv], page_table int32 [num_seqs, table_width], seq_lens int32 [num_seqs].  The tensors are the
-    caller's: writing other pages or lengths into them changes the next call."""
+    caller's: writing other pages or lengths into them changes the next call, and so does putting another tensor of the
+    same shape into an attribute."""
+
+    _TYPES = {"k_codes": "uint8", "v_codes": "uint8", "k_scale": "float32", "v_scale": "float32", "page_table": "int32",
+              "seq_lens": "int32"}
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens):
         _dev(k_codes, "uint8", "k_codes")
@@ -788,6 +792,16 @@ class KVCache:
         self.buffers = CacheBuffers(*[_ptr(t) for t in self.tensors])
         self.device_index = k_codes.get_device()
         self._refs = (ctypes.byref(self.desc), ctypes.byref(self.buffers))
+
+    def __setattr__(self, name, t):
+        if name in self._TYPES and "_refs" in self.__dict__:
+            old = getattr(self, name)
+            _dev(t, self._TYPES[name], name)
+            if t.shape != old.shape or t.device != old.device:
+                raise ValueError("%s is %s on %s, the cache's %s on %s" % (name, list(t.shape), t.device, list(old.shape), old.device))
+            setattr(self.buffers, name, _ptr(t))
+            self.tensors = tuple(t if x == name else getattr(self, x) for x in self._TYPES)
+        object.__setattr__(self, name, t)
 
 
 def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int):

@@ -51,16 +51,17 @@ struct CacheAttnArgs {
 struct Steps {
   int32_t sinks;   // sink steps
   int32_t win0;    // first token of the window steps (a multiple of 32)
+  int32_t lo;      // first token of a window, win0 or up to 31 behind it
   int32_t total;
 };
 
 __device__ __forceinline__ Steps cache_steps(int32_t plo, int32_t phi, int32_t cap, int32_t window, int32_t sinks) {
   phi = min(phi, cap - 1);
-  if (phi < 0) return Steps{0, 0, 0};
+  if (phi < 0) return Steps{0, 0, 0, 0};
   const int32_t lo = max(0, max(plo, 0) - (window - 1));
   const int32_t win0 = min(lo, phi + 1) & ~31;
   const int32_t ns = (min(sinks, win0) + 31) / 32;
-  return Steps{ns, win0, ns + (phi >= win0 ? (phi - win0) / 32 + 1 : 0)};
+  return Steps{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / 32 + 1 : 0)};
 }
 
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
@@ -170,13 +171,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     VT v[8];
     float ks[2], vs[2];
     int32_t j0;
-    bool held[2];  // each half of 16 tokens lies in a page and has a token that is seen
+    bool held[2];  // each half of 16 tokens lies in a page
   };
   // Pages of a step's halves (-1: none), looked up a step before its codes are asked for, those a step before their use.
   struct Where {
     int32_t page[2];
   };
   auto first_token = [&](int32_t s) { return s < steps.sinks ? 32 * s : steps.win0 + 32 * (s - steps.sinks); };
+  // Of a step's tokens up to `top` some row sees those from the first window on and the sinks, so all of them behind the first
+  // window step; in the steps before that (tokens that the sink steps show belong to them alone) and in it, a place that
+  // no row sees may hold anything, NaN included.
+  auto seen = [&](int32_t s, int32_t first, int32_t last) {  // has `first` .. `last` a token that some row sees
+    return s < steps.sinks ? first < min(a.sinks, steps.win0) : last >= steps.lo || first < a.sinks;
+  };
   auto look_up = [&](int32_t s) __attribute__((always_inline)) {
     Where x{{-1, -1}};
     if (s < s_end) {
@@ -236,7 +243,6 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
         }
       }
     const int32_t jl = x.j0 + 31;
-    // tokens that the sink steps show belong to them alone; a window step's may be sinks too
     const int32_t sinks = s < steps.sinks ? min(a.sinks, steps.win0) : a.sinks;
     const int32_t near = s < steps.sinks ? 0 : a.window;
     // every row of the tile sees every token of the step
@@ -304,10 +310,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     VT v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) v[y] = x.v[y];
-    if (jl > top || !x.held[0] || !x.held[1]) {  // what lies behind the last token is whatever the page held before
+    if (jl > top || !x.held[0] || !x.held[1] || s <= steps.sinks) {  // P is 0 there, V whatever the page holds
 #pragma unroll
-      for (int y = 0; y < 8; ++y)
-        if (x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3) > top || !x.held[y >> 2]) v[y] = VT{};
+      for (int half = 0; half < 2; ++half)
+        if (!seen(s, x.j0 + 16 * half, x.j0 + 16 * half + 15)) vpow[half] = 1.f;  // (nor need its scale be one)
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int32_t j = x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3);
+        if (j > top || !x.held[y >> 2] || !seen(s, j, j)) v[y] = VT{};
+      }
     }
 #pragma unroll
     for (int c4 = 0; c4 < CB / 4; ++c4) {

@@ -268,6 +268,80 @@ def test_bad_and_handed_back_pages():
     _check_attn([90], [30], 16, 2, 1, 64, pages=p)
 
 
+@pytest.mark.parametrize("d,size", [(64, 16), (128, 16), (128, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (20, 0), (21, 3), (40, 17)])
+def test_places_that_no_row_sees_may_hold_anything(window, sinks, d, size):
+    # pages handed back and written by others, NaN codes and scales among them: the bits are those of finite values there
+    print(window, sinks, d, size, flush=True)
+    lens, hq = np.array([300, 77, 3, 129, 160]), 4
+    for new, one in ((np.ones(5, int), True), (np.array([40, 1, 3, 9, 0]), False)):
+        got = []
+        for poison in (False, True):
+            p = Pages(lens, size, 2, d, seed=size).fill(lens)
+            for s, n in enumerate(lens if poison else []):
+                i, j = np.arange(n - new[s], n)[:, None], np.arange(n)[None]
+                seen = ((j <= i) & ((i - j < window) | (j < sinks))).any(0)
+                for page in range(-(-n // size)):
+                    here = seen[page * size:(page + 1) * size]
+                    for x in "kv":
+                        if not here.any():
+                            p.scales[x][p.table[s, page]] = [np.nan, np.inf]
+                        p.codes[x][p.table[s, page], :, np.flatnonzero(~here)] = 0xFF
+            got.append(_check_attn(lens, new, size, hq, 2, d, window, sinks, pages=p, one=one)
+                       if not poison else _attn_only(p, lens, new, hq, window, sinks, one))
+        assert torch.equal(got[0], got[1])
+
+
+def _attn_only(p, lens, new, hq, window, sinks, one):
+    cache, n = p.device(lens), int(new.sum())
+    q = torch.randn(n, hq, p.d, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+    o = torch.full((n, hq, p.d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((L.cache_attn_workspace(cache, hq, n),), 0xFF, dtype=torch.uint8, device="cuda")
+    cu = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).cuda()
+    L.cache_attn(cache, hq, 1 / math.sqrt(p.d), q, None if one else cu, o, None, ws, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    return o
+
+
+def test_rotated_in_place():
+    # k_out may be k and q_out q, where their rows are contiguous
+    lens, new = [40, 9, 17], [30, 1, 17]
+    for interleaved in (False, True):
+        for one in (False, True):
+            count = [1, 1, 1] if one else new
+            n, cu = sum(count), torch.tensor(np.concatenate([[0], np.cumsum(count)]), dtype=torch.int32, device="cuda")
+            g = torch.Generator().manual_seed(1)
+            q, k, v = (torch.randn(n, h, 64, generator=g).to(torch.bfloat16).cuda() for h in (4, 2, 2))
+            caches = [Pages(lens, 16, 2, 64, seed=1).fill(np.subtract(lens, count)).device() for _ in range(2)]
+            q_out, k_out, args = torch.empty_like(q), torch.empty_like(k), dict(cos_sin=_cos_sin(64, 32), interleaved=interleaved)
+            L.cache_append(caches[0], k, v, None if one else cu, k_out=k_out, q=q, q_out=q_out, **args)
+            L.cache_append(caches[1], k, v, None if one else cu, k_out=k, q=q, q_out=q, **args)
+            torch.cuda.synchronize()
+            assert torch.equal(q, q_out) and torch.equal(k, k_out)
+            for a, b in zip(caches[0].tensors, caches[1].tensors):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_other_tensors_put_into_a_cache():
+    p = Pages([40, 50], 16, 2, 64, seed=1).fill([40, 50])
+    cache = p.device([40, 50])
+    q = torch.randn(2, 4, 64, device="cuda").to(torch.bfloat16)
+    ws = torch.empty(L.cache_attn_workspace(cache, 4, 2), dtype=torch.uint8, device="cuda")
+    o, want = torch.empty_like(q), torch.empty_like(q)
+    L.cache_attn(p.device([17, 30]), 4, 0.1, q, None, want, None, ws)
+    cache.seq_lens = cache.seq_lens - torch.tensor([23, 20], dtype=torch.int32, device="cuda")
+    L.cache_attn(cache, 4, 0.1, q, None, o, None, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(o, want)
+    cache.seq_lens += 1
+    assert cache.tensors[5] is cache.seq_lens and cache.seq_lens.tolist() == [18, 31]
+    for bad in (cache.seq_lens.cpu(), cache.seq_lens.long(), cache.seq_lens[:1]):
+        with pytest.raises((TypeError, ValueError)):
+            cache.seq_lens = bad
+    with pytest.raises(ValueError):
+        cache.page_table = cache.page_table.view(1, -1)
+
+
 def test_shared_pages():
     p = Pages([64, 64], 16, 1, 64, seed=4).fill([64, 0])
     p.table[1, :4] = p.table[0, :4]
