@@ -818,7 +818,7 @@ hsap_status hsap_cache_append(const hsap_cache_desc* desc, const hsap_cache* cac
                               void* hip_stream);
 
 /* Bytes of device workspace hsap_cache_attn needs for any window (host); -1 for invalid arguments.  desc's num_pages is
- * not read. */
+ * not read.  Fewer rows are cut into more parts, so a call of fewer may need more: take the largest over the calls. */
 int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each);
 
 /*

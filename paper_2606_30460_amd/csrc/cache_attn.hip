@@ -20,6 +20,7 @@
 #include "cache.h"
 #include "hsap_internal.h"
 #include "mfma.h"
+#include "window.h"
 
 namespace hsap {
 
@@ -46,26 +47,39 @@ struct CacheAttnArgs {
   float scale_log2;
 };
 
-// Token ranges that the rows at positions plo .. phi of one sequence see, in steps of 32: the sinks' from 0 on, then the
+// Token ranges that the rows at positions plo .. phi of one sequence see, in steps of STEP: the sinks' from 0 on, then the
 // windows'.  Tokens at or behind cap are in no page.
+template <int STEP>
 struct Steps {
   int32_t sinks;   // sink steps
-  int32_t win0;    // first token of the window steps (a multiple of 32)
-  int32_t lo;      // first token of a window, win0 or up to 31 behind it
+  int32_t win0;    // first token of the window steps (a multiple of STEP)
+  int32_t lo;      // first token of a window, win0 or less than STEP behind it
   int32_t total;
+
+  __device__ __forceinline__ int32_t first(int32_t s) const { return s < sinks ? STEP * s : win0 + STEP * (s - sinks); }
+  // Of a step's tokens up to the last row's position some row sees those from the first window on and the sinks, so all of
+  // them behind the first window step; in the steps before that (tokens that the sink steps show belong to them alone) and
+  // in it, a place that no row sees may hold anything, NaN included.
+  __device__ __forceinline__ bool edge(int32_t s) const { return s <= sinks; }
+  __device__ __forceinline__ bool seen(int32_t s, int32_t all_sinks, int32_t from, int32_t to) const {  // a token of from .. to
+    return s < sinks ? from < min(all_sinks, win0) : to >= lo || from < all_sinks;
+  }
 };
 
-__device__ __forceinline__ Steps cache_steps(int32_t plo, int32_t phi, int32_t cap, int32_t window, int32_t sinks) {
+template <int STEP>
+__device__ __forceinline__ Steps<STEP> cache_steps(int32_t plo, int32_t phi, int32_t cap, int32_t window, int32_t sinks) {
   phi = min(phi, cap - 1);
-  if (phi < 0) return Steps{0, 0, 0, 0};
+  if (phi < 0) return Steps<STEP>{0, 0, 0, 0};
   const int32_t lo = max(0, max(plo, 0) - (window - 1));
-  const int32_t win0 = min(lo, phi + 1) & ~31;
-  const int32_t ns = (min(sinks, win0) + 31) / 32;
-  return Steps{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / 32 + 1 : 0)};
+  const int32_t win0 = min(lo, phi + 1) & ~(STEP - 1);
+  const int32_t ns = (min(sinks, win0) + STEP - 1) / STEP;
+  return Steps<STEP>{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / STEP + 1 : 0)};
 }
 
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
 __device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
+
+constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -138,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
   const int32_t pos0 = len - rt.count;  // position of the sequence's first new token
   const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
-  const Steps steps = cache_steps(plo, phi, cap, a.window, a.sinks);
+  const Steps<32> steps = cache_steps<32>(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
   const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
   if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
@@ -177,17 +191,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   struct Where {
     int32_t page[2];
   };
-  auto first_token = [&](int32_t s) { return s < steps.sinks ? 32 * s : steps.win0 + 32 * (s - steps.sinks); };
-  // Of a step's tokens up to `top` some row sees those from the first window on and the sinks, so all of them behind the first
-  // window step; in the steps before that (tokens that the sink steps show belong to them alone) and in it, a place that
-  // no row sees may hold anything, NaN included.
-  auto seen = [&](int32_t s, int32_t first, int32_t last) {  // has `first` .. `last` a token that some row sees
-    return s < steps.sinks ? first < min(a.sinks, steps.win0) : last >= steps.lo || first < a.sinks;
-  };
   auto look_up = [&](int32_t s) __attribute__((always_inline)) {
     Where x{{-1, -1}};
     if (s < s_end) {
-      const int32_t j0 = first_token(s);
+      const int32_t j0 = steps.first(s);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int32_t at = (j0 + 16 * half) >> a.page_shift;
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     return x;
   };
   auto load = [&](int32_t s, const Where& where, Tokens& x) __attribute__((always_inline)) {
-    x.j0 = first_token(s);
+    x.j0 = steps.first(s);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int32_t j = x.j0 + 16 * half;
@@ -310,14 +317,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     VT v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) v[y] = x.v[y];
-    if (jl > top || !x.held[0] || !x.held[1] || s <= steps.sinks) {  // P is 0 there, V whatever the page holds
+    if (jl > top || !x.held[0] || !x.held[1] || steps.edge(s)) {  // P is 0 there, V whatever the page holds
 #pragma unroll
       for (int half = 0; half < 2; ++half)
-        if (!seen(s, x.j0 + 16 * half, x.j0 + 16 * half + 15)) vpow[half] = 1.f;  // (nor need its scale be one)
+        if (!steps.seen(s, a.sinks, x.j0 + 16 * half, x.j0 + 16 * half + 15)) vpow[half] = 1.f;  // (nor need its scale be one)
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
         const int32_t j = x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3);
-        if (j > top || !x.held[y >> 2] || !seen(s, j, j)) v[y] = VT{};
+        if (j > top || !x.held[y >> 2] || !steps.seen(s, a.sinks, j, j)) v[y] = VT{};
       }
     }
 #pragma unroll
@@ -438,6 +445,247 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   }
 }
 
+// Many rows of a sequence (a prompt's chunk): bound by products and exponentials, no longer by the codes, so a workgroup
+// takes 128 rows, a wave 32 of them, and every step's 64 tokens are decoded once for all: codes to registers a step ahead,
+// from there as bf16 (which e4m3 fits exactly; V times its scale's power of two) into the tiles of the window kernels, and
+// 32x32x16 products S^T = K Q^T, O^T += V^T P^T with V^T by transpose reads.  P is rounded to bf16 for the second product,
+// as in the window kernels.  2048 rows x 8 heads over 30000 tokens, head_dim 128: 665 us, 730 TFLOP/s (a step's products,
+// exponentials and decoding add up in a wave: matrix cores 0.33 busy).  head_dim 64: three workgroups per CU (185 -> 167 us).
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
+  constexpr int KB = 64, CPR = D / 8, TILE = KB * D, ROWS = kChunkRows, U = D / 64;  // U: runs of 16 codes per thread
+  constexpr float NEG_INF = -__builtin_inff(), TINY = 1.17549435e-38f;
+  constexpr float RESCALE_SLACK = 8.f;
+  __shared__ __attribute__((aligned(16))) __bf16 tiles[2][2][TILE];  // [slot][K, V]
+  __shared__ __attribute__((aligned(16))) float scales[2][2][4];     // [slot][K's times the softmax's, V's rest][16 tokens]
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = blockIdx.x % a.d.heads_kv;
+  const int32_t rest = blockIdx.x / a.d.heads_kv;
+  const int32_t split = rest % a.splits, tile = rest / a.splits;
+  RowTile rt;
+  if (!row_tile(a, tile, ROWS, rt)) return;
+  const int32_t len = max(0, a.c.seq_lens[rt.seq]);
+  const int32_t ps = a.d.page_size, cap = a.d.table_width * ps;
+  const int32_t nrows = rt.count * a.group;
+  const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
+  const int32_t pos0 = len - rt.count;
+  const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
+  const Steps<KB> steps = cache_steps<KB>(plo, phi, cap, a.window, a.sinks);
+  const int32_t per = steps_per_split(steps.total, a.splits);
+  const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
+  if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
+    const int32_t r = rt.row0 + tid, t = r / a.group;
+    if (tid < ROWS && r < nrows)
+      a.part_lse[((int64_t)split * a.total_q + rt.t0 + t) * a.heads_q + g * a.group + (r - t * a.group)] = NEG_INF;
+    return;
+  }
+  // this lane's query, and the first and last position of the wave's
+  const bool busy = rt.row0 + 32 * w <= last_row;
+  const int32_t row = min(rt.row0 + 32 * w + l32, last_row), tok = row / a.group;
+  const int32_t pos = pos0 + tok;
+  const int32_t wlo = pos0 + min(rt.row0 + 32 * w, last_row) / a.group;
+  const int32_t whi = pos0 + min(rt.row0 + 32 * w + 31, last_row) / a.group;
+  const int h = g * a.group + (row - tok * a.group);
+  bf16x8 qf[D / 16];
+  {
+    const __bf16* qp = a.q + (int64_t)(rt.t0 + tok) * a.q_stride + (int64_t)h * D + 8 * hi;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
+  }
+  const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
+  const int32_t top = min(phi, cap - 1);  // last token any row sees
+
+  // Thread's codes of a step: of the 64 tokens those of 16-token group group_of(u) (one page each), 16 codes of a token.
+  auto group_of = [&](int u) { return D == 64 ? w : (w >> 1) + 2 * u; };
+  const int slot_in = D == 64 ? (lane >> 2) : 8 * (w & 1) + (lane >> 3);  // token within the group
+  const int column = 16 * (D == 64 ? lane & 3 : lane & 7);
+  // Pages and scales are read as vectors: a scalar load, which may come back out of order, would make every wait for an LDS
+  // read a wait for memory.
+  int zero;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+  struct Codes {
+    uint4 k[U], v[U];
+    float ks[U], vs[U];
+    bool held[U];  // the group lies in a page
+  };
+  struct Where {
+    int32_t page[U];
+  };
+  auto look_up = [&](int32_t s) __attribute__((always_inline)) {
+    Where x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = steps.first(s) + 16 * group_of(u);
+      x.page[u] = s < s_end && j <= top ? table[(j >> a.page_shift) + zero] : -1;
+    }
+    return x;
+  };
+  auto load = [&](int32_t s, const Where& where, Codes& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = steps.first(s) + 16 * group_of(u);
+      const int32_t page = uniform(where.page[u]);
+      x.held[u] = (uint32_t)page < (uint32_t)a.d.num_pages;
+      const int64_t at = (int64_t)(x.held[u] ? page : 0) * a.d.heads_kv + g;
+      x.ks[u] = (a.c.k_scale + at)[zero];
+      x.vs[u] = (a.c.v_scale + at)[zero];
+      const int64_t first = ((at << a.page_shift) + (j & (ps - 1)) + slot_in) * D + column;
+      x.k[u] = *(const uint4*)(a.c.k_codes + first);
+      x.v[u] = *(const uint4*)(a.c.v_codes + first);
+    }
+  };
+  auto decode = [&](const uint4& c, float pow2, __bf16* out0, __bf16* out1) __attribute__((always_inline)) {
+    bf16x2 p[8];
+    decode4(c.x, pow2, p[0], p[1]);
+    decode4(c.y, pow2, p[2], p[3]);
+    decode4(c.z, pow2, p[4], p[5]);
+    decode4(c.w, pow2, p[6], p[7]);
+    *(bf16x8*)out0 = bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+    *(bf16x8*)out1 = bf16x8{p[4][0], p[4][1], p[5][0], p[5][1], p[6][0], p[6][1], p[7][0], p[7][1]};
+  };
+  auto store = [&](int32_t s, Codes& x, int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int token = 16 * group_of(u) + slot_in;
+      const int32_t j = steps.first(s) + token;
+      float vpow = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
+      if (j > top || !x.held[u] || (steps.edge(s) && !steps.seen(s, a.sinks, j, j))) {  // anything may be there
+        x.k[u] = x.v[u] = uint4{0, 0, 0, 0};
+        vpow = 1.f;
+      }
+      const int at0 = swz<CPR>(token, column), at1 = swz<CPR>(token, column + 8);
+      decode(x.k[u], 1.f, tiles[slot][0] + at0, tiles[slot][0] + at1);
+      decode(x.v[u], vpow, tiles[slot][1] + at0, tiles[slot][1] + at1);
+      // (a scale of 0 stands for no page; at least the smallest normal number, so that -inf times it stays -inf)
+      if (lane == 0) {
+        scales[slot][0][group_of(u)] = x.held[u] ? fmaxf(x.ks[u] * a.scale_log2, TINY) : 0.f;
+        scales[slot][1][group_of(u)] = __uint_as_float((__float_as_uint(x.vs[u]) & 0x007FFFFFu) | 0x3F800000u);
+      }
+    }
+  };
+
+  TileReads<D> rd;
+  rd.init(lane);
+  float m_run = NEG_INF, l_run = 0.f;
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
+
+  auto compute = [&](int32_t s, int slot) __attribute__((always_inline)) {
+    const int32_t j0 = steps.first(s);
+    const f32x4 sl = *(const f32x4*)scales[slot][0], vrest = *(const f32x4*)scales[slot][1];
+    f32x16 sc[2];
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      bf16x8 kf[D / 16];
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) kf[kk] = rd.rows(tiles[slot][0] + 32 * nb * D, kk);
+      sc[nb] = f32x16{};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) sc[nb] = mfma32(kf[kk], qf[kk], sc[nb]);
+    }
+    const int32_t sinks = s < steps.sinks ? min(a.sinks, steps.win0) : a.sinks;
+    const int32_t near = s < steps.sinks ? 0 : a.window;
+    const bool held = sl[0] > 0.f && sl[1] > 0.f && sl[2] > 0.f && sl[3] > 0.f;
+    // every row of the wave sees every token of the step
+    const bool all = __builtin_amdgcn_ballot_w64(!held) == 0 && j0 + KB - 1 <= wlo && (whi - j0 < near || j0 + KB - 1 < sinks);
+    if (!all) {
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int32_t t = j0 + 32 * nb + c_row(j, hi);
+          const bool see = (t <= pos) & (((int32_t)((uint32_t)pos - (uint32_t)t) < near) | (t < sinks)) & (sl[2 * nb + (j >> 3)] > 0.f);
+          sc[nb][j] = see ? sc[nb][j] : NEG_INF;
+        }
+    }
+    float mx = NEG_INF;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float x = sc[q >> 1][8 * (q & 1)];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) x = fmaxf(x, sc[q >> 1][8 * (q & 1) + j]);
+      mx = fmaxf(mx, x * fmaxf(sl[q], TINY));
+    }
+    // (the two lanes of a row join their maxima only when some row's rose by more than the slack)
+    if (__builtin_amdgcn_ballot_w64(mx > m_run + RESCALE_SLACK) != 0) {
+      const float m_new = fmaxf(m_run, pair_max(mx));
+      const float alpha = m_run == NEG_INF ? 0.f : fast_exp2(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == NEG_INF ? 0.f : m_run;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float x = fmaxf(sl[q], TINY);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float p = fast_exp2(__builtin_fmaf(sc[q >> 1][8 * (q & 1) + j], x, -m_use));
+        l_run += p;
+        sc[q >> 1][8 * (q & 1) + j] = p;
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(vrest[0] != 1.f || vrest[1] != 1.f || vrest[2] != 1.f || vrest[3] != 1.f) != 0) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) sc[j >> 4][j & 15] *= vrest[j >> 3];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x8 pb;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pb[j] = (__bf16)sc[q >> 1][8 * (q & 1) + j];
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) o[mb] = mfma32(rd.turned(tiles[slot][1] + 16 * q * D, mb), pb, o[mb]);
+    }
+  };
+
+  if (s_begin < s_end) {
+    Codes x;
+    load(s_begin, look_up(s_begin), x);
+    store(s_begin, x, 0);
+    Where next = look_up(s_begin + 1);
+    hsap_lds_barrier();
+    for (int32_t s = s_begin; s < s_end; ++s) {
+      const int slot = (s - s_begin) & 1;
+      const bool more = s + 1 < s_end;
+      if (more) load(s + 1, next, x);
+      next = look_up(s + 2);
+      const int32_t j0 = steps.first(s);
+      if (busy && j0 <= whi && (s < steps.sinks || j0 + KB - 1 >= max(wlo, 0) - (a.window - 1) || j0 < a.sinks)) compute(s, slot);
+      if (more) store(s + 1, x, slot ^ 1);
+      hsap_lds_barrier();
+    }
+  }
+  l_run = pair_sum(l_run);
+  if (rt.row0 + 32 * w + l32 > last_row) return;
+  const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+  const float lse2 = l_run > 0.f ? m_run + __log2f(l_run) : NEG_INF;
+  const int64_t out = (int64_t)(rt.t0 + tok) * a.heads_q + h;
+  if (a.splits == 1) {
+    __bf16* op = a.o + out * D + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(bf16x4*)(op + 32 * mb + 8 * q) = bf16x4{(__bf16)(o[mb][4 * q] * inv), (__bf16)(o[mb][4 * q + 1] * inv),
+                                                  (__bf16)(o[mb][4 * q + 2] * inv), (__bf16)(o[mb][4 * q + 3] * inv)};
+    if (hi == 0 && a.lse) a.lse[(int64_t)h * a.total_q + rt.t0 + tok] = lse2 * 0.69314718055994530942f;
+  } else {
+    const int64_t at = (int64_t)split * a.total_q * a.heads_q + out;
+    float* op = a.part_o + at * D + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(op + 32 * mb + 8 * q) = f32x4{o[mb][4 * q] * inv, o[mb][4 * q + 1] * inv, o[mb][4 * q + 2] * inv, o[mb][4 * q + 3] * inv};
+    if (hi == 0) a.part_lse[at] = lse2;
+  }
+}
+
 // Joins the splits of every row by their LSE.  Up to eight: D / 4 lanes per row, four values each, every load of a row
 // in flight together.
 template <int D>
@@ -526,29 +774,54 @@ __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
     a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
 }
 
-// How a call is cut: row tiles of 16 mt rows (two blocks where the sequences have more than 16 rows: 28 x 50 rows x 8 of 64
-// heads of 128 28 us, one block 34, four 48; 2048 rows over 30000 tokens, head_dim 64, 769, 1305 and 1012), and splits of a tile's tokens so that the grid fills the chip, each of
-// at least 256 tokens, at most 128 (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits 24.5, 128 19.4,
-// 256 22.0: more partials to join).
+// How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip, each of at least 256 tokens.
 struct CacheCut {
-  int mt;
+  int rows;  // of a tile: 16 or 32 (cache_attn_kernel), kChunkRows (cache_chunk_kernel)
   int64_t tiles;
   int32_t splits;
 };
 
-// Workgroups to aim at: twice what the chip holds at once (64 sequences of 8k tokens: 129 us with 512, 128 with 1024, 127
-// with 2048; 3 x 700 rows: 49, 43 and 47 us, where the fp32 partials begin to weigh).
+// Workgroups of cache_attn_kernel to aim at: twice what the chip holds at once (64 sequences of 8k tokens: 129 us with 512,
+// 128 with 1024, 127 with 2048).  At most 128 splits (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits
+// 24.5, 128 19.4, 256 22.0: more partials to join).
 constexpr int64_t kCacheGrid = 1024;
+
+// Two 16-row blocks where the sequences have more than 16 rows (28 x 50 rows x 8 of 64 heads of 128, us: 28, one block 34,
+// four 48).  128 rows, where the sequences have more than 64 and the grid can be filled: at head_dim 64 always (us, 32 -> 128
+// rows: 3 x 700 x 4 over 12000 tokens 44 -> 38; 4 x 300 x 4 over 6000 50 -> 48; 400 x 5 over 200000 445 -> 344), at 128
+// over many tokens, since it needs splits sooner and their partials are twice as large (2048 x 8 over 30000 787 -> 665,
+// 512 x 4 over 16000 217 -> 188, but 512 x 4, twice, over 8000 103 -> 116 and 32 x 8, 64 times, over 3125 94 -> 119).
+constexpr int64_t kChunkGrid = 2 * kComputeUnits, kChunkSplits = 16, kChunkTokens128 = 12000;
 
 static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
   const int64_t group = heads_q / d.heads_kv;
   const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
-  c.mt = rows > 16 ? 2 : 1;
-  c.tiles = one_each ? (int64_t)d.num_seqs * ((group + 16 * c.mt - 1) / (16 * c.mt))
-                     : item_base(total_q, group, 16 * c.mt, 1, d.num_seqs);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
-  c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+  // workgroups of 128 rows without splits (c.tiles counts a tile more per sequence, which does nothing)
+  const int64_t full = (total_q * group + kChunkRows - 1) / kChunkRows * d.heads_kv;
+  const bool chunk = rows > 64 && full * std::min(most, kChunkSplits) >= kChunkGrid && (d.head_dim == 64 || tokens >= kChunkTokens128);
+  c.rows = chunk ? kChunkRows : rows > 16 ? 32 : 16;
+  c.tiles = one_each ? (int64_t)d.num_seqs * ((group + c.rows - 1) / c.rows) : item_base(total_q, group, c.rows, 1, d.num_seqs);
+  if (!chunk) {
+    c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+    return c;
+  }
+  // Splits that make whole rounds of the chip's 512 workgroups, in ns: a round's steps of 64 tokens (2.2 us, head_dim 64 1.5)
+  // and its beginning and end, a join and the partials written and read (2048 x 8 rows over 30000 tokens: one split 1086,
+  // three 760, two 665).
+  c.splits = 1;
+  int64_t least = INT64_MAX;
+  for (int64_t s = 1; s <= std::min(most, kChunkSplits); ++s) {
+    const int64_t rounds = (full * s + kChunkGrid - 1) / kChunkGrid;
+    const int64_t steps = (tokens + 64 * s - 1) / (64 * s);
+    const int64_t ns = rounds * (steps * (d.head_dim == 64 ? 1500 : 2200) + 6000) +
+                       (s > 1 ? 4000 + total_q * heads_q * d.head_dim * 8 * s / 4000 : 0);
+    if (ns < least) {
+      least = ns;
+      c.splits = (int32_t)s;
+    }
+  }
   return c;
 }
 
@@ -557,10 +830,11 @@ static int64_t cache_workspace(const CacheCut& c, int32_t heads_q, int64_t total
 }
 
 template <int D>
-static void launch_cache_attn(const CacheAttnArgs& a, int mt, int64_t blocks, hipStream_t s) {
+static void launch_cache_attn(const CacheAttnArgs& a, int rows, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
   const int64_t bytes = 2 * (int64_t)a.d.num_seqs * a.d.table_width * a.d.page_size * a.d.heads_kv * D;
-  if (mt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
+  if (rows == kChunkRows) hipLaunchKernelGGL(cache_chunk_kernel<D>, grid, block, 0, s, a);
+  else if (rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
   else if (!a.cu && bytes > (int64_t(256) << 20)) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false>), grid, block, 0, s, a);
 }
@@ -630,8 +904,8 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
   if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
-  if (d == 128) launch_cache_attn<128>(a, c.mt, blocks, s);
-  else launch_cache_attn<64>(a, c.mt, blocks, s);
+  if (d == 128) launch_cache_attn<128>(a, c.rows, blocks, s);
+  else launch_cache_attn<64>(a, c.rows, blocks, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
   if (c.splits > 1) {

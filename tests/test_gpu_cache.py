@@ -247,6 +247,54 @@ def test_split_contexts(d):
     _check_attn([3000], [5], 128, 4, 1, d, window=700, sinks=4, seed=3, width=100)
 
 
+# Many rows over a table wide enough for the 128-row kernel (its tokens in many splits, most of them idle for the short
+# sequences), and a grid that needs no splits.
+CHUNKS = [([700, 77, 300, 0, 130], [200, 5, 64, 0, 130]), ([3000, 5], [300, 9])]
+
+
+@pytest.mark.parametrize("d,size", [(64, 16), (64, 64), (128, 32), (128, 128)])
+@pytest.mark.parametrize("lens,new", CHUNKS)
+@pytest.mark.parametrize("window,sinks", [(L.MAX_WINDOW, 0), (1, 0), (70, 3), (64, 100), (500, 17)])
+def test_chunks(lens, new, window, sinks, d, size):
+    print(lens, window, sinks, d, size, flush=True)
+    _check_attn(lens, new, size, 16, 8, d, window, sinks, width=12800 // size, pad=3, strided=size == 64, seed=size)
+
+
+def test_chunks_in_one_part():
+    _check_attn([300, 450], [200, 312], 32, 128, 8, 64, window=100, sinks=5, width=16)
+
+
+def test_chunks_of_other_scales_and_bad_pages():
+    for d, size in ((64, 16), (128, 64)):
+        p = Pages([600, 400], size, 8, d, seed=15, width=12800 // size).fill([600, 400])
+        rng = np.random.default_rng(1)
+        for x in "kv":
+            p.scales[x] *= rng.uniform(0.3, 3.0, p.scales[x].shape).astype(np.float32)
+        _check_attn([600, 400], [250, 100], size, 16, 8, d, pages=p, seed=15)
+        p.table[0, 3], p.table[1, 2] = -1, 10 ** 6          # no pages: their tokens are not seen
+        _check_attn([600, 400], [250, 100], size, 16, 8, d, window=400, sinks=9, pages=p, seed=16, lse=False)
+
+
+@pytest.mark.parametrize("d,size", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (90, 3), (40, 70)])
+def test_chunks_leave_unseen_places_alone(window, sinks, d, size):
+    lens, new = np.array([700, 500]), np.array([150, 200])
+    got = []
+    for poison in (False, True):
+        p = Pages(lens, size, 8, d, seed=size, width=12800 // size).fill(lens)
+        for s, n in enumerate(lens if poison else []):
+            i, j = np.arange(n - new[s], n)[:, None], np.arange(n)[None]
+            seen = ((j <= i) & ((i - j < window) | (j < sinks))).any(0)
+            for page in range(-(-n // size)):
+                here = seen[page * size:(page + 1) * size]
+                for x in "kv":
+                    if not here.any():
+                        p.scales[x][p.table[s, page]] = np.nan
+                    p.codes[x][p.table[s, page], :, np.flatnonzero(~here)] = 0xFF
+        got.append(_attn_only(p, lens, new, 16, window, sinks, False))
+    assert torch.equal(got[0], got[1]) and bool(torch.isfinite(got[0]).all())
+
+
 def test_large_scores_and_scales():
     p = Pages([90], 16, 1, 64, seed=5).fill([90], spread=4.0)
     _check_attn([90], [3], 16, 4, 1, 64, pages=p, seed=5)
