@@ -5,7 +5,9 @@
 // Few rows against many cached tokens: bound by reading the codes, 2 d bytes per token and K/V head.  So the query
 // heads of a K/V head (and a sequence's several new tokens) share one pass: rows r = (token, head of the group) in
 // tiles of 16 MT, one workgroup per (row tile, K/V head, split of the tile's tokens), a running maximum and sum per
-// wave, the waves' results joined in LDS, the splits' by a second launch over fp32 partials.
+// wave, the waves' results joined in LDS, the splits' by a second launch over fp32 partials.  64 sequences of up to 8192
+// tokens, 32 heads over 8 of 128: 115 us for the codes (5.5 TB/s; a large sum reads at 6.0) and 4.5 for the join.  One of
+// 131072 tokens, 16 heads over 2: 15 and 4 us, a chain of table, codes, sixteen steps and joins.
 //
 // A wave takes 32 tokens at a time (its workgroup's four waves take turns), with the next ones' codes in flight in
 // registers: no LDS on the way.  S^T = K Q^T by 16x16x32 products, tokens as rows: lane l holds row l % 16 of K and
@@ -13,7 +15,7 @@
 // has query l % 16 on lane l and tokens 4 (l / 16) .. +3 of each 16, which is the layout of the B operand of
 // O^T += V^T P^T if its eight tokens per lane are 4 (l / 16) + 0..3 of both halves; V's rows are loaded by those tokens
 // and turned in registers, two codes of two tokens at a time (v_perm, then the conversion to bf16, which e4m3 fits
-// exactly).
+// exactly).  P is rounded to bf16 for the second product (2^-8 relative at most, summed in fp32), O once at the end.
 #include <algorithm>
 #include <type_traits>
 
@@ -687,7 +689,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
 }
 
 // Joins the splits of every row by their LSE.  Up to eight: D / 4 lanes per row, four values each, every load of a row
-// in flight together.
+// in flight together (4.5 us for 64 rows x 32 heads x 2 splits, of which about 3 are the launch).
 template <int D>
 __global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a) {
   constexpr float NEG_INF = -__builtin_inff();

@@ -98,8 +98,8 @@ __device__ __forceinline__ DocSpan doc_span(const int32_t* cu, int32_t nd, int32
   return d;
 }
 
-// Transfers of a [R][D] bf16 tile (R = 64 by default) from global memory to a swizzled LDS tile (mfma.h), WAVES waves, 64 16-byte chunks
-// per instruction.  Issued from asm and ordered by the kernels' own vmcnt waits (vm_wait_barrier): the compiler would
+// Transfers of a [R][D] bf16 tile (R = 64 by default) from global memory to a swizzled LDS tile (mfma.h), WAVES waves, 64
+// 16-byte chunks per instruction.  Issued from asm and ordered by the kernels' own vmcnt waits (vm_wait_barrier): the compiler would
 // wait for every transfer before any later LDS read.
 template <int D, int WAVES, int R = 64>
 struct TileStage {

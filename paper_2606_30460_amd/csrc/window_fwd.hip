@@ -12,7 +12,13 @@
 // Per step: S^T = K Q^T with Q in registers (a lane holds one query and 16 keys of each 32-key block, so the row
 // statistics need only the lane and lane l ^ 32), then O^T += V^T P^T with P straight from registers and V^T by
 // LDS transpose reads.  K and V go from global memory to LDS directly, K two steps ahead and V one; the scores
-// of step s + 1 are formed beside the exponentials of step s.
+// of step s + 1 are formed beside the exponentials of step s.  P is rounded to bf16 for the second product (2^-8
+// relative at most, summed in fp32; the row sum takes the unrounded values); O is rounded once, at the end.
+//
+// Bound by the products and, beside them, the softmax's vector work (per 64-key step and wave, head_dim 128: 32 products,
+// 32 exponentials, 115 other vector instructions; with two waves per SIMD they come close to a sum).  65536 tokens,
+// 16 heads of 128, window 4096: 2080 us, 1014 TFLOP/s (library product 1314).  4096 of 32768 tokens, 32 heads, window 1024:
+// 95 us, where a workgroup's beginning and end are 8 of its 47 us.  2048 tokens, 4 heads of 64: 9.8 us, latency alone.
 #include <algorithm>
 #include <type_traits>
 
