@@ -1,11 +1,24 @@
 // Device helpers of the window-attention kernels: document bounds of a wave's positions, the row of a position in
-// sharded order, and the direct-to-LDS transfer of a 64-row tile.
+// sharded order, and the direct-to-LDS transfer of a 64-row tile.  What is index arithmetic alone also builds for the host
+// (tests).
 #pragma once
 
 #include "hsap_internal.h"
+
+#if defined(__HIPCC__)
 #include "mfma.h"
+#endif
 
 namespace hsap {
+
+// Key row that the dQ kernel reads for position x when it forms delta of a wave's short rows, whose windows begin at lo or
+// behind it and whose sinks before position g0, the wave's first row, are far .. far_end - 1.  A place that none of them
+// sees is g0's own instead: the rows that no query of the shard sees are not read.  (Positions from g0 to `last` are the
+// shard's own rows.)
+HSAP_HD inline int32_t short_row_key(int32_t x, int32_t g0, int32_t lo, int32_t far, int32_t far_end, int32_t last) {
+  if (x < lo && (x < far || x >= far_end)) return g0;
+  return x < last ? x : last;
+}
 
 #if defined(__HIPCC__)
 

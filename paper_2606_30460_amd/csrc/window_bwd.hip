@@ -159,15 +159,21 @@ __global__ __launch_bounds__(64 * WAVES * KS, KS * D > 128 ? 1 : 2) void window_
   const __bf16* vbase = a.v + (int64_t)g * D;
   // delta from O carries O's rounding, which dS = P (dP - delta) feels where a row has few keys (one key: dS is 0, but
   // for that rounding).  Rows of fewer than 32 keys take delta = sum_j P_ij dP_ij instead, over the 64 positions up
-  // to the wave's last row and the sinks of its first row's document, read straight from global memory.
+  // to the wave's last row and the sinks of its first row's document, read straight from global memory (a place of those
+  // that no short row sees: the wave's first row instead).
   const bool few = valid && gq - wlo + 1 + slen < 32;
-  if (__builtin_amdgcn_ballot_w64(few) != 0) {
+  const uint64_t short_rows = __builtin_amdgcn_ballot_w64(few);
+  if (short_rows != 0) {
     const int32_t g0 = __builtin_amdgcn_readlane(gq, 0), far = __builtin_amdgcn_readlane(doc.start, 0);
+    // (windows begin later from row to row, and a later row of a document has as many sinks before its window or more)
+    const int32_t lo = __builtin_amdgcn_readlane(wlo, __builtin_ctzll(short_rows));
+    const uint32_t of_far = (uint32_t)__builtin_amdgcn_ballot_w64(few && doc.start == far);
+    const int32_t far_end = far + (of_far ? __builtin_amdgcn_readlane(slen, 31 - __builtin_clz(of_far)) : 0);
     const bool sinks = __builtin_amdgcn_ballot_w64(few && slen > 0 && doc.start < g0 - 32) != 0;
     float sum = 0.f;
     for (int b = 0; b < (sinks ? 3 : 2); ++b) {
       const int32_t j0 = b == 2 ? far : g0 - 32 + 32 * b;
-      const int32_t j = max(0, min(j0 + l32, i1));  // this lane's key row
+      const int32_t j = short_row_key(j0 + l32, g0, lo, far, far_end, i1);  // this lane's key row
       const int64_t at = ((int64_t)(j + key_span(a.geom, j).delta) * a.hkv + g) * D + 8 * hi;
       f32x16 sc = f32x16{}, dp = f32x16{};
 #pragma unroll
