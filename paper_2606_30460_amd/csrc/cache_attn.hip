@@ -49,35 +49,6 @@ struct CacheAttnArgs {
   float scale_log2;
 };
 
-// Token ranges that the rows at positions plo .. phi of one sequence see, in steps of STEP: the sinks' from 0 on, then the
-// windows'.  Tokens at or behind cap are in no page.
-template <int STEP>
-struct Steps {
-  int32_t sinks;   // sink steps
-  int32_t win0;    // first token of the window steps (a multiple of STEP)
-  int32_t lo;      // first token of a window, win0 or less than STEP behind it
-  int32_t total;
-
-  __device__ __forceinline__ int32_t first(int32_t s) const { return s < sinks ? STEP * s : win0 + STEP * (s - sinks); }
-  // Of a step's tokens up to the last row's position some row sees those from the first window on and the sinks, so all of
-  // them behind the first window step; in the steps before that (tokens that the sink steps show belong to them alone) and
-  // in it, a place that no row sees may hold anything, NaN included.
-  __device__ __forceinline__ bool edge(int32_t s) const { return s <= sinks; }
-  __device__ __forceinline__ bool seen(int32_t s, int32_t all_sinks, int32_t from, int32_t to) const {  // a token of from .. to
-    return s < sinks ? from < min(all_sinks, win0) : to >= lo || from < all_sinks;
-  }
-};
-
-template <int STEP>
-__device__ __forceinline__ Steps<STEP> cache_steps(int32_t plo, int32_t phi, int32_t cap, int32_t window, int32_t sinks) {
-  phi = min(phi, cap - 1);
-  if (phi < 0) return Steps<STEP>{0, 0, 0, 0};
-  const int32_t lo = max(0, max(plo, 0) - (window - 1));
-  const int32_t win0 = min(lo, phi + 1) & ~(STEP - 1);
-  const int32_t ns = (min(sinks, win0) + STEP - 1) / STEP;
-  return Steps<STEP>{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / STEP + 1 : 0)};
-}
-
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
 __device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
 
@@ -200,7 +171,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int32_t at = (j0 + 16 * half) >> a.page_shift;
-        if (j0 + 16 * half <= top) x.page[half] = table[at];  // (top is below the table's capacity)
+        if (steps.looked_up(a.sinks, j0 + 16 * half, top)) x.page[half] = table[at];  // (top is below the table's capacity)
       }
     }
     return x;
@@ -321,12 +292,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     for (int y = 0; y < 8; ++y) v[y] = x.v[y];
     if (jl > top || !x.held[0] || !x.held[1] || steps.edge(s)) {  // P is 0 there, V whatever the page holds
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
-        if (!steps.seen(s, a.sinks, x.j0 + 16 * half, x.j0 + 16 * half + 15)) vpow[half] = 1.f;  // (nor need its scale be one)
-#pragma unroll
       for (int y = 0; y < 8; ++y) {
         const int32_t j = x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3);
-        if (j > top || !x.held[y >> 2] || !steps.seen(s, a.sinks, j, j)) v[y] = VT{};
+        if (j > top || !x.held[y >> 2] || !steps.seen(a.sinks, j, j)) v[y] = VT{};
       }
     }
 #pragma unroll
@@ -520,7 +488,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int32_t j = steps.first(s) + 16 * group_of(u);
-      x.page[u] = s < s_end && j <= top ? table[(j >> a.page_shift) + zero] : -1;
+      x.page[u] = (s < s_end) & steps.looked_up(a.sinks, j, top) ? table[(j >> a.page_shift) + zero] : -1;
     }
     return x;
   };
@@ -553,7 +521,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       const int token = 16 * group_of(u) + slot_in;
       const int32_t j = steps.first(s) + token;
       float vpow = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
-      if (j > top || !x.held[u] || (steps.edge(s) && !steps.seen(s, a.sinks, j, j))) {  // anything may be there
+      if (j > top || !x.held[u] || (steps.edge(s) && !steps.seen(a.sinks, j, j))) {  // anything may be there
         x.k[u] = x.v[u] = uint4{0, 0, 0, 0};
         vpow = 1.f;
       }
