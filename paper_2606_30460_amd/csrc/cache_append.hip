@@ -171,12 +171,11 @@ __device__ __forceinline__ void rotate_q(const AppendArgs& a, int64_t item) {
   const int64_t row = item / UNITS;
   const int64_t t = row / a.heads_q;
   const int h = (int)(row - t * a.heads_q);
-  if (t >= a.total_new) return;
+  if (t >= a.total_new || (a.cu && t >= a.cu[a.d.num_seqs])) return;  // (behind the last sequence: not read)
   Unit x = load_unit<D>(a, a.q + t * a.q_stride + (int64_t)h * D, u, true);  // (under way while the position is looked up)
   int64_t pos;
   if (a.cu) {
     int32_t l = 0, r = a.d.num_seqs;  // cu[l] <= t < cu[r]
-    if (t >= a.cu[r]) return;         // a row behind the last sequence
     while (r - l > 1) {
       const int32_t mid = (l + r) >> 1;
       if (a.cu[mid] <= t) l = mid;
