@@ -44,7 +44,6 @@ struct CacheAttnArgs {
   int32_t page_shift;  // log2 of the page size
   int32_t window;
   int32_t sinks;
-  int32_t tiles;   // row tiles, all sequences
   int32_t splits;
   float scale_log2;
 };
@@ -868,7 +867,6 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   a.page_shift = __builtin_ctz((unsigned)desc->page_size);
   a.window = window;
   a.sinks = sinks;
-  a.tiles = (int32_t)c.tiles;
   a.splits = c.splits;
   a.scale_log2 = softmax_scale * 1.44269504088896340736f;
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
