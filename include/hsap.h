@@ -770,6 +770,7 @@ hsap_status hsap_window_attn_bwd(const hsap_attn_desc* desc, int32_t window, int
  *               NULL: one row for each sequence (total_new = num_seqs).
  * These arrays are read by the kernels, so a captured call follows their contents at each replay.  No entry point below
  * allocates or synchronises.
+ * A call that would take 2^32 threads (2^24 workgroups) or more is refused with HSAP_ERR_INVALID_ARG.
  * --------------------------------------------------------------------- */
 typedef struct {
   int32_t num_pages;    /* >= 1                                     */

@@ -33,6 +33,9 @@ HSAP_CACHE_HD int64_t cache_row(int64_t page, int32_t heads, int32_t head, int32
 // sequence whose base is not above it.
 HSAP_CACHE_HD int64_t item_base(int64_t cu, int64_t num, int64_t den, int64_t add, int64_t s) { return cu * num / den + add * s; }
 
+// Workgroups of 256 threads that a launch can have: the runtime counts its threads in 32 bits.
+constexpr int64_t kMaxBlocks256 = (int64_t(1) << 32) / 256 - 1;
+
 // e of a page's scale 2^e: the smallest exponent with amax <= 448 * 2^e, within [-100, 120].  448 = 1.75 * 2^8, so e is
 // amax's own exponent less 8, and one more where its significand is above 1.75.
 constexpr int kMinScaleExp = -100, kMaxScaleExp = 120;

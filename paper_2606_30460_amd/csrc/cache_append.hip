@@ -378,7 +378,7 @@ extern "C" hsap_status hsap_cache_append(const hsap_cache_desc* desc, const hsap
   const int64_t kv = cu_new ? (item_base(total_new, 1, desc->page_size, 2, desc->num_seqs)) * desc->heads_kv * 2
                             : ((int64_t)desc->num_seqs * desc->heads_kv * 2 * units + 255) / 256;
   const int64_t blocks = kv + (q ? (total_new * heads_q * units + 255) / 256 : 0);
-  if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens x heads");
+  if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens x heads");
   a.kv_blocks = (int32_t)kv;
   hipStream_t s = (hipStream_t)hip_stream;
   const dim3 grid((unsigned)blocks), block(256);

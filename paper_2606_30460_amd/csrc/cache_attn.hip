@@ -870,7 +870,7 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   a.splits = c.splits;
   a.scale_log2 = softmax_scale * 1.44269504088896340736f;
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
-  if (blocks > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
+  if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
   if (d == 128) launch_cache_attn<128>(a, c.rows, blocks, s);
   else launch_cache_attn<64>(a, c.rows, blocks, s);
