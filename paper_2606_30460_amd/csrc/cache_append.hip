@@ -300,9 +300,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   if (tid == 0) *scale = now;
 }
 
-hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c) {
-  if (!d || !c) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "cache descriptor is NULL");
-  if (d->num_pages < 1 || d->heads_kv < 1 || d->num_seqs < 0 || d->table_width < 1)
+hsap_status check_cache_desc(const hsap_cache_desc* d, bool pages) {
+  if (!d) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "cache descriptor is NULL");
+  if ((pages && d->num_pages < 1) || d->heads_kv < 1 || d->num_seqs < 0 || d->table_width < 1)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad cache: num_pages %d, heads_kv %d, num_seqs %d, table_width %d", d->num_pages,
               d->heads_kv, d->num_seqs, d->table_width);
   if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128)
@@ -311,6 +311,13 @@ hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c) {
     HSAP_FAIL(HSAP_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", d->head_dim);
   if ((int64_t)d->table_width * d->page_size > INT32_MAX)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "table_width %d x page_size %d beyond 2^31-1 positions", d->table_width, d->page_size);
+  return HSAP_OK;
+}
+
+hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c) {
+  const hsap_status st = check_cache_desc(d, true);
+  if (st != HSAP_OK) return st;
+  if (!c) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "cache descriptor is NULL");
   if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer in the cache");
   if (d->num_seqs > 0 && (!c->page_table || !c->seq_lens)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL page_table or seq_lens");

@@ -26,6 +26,7 @@
 
 namespace hsap {
 
+hsap_status check_cache_desc(const hsap_cache_desc* d, bool pages);
 hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c);
 
 struct CacheAttnArgs {
@@ -798,6 +799,13 @@ static int64_t cache_workspace(const CacheCut& c, int32_t heads_q, int64_t total
   return c.splits == 1 ? 0 : (int64_t)c.splits * total_q * heads_q * (head_dim + 1) * 4;
 }
 
+static hsap_status check_attn_rows(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q) {
+  if (heads_q < 1 || heads_q % d.heads_kv)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "heads_q=%d must be a positive multiple of heads_kv=%d", heads_q, d.heads_kv);
+  if (total_q < 0 || total_q > INT32_MAX / heads_q) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_q %lld", (long long)total_q);
+  return HSAP_OK;
+}
+
 template <int D>
 static void launch_cache_attn(const CacheAttnArgs& a, int rows, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
@@ -814,11 +822,7 @@ using namespace hsap;
 
 extern "C" int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
   clear_error();
-  if (!desc || heads_q < 1 || total_q < 0 || desc->heads_kv < 1 || heads_q % desc->heads_kv || desc->num_seqs < 0 ||
-      desc->table_width < 1 || (desc->head_dim != 64 && desc->head_dim != 128) || desc->page_size < 1) {
-    set_error("bad cache or head counts");
-    return -1;
-  }
+  if (check_cache_desc(desc, false) != HSAP_OK || check_attn_rows(*desc, heads_q, total_q) != HSAP_OK) return -1;
   const CacheCut c = cache_cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
   return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
 }
@@ -831,12 +835,10 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   hsap_status st = check_cache(desc, cache);
   if (st != HSAP_OK) return st;
   const int d = desc->head_dim;
-  if (heads_q < 1 || heads_q % desc->heads_kv)
-    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "heads_q=%d must be a positive multiple of heads_kv=%d", heads_q, desc->heads_kv);
+  if ((st = check_attn_rows(*desc, heads_q, total_q)) != HSAP_OK) return st;
   if (!(softmax_scale > 0.f) || softmax_scale > 1e30f) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
   if (window < 1) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "window %d < 1 (a query always sees itself)", window);
   if (sinks < 0) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "sinks %d < 0", sinks);
-  if (total_q < 0 || total_q * heads_q > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_q %lld", (long long)total_q);
   if (!cu_new && total_q != desc->num_seqs)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "without cu_new every sequence has one row: total_q %lld, num_seqs %d", (long long)total_q,
               desc->num_seqs);

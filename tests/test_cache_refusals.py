@@ -32,3 +32,15 @@ def test_attention_of_more_threads_than_a_launch_has():
     st = L.lib().hsap_cache_attn(ctypes.byref(_desc()), ctypes.byref(_bufs()), heads_q, 0.1, 10, 0, FAKE, 256, FAKE, total, FAKE,
                                  None, FAKE, 2 ** 60, None)
     assert st == L.HSAP_ERR_INVALID_ARG and "too many" in L.lib().hsap_last_error().decode()
+
+
+def test_workspace_of_what_the_call_refuses():
+    lib, heads_q, total = L.lib(), 4, 3
+    assert lib.hsap_cache_attn_workspace(ctypes.byref(_desc()), heads_q, total, 1) >= 0
+    for over in (dict(page_size=24), dict(page_size=256), dict(table_width=2 ** 28), dict(head_dim=96), dict(table_width=0)):
+        d = _desc(**over)
+        st = lib.hsap_cache_attn(ctypes.byref(d), ctypes.byref(_bufs()), heads_q, 0.1, 10, 0, FAKE, 256, None, total, FAKE, None, FAKE,
+                                 2 ** 60, None)
+        assert st != L.HSAP_OK, over
+        assert lib.hsap_cache_attn_workspace(ctypes.byref(d), heads_q, total, 1) == -1 and lib.hsap_last_error().decode(), over
+    assert lib.hsap_cache_attn_workspace(ctypes.byref(_desc()), heads_q, 2 ** 29, 0) == -1     # total_q x heads_q beyond 32 bits
