@@ -1,7 +1,9 @@
 // Device helpers of the window-attention kernels: document bounds of a wave's positions, the row of a position in
-// sharded order, and the direct-to-LDS transfer of a 64-row tile.  What is index arithmetic alone also builds for the host
-// (tests).
+// sharded order, and the direct-to-LDS transfer of a 64-row tile.  What comes before them, the choices of a call's kernels and
+// index arithmetic, also builds without HIP.
 #pragma once
+
+#include <algorithm>
 
 #include "hsap_internal.h"
 
@@ -20,23 +22,6 @@ HSAP_HD inline int32_t short_row_key(int32_t x, int32_t g0, int32_t lo, int32_t 
   return x < last ? x : last;
 }
 
-#if defined(__HIPCC__)
-
-// Most sink tokens per document that the backward takes: one workgroup holds them all (4 waves x 32 keys).
-constexpr int32_t kMaxBwdSinks = 128;
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-
-// Shard segments: local rows in pieces of consecutive positions, one (CONTIGUOUS) or two (ZIGZAG) per sequence of the
-// batch, each of geom.m rows.  Segment sg holds local rows sg * m .. sg * m + m - 1.
-__host__ __device__ inline int32_t segments_per_sequence(const Geom& g) { return g.layout == HSAP_LAYOUT_CONTIGUOUS ? 1 : 2; }
-
-// First position of segment sg of chunk x.
-__device__ __forceinline__ int32_t segment_start(const Geom& g, int32_t x, int32_t sg) {
-  return (int32_t)global_pos(g, x, (int64_t)sg * g.m);
-}
-
 // 32-row blocks of a workgroup's four waves: four, or fewer, each then taken by several waves that share its steps as
 // streams, so that a small grid has more and shorter workgroups.  `tiles`: workgroups that four blocks would give.  A split
 // pays as long as all its workgroups are resident at once: one per CU at head_dim 128, two at 64 (their LDS).
@@ -50,11 +35,64 @@ inline int window_row_blocks(int64_t tiles, int head_dim) {
   const int64_t resident = kComputeUnits * (head_dim == 64 ? 2 : 1);
   return 4 * tiles <= resident ? 1 : 2 * tiles <= resident ? 2 : 4;
 }
-inline int64_t window_q_tiles(const Geom& g, int heads_q) { return g.n / g.m * ((g.m + 127) / 128) * heads_q; }
-// (of the chunks' keys, those that the shard's windows reach)
+// Blocks of the kernels by query tiles (forward, dQ): two or four (one block in four streams gains nothing over two in two).
+inline int window_query_blocks(const Geom& g, int heads_q, int head_dim) {
+  return window_row_blocks(g.n / g.m * ((g.m + 127) / 128) * heads_q, head_dim) < 4 ? 2 : 4;
+}
+// Key tiles of dK/dV: of the chunks' keys, those that the shard's windows reach.
 inline int64_t window_key_tiles(const Geom& g, int heads_kv, int64_t window) {
   const int64_t keys = g.n / g.m * (g.m + window);
   return (keys < g.N ? keys : g.N) / 128 * heads_kv;
+}
+
+// Queries of a sink chunk: a workgroup per CU over all chunks and K/V heads, at least 256 (8192 rows x 8 heads: chunks of 256
+// 33 us, of 1024 177 us; 16384 rows x 16 heads: 256 58 us, 1024 26 us).
+inline int32_t sink_chunk(const hsap_attn_desc* d, const Geom& g) {
+  int32_t c = 256;
+  while (c < 4096 && g.n * d->heads_kv > c * kComputeUnits) c *= 2;
+  return c;
+}
+
+// Sink chunks per segment; 0 where no chunk begins inside a document that has a sink further than a window from its queries.
+inline int32_t sink_chunks(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
+  if (sinks == 0 || window >= g.Ns) return 0;
+  const int32_t c = sink_chunk(d, g), per = (int32_t)((g.m + c - 1) / c);
+  return per == 1 && g.P == 1 && g.layout == HSAP_LAYOUT_CONTIGUOUS ? 0 : per;
+}
+
+// Up to so many chunks per segment the dK/dV kernel adds a document's partials itself.
+constexpr int32_t kDirectChunks = 8;
+
+// Workgroups that share a key tile's heads: while all stay resident at once and each keeps at least eight steps, its parts
+// within 64 MiB.
+inline int32_t head_split(const hsap_attn_desc* d, const Geom& g, int32_t window) {
+  const int grp = d->heads_q / d->heads_kv;
+  const int64_t tiles = window_key_tiles(g, d->heads_kv, window);
+  const int blocks = window_row_blocks(tiles, d->head_dim);
+  if (blocks == 4 || grp == 1) return 1;
+  const int64_t resident = kComputeUnits * (d->head_dim == 64 ? 2 : 1);
+  const int64_t per_head = (std::min<int64_t>(window, g.m) + 32 * blocks) / 32;  // 32-query steps of one head
+  const int64_t steps = per_head * grp * blocks / 4;                             // a stream's
+  const int64_t bytes = (int64_t)g.P * g.n * d->heads_kv * 2 * d->head_dim * 4;
+  const int64_t most = std::min<int64_t>(std::min<int64_t>(grp, steps / 8),
+                                         std::min(resident / std::max<int64_t>(1, tiles * 4 / blocks), (int64_t(64) << 20) / bytes));
+  return (int32_t)std::max<int64_t>(1, most);
+}
+
+#if defined(__HIPCC__)
+// Shard segments: local rows in pieces of consecutive positions, one (CONTIGUOUS) or two (ZIGZAG) per sequence of the
+// batch, each of geom.m rows.  Segment sg holds local rows sg * m .. sg * m + m - 1.
+__host__ __device__ inline int32_t segments_per_sequence(const Geom& g) { return g.layout == HSAP_LAYOUT_CONTIGUOUS ? 1 : 2; }
+
+// Most sink tokens per document that the backward takes: one workgroup holds them all (4 waves x 32 keys).
+constexpr int32_t kMaxBwdSinks = 128;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// First position of segment sg of chunk x.
+__device__ __forceinline__ int32_t segment_start(const Geom& g, int32_t x, int32_t sg) {
+  return (int32_t)global_pos(g, x, (int64_t)sg * g.m);
 }
 
 // Storage of keys in sharded order as runs of consecutive positions: [lo, hi) are the positions whose row is

@@ -720,41 +720,7 @@ static hsap_status check_launch_window(const char* what) {
   return HSAP_OK;
 }
 
-// Queries of a sink chunk: a workgroup per CU over all chunks and K/V heads, at least 256 (8192 rows x 8 heads: chunks of 256
-// 33 us, of 1024 177 us; 16384 rows x 16 heads: 256 58 us, 1024 26 us).
-static int32_t sink_chunk(const hsap_attn_desc* d, const Geom& g) {
-  int32_t c = 256;
-  while (c < 4096 && g.n * d->heads_kv > c * kComputeUnits) c *= 2;
-  return c;
-}
-
-// Sink chunks per segment; 0 where no chunk begins inside a document that has a sink further than a window from its queries.
-static int32_t sink_chunks(const hsap_attn_desc* d, const Geom& g, int32_t window, int32_t sinks) {
-  if (sinks == 0 || window >= g.Ns) return 0;
-  const int32_t c = sink_chunk(d, g), per = (int32_t)((g.m + c - 1) / c);
-  return per == 1 && g.P == 1 && g.layout == HSAP_LAYOUT_CONTIGUOUS ? 0 : per;
-}
-
-// Up to so many chunks per segment the dK/dV kernel adds a document's partials itself.
-constexpr int32_t kDirectChunks = 8;
-
 static int64_t delta_bytes(const hsap_attn_desc* d, const Geom& g) { return (4 * g.n * d->heads_q + 255) / 256 * 256; }
-
-// Workgroups that share a key tile's heads: while all stay resident at once and each keeps at least eight steps, its parts
-// within 64 MiB.
-static int32_t head_split(const hsap_attn_desc* d, const Geom& g, int32_t window) {
-  const int grp = d->heads_q / d->heads_kv;
-  const int64_t tiles = window_key_tiles(g, d->heads_kv, window);
-  const int blocks = window_row_blocks(tiles, d->head_dim);
-  if (blocks == 4 || grp == 1) return 1;
-  const int64_t resident = kComputeUnits * (d->head_dim == 64 ? 2 : 1);
-  const int64_t per_head = (std::min<int64_t>(window, g.m) + 32 * blocks) / 32;  // 32-query steps of one head
-  const int64_t steps = per_head * grp * blocks / 4;                             // a stream's
-  const int64_t bytes = (int64_t)g.P * g.n * d->heads_kv * 2 * d->head_dim * 4;
-  const int64_t most = std::min<int64_t>(std::min<int64_t>(grp, steps / 8),
-                                         std::min(resident / std::max<int64_t>(1, tiles * 4 / blocks), (int64_t(64) << 20) / bytes));
-  return (int32_t)std::max<int64_t>(1, most);
-}
 
 static int64_t heads_bytes(const hsap_attn_desc* d, const Geom& g, int32_t window) {
   const int64_t split = head_split(d, g, window);
@@ -787,7 +753,7 @@ static hsap_status launch_dkv(WindowBwdArgs& a, hipStream_t s) {
 
 template <int D>
 static hsap_status launch_window_bwd(WindowBwdArgs& a, hipStream_t s) {
-  hsap_status st = window_row_blocks(window_q_tiles(a.geom, a.hq), D) < 4 ? launch_dq<D, 2, 2>(a, s) : launch_dq<D, 4, 1>(a, s);
+  hsap_status st = window_query_blocks(a.geom, a.hq, D) == 2 ? launch_dq<D, 2, 2>(a, s) : launch_dq<D, 4, 1>(a, s);
   if (st != HSAP_OK) return st;
   if (a.chunks) {
     // as many key blocks as there are sinks; the other waves are streams over the queries

@@ -328,8 +328,7 @@ static hsap_status launch_window_fwd(WindowFwdArgs& a, hipStream_t stream) {
 
 template <int D>
 static hsap_status dispatch_window_fwd(WindowFwdArgs& a, hipStream_t stream) {
-  // (one block in four streams gains nothing over two in two)
-  if (window_row_blocks(window_q_tiles(a.geom, a.hq), D) < 4) return launch_window_fwd<D, 2, 2>(a, stream);
+  if (window_query_blocks(a.geom, a.hq, D) == 2) return launch_window_fwd<D, 2, 2>(a, stream);
   return launch_window_fwd<D, 4, 1>(a, stream);
 }
 

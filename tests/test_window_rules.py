@@ -1,27 +1,14 @@
 """Index arithmetic of the window kernels (csrc/window.h, built for the host)."""
-import ctypes
-import os
-import subprocess
-
 import numpy as np
 import pytest
 
 import oracle
-
-ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+import _window_host as H
 
 
 @pytest.fixture(scope="module")
-def host(tmp_path_factory):
-    src = tmp_path_factory.mktemp("window_h") / "window_h.cpp"
-    src.write_text('#include "%s"\nusing namespace hsap;\nextern "C" {\n'
-                   "int32_t short_row(int32_t x, int32_t g0, int32_t lo, int32_t f, int32_t fe, int32_t last) {\n"
-                   "  return short_row_key(x, g0, lo, f, fe, last); }\n}\n"
-                   % os.path.join(ROOT, "paper_2606_30460_amd", "csrc", "window.h"))
-    out = str(src.with_suffix(".so"))
-    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover=all",
-                    "-static-libubsan", str(src), "-o", out], check=True)
-    return ctypes.CDLL(out)
+def host():
+    return H.lib()
 
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (5, 0), (7, 9), (20, 2), (31, 0), (31, 40), (100, 4)])
