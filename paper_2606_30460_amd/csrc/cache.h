@@ -1,10 +1,12 @@
 // Index arithmetic and token ranges of the paged K/V cache shared by its kernels and, built for the host, by the tests.
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 
+#include "hsap_internal.h"
+
 #if defined(__HIPCC__)
-#include <hip/hip_runtime.h>
 #define HSAP_CACHE_HD __host__ __device__ __forceinline__
 #else
 #define HSAP_CACHE_HD inline
@@ -76,6 +78,62 @@ HSAP_CACHE_HD Steps<STEP> cache_steps(int32_t plo, int32_t phi, int32_t cap, int
   const int32_t win0 = (lo <= phi ? lo : phi + 1) & ~(STEP - 1);
   const int32_t ns = ((sinks < win0 ? sinks : win0) + STEP - 1) / STEP;
   return Steps<STEP>{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / STEP + 1 : 0)};
+}
+
+constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
+constexpr int kMaxSplits = 128;  // of a row tile's tokens
+
+// How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip, each of at least 256 tokens.
+struct CacheCut {
+  int rows;  // of a tile: 16 or 32 (cache_attn_kernel), kChunkRows (cache_chunk_kernel)
+  bool once;  // cache_attn_kernel's ONCE
+  int64_t tiles;
+  int32_t splits;
+};
+
+// Workgroups of cache_attn_kernel to aim at: twice what the chip holds at once (64 sequences of 8k tokens: 129 us with 512,
+// 128 with 1024, 127 with 2048).  At most 128 splits (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits
+// 24.5, 128 19.4, 256 22.0: more partials to join).
+constexpr int64_t kCacheGrid = 1024;
+
+// Two 16-row blocks where the sequences have more than 16 rows (28 x 50 rows x 8 of 64 heads of 128, us: 28, one block 34,
+// four 48).  128 rows, where the sequences have more than 64 and the grid can be filled: at head_dim 64 always (us, 32 -> 128
+// rows: 3 x 700 x 4 over 12000 tokens 44 -> 38; 4 x 300 x 4 over 6000 50 -> 48; 400 x 5 over 200000 445 -> 344), at 128
+// over many tokens, since it needs splits sooner and their partials are twice as large (2048 x 8 over 30000 787 -> 665,
+// 512 x 4 over 16000 217 -> 188, but 512 x 4, twice, over 8000 103 -> 116 and 32 x 8, 64 times, over 3125 94 -> 119).
+constexpr int64_t kChunkGrid = 2 * kComputeUnits, kChunkSplits = 16, kChunkTokens128 = 12000;
+
+inline CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
+  CacheCut c;
+  const int64_t group = heads_q / d.heads_kv;
+  const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
+  // workgroups of 128 rows without splits (c.tiles counts a tile more per sequence, which does nothing)
+  const int64_t full = (total_q * group + kChunkRows - 1) / kChunkRows * d.heads_kv;
+  const bool chunk = rows > 64 && full * std::min(most, kChunkSplits) >= kChunkGrid && (d.head_dim == 64 || tokens >= kChunkTokens128);
+  c.rows = chunk ? kChunkRows : rows > 16 ? 32 : 16;
+  c.once = one_each && c.rows == 16 && 2 * d.num_seqs * tokens * d.heads_kv * d.head_dim > (int64_t(256) << 20);
+  c.tiles = one_each ? (int64_t)d.num_seqs * ((group + c.rows - 1) / c.rows) : item_base(total_q, group, c.rows, 1, d.num_seqs);
+  if (!chunk) {
+    c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
+    return c;
+  }
+  // Splits that make whole rounds of the chip's 512 workgroups, in ns: a round's steps of 64 tokens (2.2 us, head_dim 64 1.5)
+  // and its beginning and end, a join and the partials written and read (2048 x 8 rows over 30000 tokens: one split 1086,
+  // three 760, two 665).
+  c.splits = 1;
+  int64_t least = INT64_MAX;
+  for (int64_t s = 1; s <= std::min(most, kChunkSplits); ++s) {
+    const int64_t rounds = (full * s + kChunkGrid - 1) / kChunkGrid;
+    const int64_t steps = (tokens + 64 * s - 1) / (64 * s);
+    const int64_t ns = rounds * (steps * (d.head_dim == 64 ? 1500 : 2200) + 6000) +
+                       (s > 1 ? 4000 + total_q * heads_q * d.head_dim * 8 * s / 4000 : 0);
+    if (ns < least) {
+      least = ns;
+      c.splits = (int32_t)s;
+    }
+  }
+  return c;
 }
 
 }  // namespace hsap

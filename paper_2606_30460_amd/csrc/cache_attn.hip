@@ -52,8 +52,6 @@ struct CacheAttnArgs {
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
 __device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
 
-constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // four e4m3 codes times a power of two to bf16 (exact within bf16's range)
@@ -690,7 +688,6 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a) {
 
 // More splits: a workgroup per row.  Every wave forms the weights of all splits (up to 128, two to a lane); the
 // 256 / (D / 4) groups of lanes then take every so manieth split and are added up in LDS.
-constexpr int kMaxSplits = 128;
 template <int D>
 __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
   constexpr float NEG_INF = -__builtin_inff();
@@ -744,57 +741,6 @@ __global__ __launch_bounds__(256) void cache_join_many_kernel(CacheAttnArgs a) {
     a.lse[(row - tok * a.heads_q) * a.total_q + tok] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994530942f : NEG_INF;
 }
 
-// How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip, each of at least 256 tokens.
-struct CacheCut {
-  int rows;  // of a tile: 16 or 32 (cache_attn_kernel), kChunkRows (cache_chunk_kernel)
-  int64_t tiles;
-  int32_t splits;
-};
-
-// Workgroups of cache_attn_kernel to aim at: twice what the chip holds at once (64 sequences of 8k tokens: 129 us with 512,
-// 128 with 1024, 127 with 2048).  At most 128 splits (one sequence of 128k tokens, two K/V heads, pass in us: 64 splits
-// 24.5, 128 19.4, 256 22.0: more partials to join).
-constexpr int64_t kCacheGrid = 1024;
-
-// Two 16-row blocks where the sequences have more than 16 rows (28 x 50 rows x 8 of 64 heads of 128, us: 28, one block 34,
-// four 48).  128 rows, where the sequences have more than 64 and the grid can be filled: at head_dim 64 always (us, 32 -> 128
-// rows: 3 x 700 x 4 over 12000 tokens 44 -> 38; 4 x 300 x 4 over 6000 50 -> 48; 400 x 5 over 200000 445 -> 344), at 128
-// over many tokens, since it needs splits sooner and their partials are twice as large (2048 x 8 over 30000 787 -> 665,
-// 512 x 4 over 16000 217 -> 188, but 512 x 4, twice, over 8000 103 -> 116 and 32 x 8, 64 times, over 3125 94 -> 119).
-constexpr int64_t kChunkGrid = 2 * kComputeUnits, kChunkSplits = 16, kChunkTokens128 = 12000;
-
-static CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
-  CacheCut c;
-  const int64_t group = heads_q / d.heads_kv;
-  const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
-  // workgroups of 128 rows without splits (c.tiles counts a tile more per sequence, which does nothing)
-  const int64_t full = (total_q * group + kChunkRows - 1) / kChunkRows * d.heads_kv;
-  const bool chunk = rows > 64 && full * std::min(most, kChunkSplits) >= kChunkGrid && (d.head_dim == 64 || tokens >= kChunkTokens128);
-  c.rows = chunk ? kChunkRows : rows > 16 ? 32 : 16;
-  c.tiles = one_each ? (int64_t)d.num_seqs * ((group + c.rows - 1) / c.rows) : item_base(total_q, group, c.rows, 1, d.num_seqs);
-  if (!chunk) {
-    c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
-    return c;
-  }
-  // Splits that make whole rounds of the chip's 512 workgroups, in ns: a round's steps of 64 tokens (2.2 us, head_dim 64 1.5)
-  // and its beginning and end, a join and the partials written and read (2048 x 8 rows over 30000 tokens: one split 1086,
-  // three 760, two 665).
-  c.splits = 1;
-  int64_t least = INT64_MAX;
-  for (int64_t s = 1; s <= std::min(most, kChunkSplits); ++s) {
-    const int64_t rounds = (full * s + kChunkGrid - 1) / kChunkGrid;
-    const int64_t steps = (tokens + 64 * s - 1) / (64 * s);
-    const int64_t ns = rounds * (steps * (d.head_dim == 64 ? 1500 : 2200) + 6000) +
-                       (s > 1 ? 4000 + total_q * heads_q * d.head_dim * 8 * s / 4000 : 0);
-    if (ns < least) {
-      least = ns;
-      c.splits = (int32_t)s;
-    }
-  }
-  return c;
-}
-
 static int64_t cache_workspace(const CacheCut& c, int32_t heads_q, int64_t total_q, int head_dim) {
   return c.splits == 1 ? 0 : (int64_t)c.splits * total_q * heads_q * (head_dim + 1) * 4;
 }
@@ -807,12 +753,11 @@ static hsap_status check_attn_rows(const hsap_cache_desc& d, int32_t heads_q, in
 }
 
 template <int D>
-static void launch_cache_attn(const CacheAttnArgs& a, int rows, int64_t blocks, hipStream_t s) {
+static void launch_cache_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
-  const int64_t bytes = 2 * (int64_t)a.d.num_seqs * a.d.table_width * a.d.page_size * a.d.heads_kv * D;
-  if (rows == kChunkRows) hipLaunchKernelGGL(cache_chunk_kernel<D>, grid, block, 0, s, a);
-  else if (rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
-  else if (!a.cu && bytes > (int64_t(256) << 20)) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
+  if (c.rows == kChunkRows) hipLaunchKernelGGL(cache_chunk_kernel<D>, grid, block, 0, s, a);
+  else if (c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
+  else if (c.once) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false>), grid, block, 0, s, a);
 }
 
@@ -874,8 +819,8 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
-  if (d == 128) launch_cache_attn<128>(a, c.rows, blocks, s);
-  else launch_cache_attn<64>(a, c.rows, blocks, s);
+  if (d == 128) launch_cache_attn<128>(a, c, blocks, s);
+  else launch_cache_attn<64>(a, c, blocks, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
   if (c.splits > 1) {
