@@ -807,7 +807,7 @@ typedef struct {
  * the tokens it holds (a token overwritten at its position still counts until the page is begun anew).  Codes are
  * e4m3 of value / scale, fp32 rounded to nearest even, once.  When a new token raises a page's scale, the codes of
  * its older tokens are encoded for the new one.  NaN becomes the NaN code, an infinity saturates at 448 * scale;
- * neither moves the scale.
+ * neither moves the scale.  (Values from 1.9375 * 2^127 on round to 256 * 2^120, which fp32 does not hold.)
  * A token at a position below 0, at or behind cos_sin_rows (rot_dim > 0) is skipped (nothing of it written); at or
  * behind table_width * page_size or on no page it is not cached (its k_out and q_out rows are written).
  * One launch on `stream`.
@@ -834,8 +834,8 @@ int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, 
  *   lse_out     device fp32 [heads_q, total_q], or NULL.
  *   workspace   device, 16-byte aligned, workspace_bytes >= hsap_cache_attn_workspace; contents ignored.  Calls that
  *               overlap in time need workspaces of their own.
- * A row that sees no token (an idle slot, position below 0) gets O = 0, LSE = -inf.  What the cache holds at positions no
- * row sees is not used, whatever it is.  q and the cached values a row sees are finite.
+ * No output overlaps an input.  A row that sees no token (an idle slot, position below 0) gets O = 0, LSE = -inf.  What
+ * the cache holds at positions no row sees is not used, whatever it is.  q and the cached values a row sees are finite.
  * One or two launches on `stream`.
  */
 hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,

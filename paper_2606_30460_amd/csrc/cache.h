@@ -103,6 +103,9 @@ constexpr int64_t kCacheGrid = 1024;
 // 512 x 4 over 16000 217 -> 188, but 512 x 4, twice, over 8000 103 -> 116 and 32 x 8, 64 times, over 3125 94 -> 119).
 constexpr int64_t kChunkGrid = 2 * kComputeUnits, kChunkSplits = 16, kChunkTokens128 = 12000;
 
+// `tokens` is the table's capacity: the lengths are the device's, and the window is not looked at, so that a workspace is
+// enough for every window.  A table much wider than its sequences, or a window far below them, gives splits without work (one
+// token, window 1024, table of 131072: 94 of 128).
 inline CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
   const int64_t group = heads_q / d.heads_kv;

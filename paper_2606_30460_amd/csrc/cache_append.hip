@@ -222,6 +222,8 @@ __global__ __launch_bounds__(256) void cache_append_one_kernel(AppendArgs a) {
   for (int o = 1; o < UNITS; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
   float inv, ratio;
   const float now = page_scale(amax, slot > 0, old, inv, ratio);
+  // (token after token: 64 new tokens that raise the scales of pages of 16, 64, 128 take 15, 33, 58 us, of none 10, event to
+  // event)
   if (ratio != 1.f)
     for (int32_t t = 0; t < slot; ++t) recode16(codes + t * D + 16 * u, ratio);
   store_codes<D>(a, codes + slot * D, u, !is_v, x, inv);

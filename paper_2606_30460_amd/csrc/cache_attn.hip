@@ -7,7 +7,7 @@
 // tiles of 16 MT, one workgroup per (row tile, K/V head, split of the tile's tokens), a running maximum and sum per
 // wave, the waves' results joined in LDS, the splits' by a second launch over fp32 partials.  64 sequences of up to 8192
 // tokens, 32 heads over 8 of 128: 115 us for the codes (5.5 TB/s; a large sum reads at 6.0) and 4.5 for the join.  One of
-// 131072 tokens, 16 heads over 2: 15 and 4 us, a chain of table, codes, sixteen steps and joins.
+// 131072 tokens, 16 heads over 2: 16 and 4 us, a chain of table, codes, eight or nine steps per wave and joins.
 //
 // A wave takes 32 tokens at a time (its workgroup's four waves take turns), with the next ones' codes in flight in
 // registers: no LDS on the way.  S^T = K Q^T by 16x16x32 products, tokens as rows: lane l holds row l % 16 of K and
@@ -417,8 +417,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
 // takes 128 rows, a wave 32 of them, and every step's 64 tokens are decoded once for all: codes to registers a step ahead,
 // from there as bf16 (which e4m3 fits exactly; V times its scale's power of two) into the tiles of the window kernels, and
 // 32x32x16 products S^T = K Q^T, O^T += V^T P^T with V^T by transpose reads.  P is rounded to bf16 for the second product,
-// as in the window kernels.  2048 rows x 8 heads over 30000 tokens, head_dim 128: 665 us, 730 TFLOP/s (a step's products,
-// exponentials and decoding add up in a wave: matrix cores 0.33 busy).  head_dim 64: three workgroups per CU (185 -> 167 us).
+// as in the window kernels.  2048 rows x 8 heads over 30000 tokens, head_dim 128: 680 us, 765 TFLOP/s (a step's products,
+// exponentials and decoding add up in a wave: matrix cores 0.31 busy).  head_dim 64: three workgroups per CU (185 -> 167 us).
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
   constexpr int KB = 64, CPR = D / 8, TILE = KB * D, ROWS = kChunkRows, U = D / 64;  // U: runs of 16 codes per thread

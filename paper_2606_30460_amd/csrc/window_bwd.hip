@@ -10,9 +10,9 @@
 // at most, summed in fp32), each gradient once, at the end.
 //
 // Bound by LDS reads, products and exponentials following one another in a wave.  16384 of 65536 tokens, 16 heads over 16 of
-// 128, window 2048: dQ 420 us (0.75 of the library product's rate, counting what is executed), dK/dV 663 (0.64), sinks 35.
-// 8192 tokens, 32 heads over 8, window 1024: 215, 283, 32.  Three times 1999 tokens, 6 heads over 2 of 64, window 200: 21,
-// 20, 12, each the longest chain of its grid.
+// 128, window 2048: dQ 423 us (0.75 of the library product's rate, counting what is executed), dK/dV 678 (0.63), sinks 36.
+// 8192 tokens, 32 heads over 8, window 1024: 211, 270, 35.  Three times 1999 tokens, 6 heads over 2 of 64, window 200: 20,
+// 19, 12, each the longest chain of its grid.
 //
 // Two to five launches:
 //   dQ       one workgroup per (128-row q-tile, query head), over the tile's keys as in the forward; delta first

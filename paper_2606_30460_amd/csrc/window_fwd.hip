@@ -18,7 +18,7 @@
 // Bound by the products and, beside them, the softmax's vector work (per 64-key step and wave, head_dim 128: 32 products,
 // 32 exponentials, 115 other vector instructions; with two waves per SIMD they come close to a sum).  65536 tokens,
 // 16 heads of 128, window 4096: 2080 us, 1014 TFLOP/s (library product 1314).  4096 of 32768 tokens, 32 heads, window 1024:
-// 95 us, where a workgroup's beginning and end are 8 of its 47 us.  2048 tokens, 4 heads of 64: 9.8 us, latency alone.
+// 95 to 98 us, where a workgroup's beginning and end are 8 of its 47 us.  2048 tokens, 4 heads of 64: 9.8 us, latency alone.
 #include <algorithm>
 #include <type_traits>
 
