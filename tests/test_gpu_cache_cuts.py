@@ -108,3 +108,38 @@ def test_small_row_tiles_in_few_splits(d):
         c = _cut(p, 64, int(new.sum()), False)
         assert c.rows == rows and 1 < c.splits <= 8, c
         _check_attn(lens, new, 16, 64, 8, d, window=120, sinks=4, seed=most, pages=p, pad=1)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_pages_beyond_32_bits(one):
+    # the same sequences in the last pages of a cache of more than 2^32 codes: the bits of a small cache's
+    size, hkv, d, hq = 64, 8, 128, 16
+    lens, new = np.array([300, 77, 64]), np.ones(3, int) if one else np.array([40, 1, 17])
+    p = Pages(lens, size, hkv, d, seed=1).fill(lens - new)
+    small = p.device(lens)
+    pages, few = 2 ** 32 // (hkv * size * d) + 100, len(p.codes["k"])
+    t = {}
+    for x in "kv":
+        t[x + "_codes"] = torch.zeros((pages, hkv, size, d), dtype=torch.uint8, device="cuda")
+        t[x + "_scale"] = torch.zeros((pages, hkv), device="cuda")
+        t[x + "_codes"][pages - few:] = getattr(small, x + "_codes")
+        t[x + "_scale"][pages - few:] = getattr(small, x + "_scale")
+    large = L.KVCache(t["k_codes"], t["v_codes"], t["k_scale"], t["v_scale"], small.page_table + (pages - few), small.seq_lens)
+    total = int(new.sum())
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(total, h, d, generator=g).to(torch.bfloat16).cuda() for h in (hq, hkv, hkv))
+    cu = None if one else torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).cuda()
+    got = []
+    for cache in (small, large):
+        o = torch.empty_like(q)
+        ws = torch.empty(L.cache_attn_workspace(cache, hq, total), dtype=torch.uint8, device="cuda")
+        L.cache_append(cache, k, v, cu)
+        L.cache_attn(cache, hq, 0.1, q, cu, o, None, ws)
+        torch.cuda.synchronize()
+        got.append(o)
+    assert bool(torch.isfinite(got[0]).all()) and torch.equal(got[0], got[1])
+    for x in "kv":
+        assert torch.equal(getattr(large, x + "_codes")[pages - few:], getattr(small, x + "_codes"))
+        a, b = getattr(large, x + "_scale")[pages - few:], getattr(small, x + "_scale")
+        assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+        assert not bool(getattr(large, x + "_codes")[:pages - few].any()) and not bool(getattr(large, x + "_scale")[:pages - few].any())

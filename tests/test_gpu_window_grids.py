@@ -7,6 +7,7 @@ import torch
 
 import oracle
 from _window_host import Choice, choice
+from paper_2606_30460_amd import _lib as L
 from test_gpu_window import MIX, Problem, _cu
 
 pytestmark = pytest.mark.gpu
@@ -153,3 +154,30 @@ def test_same_bits_again_and_replayed():
                 assert torch.equal(first[x], cap[x]), (x, turn)
             p.backward(first)                       # eager work between the replays
             torch.cuda.synchronize()
+
+
+def test_offsets_beyond_32_bits():
+    # 70000 rows x 256 heads x 128: q, o and the gradients' last rows lie behind 2^31 elements (and 2^32 bytes)
+    n, hq, hkv, d, last, window, sinks = 70000, 256, 2, 128, 90, 40, 3
+    assert (n - last) * hq * d > 2 ** 31
+    small = Problem([0, last], last, window, sinks, hq=hq, hkv=hkv, d=d, seed=2)
+    cu = np.array([0, n - last, n], np.int32)
+    p = Problem.__new__(Problem)
+    p.__dict__.update(small.__dict__)
+    p.desc = L.attn_desc(L.shard_desc(n, 1, "contiguous", 0, 1, 1), hq, hkv, d, small.scale)
+    p.n, p.cu_dev = n, torch.from_numpy(cu).cuda()
+    for x, t in small.dev.items():
+        shape = (1, n, hkv, d) if x in "kv" else (n, hq, d)
+        p.dev = dict(p.dev) if p.dev is small.dev else p.dev
+        p.dev[x] = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+        p.dev[x].view(n, -1, d)[n - last:] = t.view(last, -1, d)
+    out = p.outputs()
+    p.forward(out)
+    p.backward(out)
+    torch.cuda.synchronize()
+    ref, _, _ = small.oracle()
+    for name in ("o", "dq", "dk", "dv"):
+        got = out[name].view(n, -1, d)[n - last:].float().cpu().numpy()
+        assert (np.abs(got - ref[name]) <= ref[name + "_tol"] + 1e-9).all(), name
+    assert (np.abs(out["lse"][:, n - last:].cpu().numpy() - ref["lse"]) <= ref["lse_tol"]).all()
+    assert not bool(out["o"][:n - last].any()) and not bool(out["dq"][:n - last].any())   # zeros elsewhere
