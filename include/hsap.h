@@ -844,6 +844,187 @@ hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache
                             void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Trees of drafted tokens -- a step verifies several guesses of what comes next at once: the last tokens of a sequence
+ * (cu_new, seq_lens as above) are drafted ones, each following another or the tokens before them.  They lie in the cache in
+ * any order that puts a token behind the one that it follows; a mask names those that it sees.  (An extension beyond the
+ * paper.)
+ * --------------------------------------------------------------------- */
+
+/*
+ * hsap_tree_masks -- masks and positions of drafted tokens, once for all layers of a step.
+ *   seq_lens, cu_new, total_new  as in hsap_cache: a sequence's count drafted tokens stand at places seq_lens[s] - count .. of it.
+ *   parents     device int32 [total_new]: the number, among its sequence's drafted tokens, of the one that a token follows;
+ *               below 0, or not below its own number: none of them.  Not read without cu_new.
+ *   mask_words  64-bit words of a mask, 1 to HSAP_MAX_MASK_WORDS: for up to 64 * mask_words drafted tokens a sequence.
+ *   mask        device uint64 [total_new, mask_words], 8-byte aligned: bit j % 64 of word j / 64 of a token is set for itself
+ *               and the drafted tokens that it follows, directly or not.
+ *   positions   device int32 [total_new]: seq_lens[s] - count + the number of drafted tokens that it follows.
+ * A drafted token behind the first 64 * mask_words of its sequence gets an empty mask and position -1.  One launch on
+ * `stream`.
+ */
+#define HSAP_MAX_MASK_WORDS 16
+hsap_status hsap_tree_masks(int32_t num_seqs, const int32_t* seq_lens, const int32_t* cu_new, int64_t total_new,
+                            const int32_t* parents, int32_t mask_words, uint64_t* mask, int32_t* positions, void* hip_stream);
+
+/* Bytes of device workspace hsap_cache_tree_attn needs for any window (host); -1 for invalid arguments.  As
+ * hsap_cache_attn_workspace: a call of fewer rows may need more. */
+int64_t hsap_cache_tree_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each);
+
+/*
+ * hsap_cache_tree_attn -- attention of drafted tokens over the cache.  Row t of sequence s, at position p = positions[t],
+ * sees
+ *   the tokens at places j < seq_lens[s] - count with p - j < window or j < sinks, and
+ *   drafted token x (place seq_lens[s] - count + x, position y) where bit x of its mask is set, with p - y < window or
+ *   y < sinks.
+ *   mask, mask_words  device uint64 [total_q, mask_words], 8-byte aligned: any bits (of hsap_tree_masks, or a mask of the
+ *               caller's own).
+ *   positions   device int32 [total_q].  Below 0: the row sees nothing.  Those of drafted tokens that a mask names are not
+ *               below 0.
+ *   window      2^31 - 1: ends nothing.
+ *   everything else  as in hsap_cache_attn (workspace_bytes >= hsap_cache_tree_attn_workspace).
+ * A row that sees no token gets O = 0, LSE = -inf.  What the cache holds where no row sees it is not used, whatever it
+ * is; the page table's entries of the drafted tokens' pages are looked at whether a mask names one of them or not.  q, the
+ * cached values that a row sees and those of drafted tokens that its mask names are finite.  One or two launches on `stream`.
+ */
+hsap_status hsap_cache_tree_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
+                                 int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
+                                 int64_t total_q, const uint64_t* mask, int32_t mask_words, const int32_t* positions, void* o_out,
+                                 float* lse_out, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * hsap_cache_compact -- kept tokens of every sequence moved together: the accepted ones of a tree, or what an eviction
+ * leaves.  The first first[s] tokens of sequence s stay where they are; token i of its list, at place keep[cu_keep[s] + i],
+ * goes to place first[s] + i.
+ *   keep        device int32 [total_keep]: a sequence's places, ascending, keep[cu_keep[s] + i] >= first[s] + i (else what
+ *               the moved places hold is undefined).  A place that lies in no page gives zeros.
+ *   cu_keep     device int32 [num_seqs + 1], 0 = cu[0] <= ... <= cu[num_seqs] <= total_keep.
+ *   first       device int32 [num_seqs], or NULL: 0 (as values below 0).
+ *   dst_table   device int32 [num_seqs, table_width]: pages that the tokens go to, every one of them in one place of the table
+ *               and none of them holding a token to be moved; faster for long lists.  NULL: in place, in the pages of
+ *               page_table, which then are the sequence's own from place first[s] on.
+ *   new_lens    device int32 [num_seqs], or NULL: receives first[s] + the length of its list.  May be cache->seq_lens, which
+ *               is not read.
+ * A page's scale is that of an append: the smallest power of two for the values moved into it, and at least the old one
+ * where the page holds tokens before them (whose codes are encoded anew if it rises).  Moved codes are multiplied by the old
+ * scale over the new in fp32 and rounded to nearest even, once: with powers of two exact but below e4m3's normal range.  Places
+ * behind the last moved token stay as they are.  One launch on `stream`; no workspace.
+ */
+hsap_status hsap_cache_compact(const hsap_cache_desc* desc, const hsap_cache* cache, const int32_t* keep, const int32_t* cu_keep,
+                               int64_t total_keep, const int32_t* first, const int32_t* dst_table, int32_t* new_lens,
+                               void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Pages -- a page table whose sequences share pages, fork, end and give pages back, on the device, so that a captured step
+ * does it too.  The caches of all layers can go by one table.  (An extension beyond the paper.)
+ *   refs        device int32 [num_pages]: the entries of the whole table that are page p.  0: p is free.  (A caller that
+ *               keeps a page in another way adds 1.)
+ *   page_table  every entry is a page or -1.
+ * Of the descriptor heads_kv and head_dim are checked, but not used, by hsap_pages_fork and hsap_pages_reserve.
+ * Results do not depend on the order of anything: counts are whole numbers, and free pages are taken from the lowest up.
+ * --------------------------------------------------------------------- */
+
+/*
+ * hsap_pages_fork -- every row of the table becomes another row, or itself: sequence s goes on from the tokens of sequence
+ * source[s] (as they were before the call), sharing its pages.  Pages of the old row that the new one does not have are given
+ * back.
+ *   source      device int32 [num_seqs]: outside [0, num_seqs) the row ends (no pages, length 0).  NULL: every row stays.
+ *   seq_lens    device int32 [num_seqs]: tokens of each sequence; with source the new rows' are written.
+ *   window, sinks  of the layers, as in hsap_cache_attn (window 2^31 - 1: ends nothing).
+ * Entries without a token, and those whose tokens the next one no longer sees, become -1: with source = NULL the pages behind
+ * rejected drafts, or behind a window, are given back.
+ * num_seqs <= 16384, else HSAP_ERR_UNSUPPORTED.  One launch on `stream`, with source two.
+ */
+hsap_status hsap_pages_fork(const hsap_cache_desc* desc, int32_t* page_table, int32_t* seq_lens, int32_t* refs, const int32_t* source,
+                            int32_t window, int32_t sinks, void* hip_stream);
+
+/* Bytes of device workspace hsap_pages_reserve needs (host); -1 for invalid arguments.  num_pages is not read. */
+int64_t hsap_pages_reserve_workspace(const hsap_cache_desc* desc, int64_t total_new);
+
+/*
+ * hsap_pages_reserve -- pages for new tokens, before they are appended: every place that hsap_cache_append will write gets a
+ * page that no other entry of the table shares.
+ *   seq_lens, cu_new, total_new  as in hsap_cache_append (the new tokens included).
+ * Places without a page get a free one.  A page that is shared is left to the others -- or, where all that share it are
+ * to write, to the last of them -- and a free one takes its place; if it holds older tokens of the sequence it has to be copied:
+ *   pairs       device int32 [num_seqs, 2]: that page and the one in its place; -1, -1 for a sequence without such a page.
+ *               For hsap_cache_copy_pages, in every layer's cache, before the append.
+ *   missing     device int32 [1]: 0, or by how many pages the free ones are too few.  Nothing but missing and pairs (-1 all
+ *               through) is changed then: look at it before the append where that can be.
+ *   workspace   device, 16-byte aligned, workspace_bytes >= hsap_pages_reserve_workspace; contents ignored.  Calls that
+ *               overlap in time need workspaces of their own.
+ * Places behind the table are left out, as by the append.  One launch on `stream`.
+ */
+hsap_status hsap_pages_reserve(const hsap_cache_desc* desc, int32_t* page_table, const int32_t* seq_lens, int32_t* refs,
+                               const int32_t* cu_new, int64_t total_new, int32_t* pairs, int32_t* missing, void* workspace,
+                               int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * hsap_cache_copy_pages -- codes and scales of pages, K's and V's, copied to other pages.
+ *   pairs       device int32 [count, 2]: from, to.  A pair with a number that is no page, or twice the same, is skipped.  No
+ *               page is copied to twice, or both to and from.
+ * One launch on `stream`.
+ */
+hsap_status hsap_cache_copy_pages(const hsap_cache_desc* desc, const hsap_cache* cache, const int32_t* pairs, int64_t count,
+                                  void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Rotation by positions of several axes -- models of images and video give every token a position per axis (time, row,
+ * column), and every pair of a head's values turns by one of them; drafted tokens of a tree have the position of their depth,
+ * not of their place in the cache.  (An extension beyond the paper, as the cache above is.)
+ *
+ * Pair i, the values (i, i + rot_dim / 2) or with interleaved != 0 (2 i, 2 i + 1), becomes
+ *   (a cos - b sin, b cos + a sin),  cos = cos_sin[p, i], sin = cos_sin[p, rot_dim / 2 + i], p = positions[pair_axis[i], t],
+ * each operation in fp32; values behind rot_dim stay.
+ *   cos_sin      device fp32 [rows, rot_dim], 16-byte aligned.
+ *   rot_dim      a multiple of 16 from 16 up to head_dim.
+ *   axes         1 to 4.
+ *   pair_axis    of each of the rot_dim / 2 pairs, below axes (host; read before the call returns).
+ * positions is device int32 [axes, tokens].  A token with a position below 0 or at or behind `rows` on any axis is skipped:
+ * nothing of it is written.
+ * --------------------------------------------------------------------- */
+typedef struct {
+  const float* cos_sin;
+  int64_t rows;
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t axes;
+  uint8_t pair_axis[64];
+} hsap_rotation;
+
+/* Rows of one tensor: token t's [heads, head_dim], contiguous, at t * stride elements; 16-byte aligned, strides multiples of
+ * 8.  bf16, or fp32 where in_f32 / out_f32 says so (gradients summed over shards; out is rounded to nearest even once). */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t in_stride;
+  int64_t out_stride;
+  int32_t heads;
+  int32_t in_f32;
+  int32_t out_f32;
+} hsap_token_rows;
+
+/*
+ * hsap_rotate -- q's rows and k's (k may be NULL) rotated; with inverse != 0 rotated back, which is the gradient: what
+ * the attention's backward gives for the rotated rows becomes that of the rows before.
+ *   head_dim   64 or 128.
+ *   positions  device int32 [axes, total]; total >= 0.
+ * out may be in (same type and stride); else no output overlaps an input.  One launch on `stream`; no workspace.
+ */
+hsap_status hsap_rotate(const hsap_rotation* rotation, int32_t head_dim, const int32_t* positions, int64_t total,
+                        const hsap_token_rows* q, const hsap_token_rows* k, int32_t inverse, void* hip_stream);
+
+/*
+ * hsap_cache_append_at -- hsap_cache_append with the rotation by positions given for every new token, device int32
+ * [axes, total_new], instead of by its place in its sequence.  Where a token goes (its place, page and slot) follows
+ * seq_lens and cu_new as there, and so does everything else; what is said there of cos_sin_rows holds for the positions.
+ * Of a page whose first token is skipped the scale is that of the tokens that are not.
+ */
+hsap_status hsap_cache_append_at(const hsap_cache_desc* desc, const hsap_cache* cache, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, const int32_t* cu_new, int64_t total_new,
+                                 const hsap_rotation* rotation, const int32_t* positions, void* k_out, const void* q,
+                                 int64_t q_stride, int32_t heads_q, void* q_out, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Step executor -- the library's runtime for one shard geometry: each packed
  * batch is planned on the host and run with one call per stage.  Not in the
  * paper; it sequences the entry points above the way a training step uses

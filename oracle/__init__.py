@@ -45,9 +45,12 @@ What it computes, with the passages it follows (HSAP paper, arxiv 2606.30460):
 * ``window`` -- window attention with sinks over the packed documents (an extension beyond the paper's full
   attention), with derived error bounds.
 * ``cache`` -- the paged 8-bit K/V cache: rotation, codes and scales of an append, attention over it (an extension).
+* ``tree``, ``pages`` -- drafted tokens' masks, positions and attention over that cache; rows of its page table that
+  fork, pages for new tokens, kept tokens moved together (extensions).
 
 Parity status: every function above is pinned by ``tests/test_oracle_pins.py`` (``window``:
-``tests/test_window_oracle.py``, ``cache``: ``tests/test_cache_oracle.py``) against brute force, closed forms, library routines or invariants; none is
+``tests/test_window_oracle.py``, ``cache``: ``tests/test_cache_oracle.py``, ``tree`` and ``pages``:
+``tests/test_drafts_oracle.py``) against brute force, closed forms, library routines or invariants; none is
 "parity unpinned".
 """
 from .attention import (  # noqa: F401

@@ -44,6 +44,8 @@ EXPORTED = (
     "hsap_executor_merge", "hsap_executor_backward",
     "hsap_window_attn_fwd", "hsap_window_attn_bwd_workspace", "hsap_window_attn_bwd",
     "hsap_cache_append", "hsap_cache_attn_workspace", "hsap_cache_attn",
+    "hsap_rotate", "hsap_cache_append_at", "hsap_tree_masks", "hsap_cache_tree_attn_workspace", "hsap_cache_tree_attn",
+    "hsap_cache_compact", "hsap_pages_fork", "hsap_pages_reserve_workspace", "hsap_pages_reserve", "hsap_cache_copy_pages",
 )
 
 EXEC_BACKWARD = 1
@@ -98,6 +100,17 @@ class CacheBuffers(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
 
 
+class RotationDesc(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("rows", ctypes.c_int64), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("axes", ctypes.c_int32), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
+class TokenRows(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("out", ctypes.c_void_p), ("in_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("in_f32", ctypes.c_int32),
+                ("out_f32", ctypes.c_int32)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 _P = ctypes.c_void_p
@@ -147,6 +160,17 @@ _SIG = {
                                          _P]),
     "hsap_cache_attn_workspace": (ctypes.c_int64, [_P, _I32, _I64, _I32]),
     "hsap_cache_attn": (ctypes.c_int, [_P, _P, _I32, ctypes.c_float, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P]),
+    "hsap_rotate": (ctypes.c_int, [_P, _I32, _P, _I64, _P, _P, _I32, _P]),
+    "hsap_cache_append_at": (ctypes.c_int, [_P, _P, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _I32, _P, _P]),
+    "hsap_tree_masks": (ctypes.c_int, [_I32, _P, _P, _I64, _P, _I32, _P, _P, _P]),
+    "hsap_cache_tree_attn_workspace": (ctypes.c_int64, [_P, _I32, _I64, _I32]),
+    "hsap_cache_tree_attn": (ctypes.c_int, [_P, _P, _I32, ctypes.c_float, _I32, _I32, _P, _I64, _P, _I64, _P, _I32, _P, _P, _P,
+                                            _P, _I64, _P]),
+    "hsap_cache_compact": (ctypes.c_int, [_P, _P, _P, _P, _I64, _P, _P, _P, _P]),
+    "hsap_pages_fork": (ctypes.c_int, [_P, _P, _P, _P, _P, _I32, _I32, _P]),
+    "hsap_pages_reserve_workspace": (ctypes.c_int64, [_P, _I64]),
+    "hsap_pages_reserve": (ctypes.c_int, [_P, _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P]),
+    "hsap_cache_copy_pages": (ctypes.c_int, [_P, _P, _P, _I64, _P]),
 }
 
 
@@ -212,7 +236,7 @@ def _load_torch():
     global _torch
     if _torch is None:
         import torch
-        for name in ("bfloat16", "float32", "int32", "uint8"):
+        for name in ("bfloat16", "float32", "int32", "int64", "uint8"):
             _dtypes[name] = getattr(torch, name)
         _torch = torch
     return _torch
@@ -804,13 +828,13 @@ class KVCache:
         object.__setattr__(self, name, t)
 
 
-def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int):
-    """Address and row stride (elements) of a bf16 tensor [rows, heads, d] on the current device, its rows contiguous."""
+def _token_rows(t, what: str, rows: int, heads: int, d: int, here: int, dtype_name: str = "bfloat16"):
+    """Address and row stride (elements) of a tensor [rows, heads, d] on the current device, its rows contiguous."""
     torch = _torch or _load_torch()
     if not isinstance(t, torch.Tensor) or t.get_device() < 0:
         raise TypeError("%s must be a device tensor" % what)
-    if t.dtype is not _dtypes["bfloat16"]:
-        raise TypeError("%s must be bfloat16, got %s" % (what, t.dtype))
+    if t.dtype is not _dtypes[dtype_name]:
+        raise TypeError("%s must be %s, got %s" % (what, dtype_name, t.dtype))
     if t.shape != (rows, heads, d):
         raise ValueError("%s is %s, expected [%d, %d, %d]" % (what, list(t.shape), rows, heads, d))
     if t.get_device() != here:
@@ -886,6 +910,197 @@ def cache_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_new, o_
         _arg(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim, here),
         0 if lse_out is None else _arg(lse_out, "float32", "lse_out", total * heads_q, here),
         _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream_on(stream, here)))
+
+
+# ---------------------------------------------------------------------------
+# rotation by positions of several axes
+# ---------------------------------------------------------------------------
+
+class Rotation:
+    """A rotation's table and the axis of each of its pairs (hsap_rotation): cos_sin fp32 [positions, rot_dim] (cos | sin),
+    pair_axis: rot_dim / 2 numbers below the number of axes (None: one axis).  The table is the caller's: writing other
+    values into it changes the next call."""
+
+    def __init__(self, cos_sin, pair_axis=None, interleaved: bool = False, axes: Optional[int] = None):
+        _dev(cos_sin, "float32", "cos_sin")
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [positions, rot_dim]")
+        rows, rot = cos_sin.shape
+        pairs = [0] * (rot // 2) if pair_axis is None else [int(x) for x in pair_axis]
+        if len(pairs) != rot // 2 or len(pairs) > 64:
+            raise ValueError("pair_axis has %d entries, expected rot_dim / 2 = %d (at most 64)" % (len(pairs), rot // 2))
+        self.axes = max(pairs, default=0) + 1 if axes is None else int(axes)
+        if min(pairs, default=0) < 0 or max(pairs, default=0) >= self.axes or not 1 <= self.axes <= 4:
+            raise ValueError("pair_axis must name axes 0 .. %d, of at most four" % (self.axes - 1))
+        self.cos_sin, self.device_index = cos_sin, cos_sin.get_device()
+        self.desc = RotationDesc(_ptr(cos_sin), rows, rot, 1 if interleaved else 0, self.axes, (ctypes.c_uint8 * 64)(*pairs))
+        self._ref = ctypes.byref(self.desc)
+
+    def _positions(self, positions, total: int, here: int) -> int:
+        """Address of positions int32 [axes, total] on the current device, which is the table's."""
+        if self.device_index != here:
+            raise ValueError("the rotation is on cuda:%d, but cuda:%d is the current device" % (self.device_index, here))
+        if positions.shape != (self.axes, total) and (self.axes > 1 or positions.shape != (total,)):
+            raise ValueError("positions is %s, expected [%d, %d]" % (list(positions.shape), self.axes, total))
+        return _arg(positions, "int32", "positions", None, here)
+
+
+def _turned_rows(x, out, what: str, total: int, here: int) -> TokenRows:
+    f32 = [getattr(t, "dtype", None) is _dtypes["float32"] for t in (x, out)]
+    d = x.shape[-1]
+    src, in_stride = _token_rows(x, what, total, x.shape[1], d, here, "float32" if f32[0] else "bfloat16")
+    dst, out_stride = _token_rows(out, what + "_out", total, x.shape[1], d, here, "float32" if f32[1] else "bfloat16")
+    return TokenRows(src, dst, in_stride, out_stride, x.shape[1], f32[0], f32[1])
+
+
+def rotate(rotation: Rotation, positions, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
+    """hsap_rotate: q [tokens, Hq, d] -> q_out and, if given, k [tokens, Hkv, d] -> k_out (rows may be strided; each bf16
+    or fp32) turned by positions int32 [axes, tokens] ([tokens] with one axis); inverse: back, the gradient's way."""
+    here = _here()
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together")
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[2] != q.shape[2])):
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    total, _, d = q.shape
+    place = rotation._positions(positions, total, here)
+    rows = _turned_rows(q, q_out, "q", total, here)
+    more = None if k is None else _turned_rows(k, k_out, "k", total, here)
+    _check(lib().hsap_rotate(rotation._ref, d, place, total, ctypes.byref(rows), None if more is None else ctypes.byref(more),
+                             1 if inverse else 0, _stream_on(stream, here)))
+
+
+def cache_append_at(cache: KVCache, k, v, cu_new, rotation: Rotation, positions, k_out=None, q=None, q_out=None,
+                    stream=None) -> None:
+    """hsap_cache_append_at: cache_append with K (and q) turned by positions int32 [axes, total_new] ([total_new] with one
+    axis) instead of by their places in their sequences."""
+    here, c = _cache_here(cache), cache.desc
+    hkv, d = c.heads_kv, c.head_dim
+    total = k.shape[0]
+    kp, ks = _token_rows(k, "k", total, hkv, d, here)
+    vp, vs = _token_rows(v, "v", total, hkv, d, here)
+    cu = 0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here)
+    place = rotation._positions(positions, total, here)
+    ko = 0 if k_out is None else _arg(k_out, "bfloat16", "k_out", total * hkv * d, here)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    heads = qp = qs = qo = 0
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _token_rows(q, "q", total, heads, d, here)
+        qo = _arg(q_out, "bfloat16", "q_out", total * heads * d, here)
+    _check(lib().hsap_cache_append_at(*cache._refs, kp, ks, vp, vs, cu, total, rotation._ref, place, ko, qp, qs, heads, qo,
+                                      _stream_on(stream, here)))
+
+
+# ---------------------------------------------------------------------------
+# trees of drafted tokens
+# ---------------------------------------------------------------------------
+
+def _mask(mask, total: int, here: int):
+    """Address and words of a mask int64 [total, mask_words]."""
+    if mask.dim() != 2 or mask.shape[0] != total:
+        raise ValueError("mask is %s, expected [%d, mask_words]" % (list(mask.shape), total))
+    return _arg(mask, "int64", "mask", None, here), mask.shape[1]
+
+
+def tree_masks(seq_lens, cu_new, parents, mask, positions, stream=None) -> None:
+    """hsap_tree_masks: parents int32 [total_new] (each drafted token's, among its sequence's; -1: none) -> mask int64
+    [total_new, mask_words] (its own and its ancestors' bits) and positions int32 [total_new].  seq_lens int32 [num_seqs]
+    counts the drafted tokens; cu_new int32 [num_seqs + 1], or None for one drafted token per sequence (parents unused)."""
+    here = _here()
+    lens = _arg(seq_lens, "int32", "seq_lens", None, here)
+    seqs, total = seq_lens.numel(), positions.numel()
+    cu = 0 if cu_new is None else _arg(cu_new, "int32", "cu_new", seqs + 1, here)
+    up = 0 if cu_new is None else _arg(parents, "int32", "parents", total, here)
+    bits, words = _mask(mask, total, here)
+    _check(lib().hsap_tree_masks(seqs, lens, cu, total, up, words, bits, _arg(positions, "int32", "positions", None, here),
+                                 _stream_on(stream, here)))
+
+
+def cache_tree_attn_workspace(cache: KVCache, heads_q: int, total_q: int, one_each: Optional[bool] = None) -> int:
+    """hsap_cache_tree_attn_workspace: bytes that cache_tree_attn needs for total_q rows.  one_each: whether the calls pass
+    no cu_new; None: the larger of both."""
+    if one_each is None:
+        return max(cache_tree_attn_workspace(cache, heads_q, total_q, x) for x in (True, False))
+    v = lib().hsap_cache_tree_attn_workspace(ctypes.byref(cache.desc), int(heads_q), int(total_q), int(one_each))
+    if v < 0:
+        raise HsapError(HSAP_ERR_INVALID_ARG, lib().hsap_last_error().decode())
+    return v
+
+
+def cache_tree_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_new, mask, positions, o_out, lse_out, workspace,
+                    window: int = MAX_WINDOW, sinks: int = 0, stream=None) -> None:
+    """hsap_cache_tree_attn: q bf16 [total_q, Hq, d] (rows may be strided; the sequences' drafted tokens) over the cache:
+    the tokens before the drafts, and the drafted ones that mask int64 [total_q, mask_words] names; positions int32 [total_q]
+    -> o_out bf16 [total_q, Hq, d], lse_out fp32 [Hq, total_q] or None; workspace: uint8, cache_tree_attn_workspace bytes."""
+    here, c = _cache_here(cache), cache.desc
+    total = q.shape[0]
+    qp, qs = _token_rows(q, "q", total, heads_q, c.head_dim, here)
+    bits, words = _mask(mask, total, here)
+    _check(lib().hsap_cache_tree_attn(
+        *cache._refs, heads_q, softmax_scale, _extent(window, "window"), _extent(sinks, "sinks"), qp, qs,
+        0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here), total, bits, words,
+        _arg(positions, "int32", "positions", total, here), _arg(o_out, "bfloat16", "o_out", total * heads_q * c.head_dim, here),
+        0 if lse_out is None else _arg(lse_out, "float32", "lse_out", total * heads_q, here),
+        _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream_on(stream, here)))
+
+
+def cache_compact(cache: KVCache, keep, cu_keep, first=None, dst_table=None, new_lens=None, stream=None) -> None:
+    """hsap_cache_compact: of every sequence the tokens at places keep[cu_keep[s] ..] (int32, ascending) move to places
+    first[s] .. (None: 0 ..), in place or into the pages of dst_table int32 [num_seqs, table_width]; new_lens int32
+    [num_seqs] takes the lengths (cache.seq_lens may be given)."""
+    here, c = _cache_here(cache), cache.desc
+    _check(lib().hsap_cache_compact(
+        *cache._refs, _arg(keep, "int32", "keep", None, here), _arg(cu_keep, "int32", "cu_keep", c.num_seqs + 1, here),
+        keep.numel(), 0 if first is None else _arg(first, "int32", "first", c.num_seqs, here),
+        0 if dst_table is None else _arg(dst_table, "int32", "dst_table", c.num_seqs * c.table_width, here),
+        0 if new_lens is None else _arg(new_lens, "int32", "new_lens", c.num_seqs, here), _stream_on(stream, here)))
+
+
+# ---------------------------------------------------------------------------
+# pages
+# ---------------------------------------------------------------------------
+
+def pages_fork(cache: KVCache, refs, source=None, seq_lens=None, window: int = MAX_WINDOW, sinks: int = 0, stream=None) -> None:
+    """hsap_pages_fork on the cache's page table: row s goes on from row source[s] (int32 [num_seqs]; -1: it ends; None:
+    every row stays), pages behind its length and those that the window has left are given back.  refs int32 [num_pages];
+    seq_lens: the sequences' lengths (None: cache.seq_lens), rewritten with source."""
+    here, c = _cache_here(cache), cache.desc
+    lens = cache.seq_lens if seq_lens is None else seq_lens
+    _check(lib().hsap_pages_fork(
+        cache._refs[0], _ptr(cache.page_table), _arg(lens, "int32", "seq_lens", c.num_seqs, here),
+        _arg(refs, "int32", "refs", c.num_pages, here),
+        0 if source is None else _arg(source, "int32", "source", c.num_seqs, here), _extent(window, "window"),
+        _extent(sinks, "sinks"), _stream_on(stream, here)))
+
+
+def pages_reserve_workspace(cache: KVCache, total_new: int) -> int:
+    """hsap_pages_reserve_workspace: bytes of workspace pages_reserve needs for total_new tokens."""
+    v = lib().hsap_pages_reserve_workspace(ctypes.byref(cache.desc), int(total_new))
+    if v < 0:
+        raise HsapError(HSAP_ERR_INVALID_ARG, lib().hsap_last_error().decode())
+    return v
+
+
+def pages_reserve(cache: KVCache, refs, cu_new, total_new: int, pairs, missing, workspace, stream=None) -> None:
+    """hsap_pages_reserve on the cache's page table: a page of its own for every place that an append of total_new tokens
+    (cu_new as there; cache.seq_lens counts them) writes.  pairs int32 [num_seqs, 2]: pages to copy first
+    (cache_copy_pages, in every layer's cache); missing int32 [1]: pages that were not to be had (then nothing is changed)."""
+    here, c = _cache_here(cache), cache.desc
+    _check(lib().hsap_pages_reserve(
+        cache._refs[0], _ptr(cache.page_table), _ptr(cache.seq_lens), _arg(refs, "int32", "refs", c.num_pages, here),
+        0 if cu_new is None else _arg(cu_new, "int32", "cu_new", c.num_seqs + 1, here), total_new,
+        _arg(pairs, "int32", "pairs", 2 * c.num_seqs, here), _arg(missing, "int32", "missing", 1, here),
+        _arg(workspace, "uint8", "workspace", None, here), workspace.numel(), _stream_on(stream, here)))
+
+
+def cache_copy_pages(cache: KVCache, pairs, stream=None) -> None:
+    """hsap_cache_copy_pages: pairs int32 [n, 2] of pages, from and to (-1: none)."""
+    here = _cache_here(cache)
+    at = _arg(pairs, "int32", "pairs", None, here)
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError("pairs is %s, expected [n, 2]" % list(pairs.shape))
+    _check(lib().hsap_cache_copy_pages(*cache._refs, at, pairs.shape[0], _stream_on(stream, here)))
 
 
 # ---------------------------------------------------------------------------

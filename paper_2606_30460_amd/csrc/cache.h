@@ -82,6 +82,7 @@ HSAP_CACHE_HD Steps<STEP> cache_steps(int32_t plo, int32_t phi, int32_t cap, int
 
 constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
 constexpr int kMaxSplits = 128;  // of a row tile's tokens
+constexpr int kMaxMaskWords = HSAP_MAX_MASK_WORDS;
 
 // How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip, each of at least 256 tokens.
 struct CacheCut {

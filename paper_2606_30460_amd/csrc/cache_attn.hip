@@ -47,6 +47,9 @@ struct CacheAttnArgs {
   int32_t sinks;
   int32_t splits;
   float scale_log2;
+  const uint64_t* mask;      // TREE kernels: [total_q, words]
+  const int32_t* positions;  // TREE kernels: [total_q]
+  int32_t words;
 };
 
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
@@ -91,6 +94,39 @@ __device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, i
   return t.count > 0 && row0 < (int64_t)t.count * a.group;
 }
 
+// Trees.  A row sees the tokens before the drafted ones, from `base` places on, by its position (window, sinks) and the
+// drafted ones that its mask names.  Bits of drafted tokens from .. from + 63 (from may be below 0) of a row's mask:
+__device__ __forceinline__ uint64_t mask_bits(const uint64_t* mask, int32_t words, int32_t from) {
+  if (from <= -64) return 0;
+  if (from < 0) return mask[0] << -from;
+  const int32_t w = from >> 6, sh = from & 63;
+  uint64_t x = w < words ? mask[w] >> sh : 0;
+  if (sh && w + 1 < words) x |= mask[w + 1] << (64 - sh);
+  return x;
+}
+// Position of drafted token x of the sequence whose first is t0 (x may be any number: it is not used then).
+__device__ __forceinline__ int32_t drafted_position(const CacheAttnArgs& a, const RowTile& rt, int32_t x) {
+  return a.positions[rt.t0 + min(max(x, 0), rt.count - 1)];
+}
+// Least and largest position of the rows that see anything (a position below 0 sees nothing): over the lanes that differ in
+// the bits of LANES.
+template <int LANES>
+__device__ __forceinline__ void position_range(int32_t& lo, int32_t& hi) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) {
+    lo = min(lo, __shfl_xor(lo, o));
+    hi = max(hi, __shfl_xor(hi, o));
+  }
+}
+// Steps of a tile whose rows' positions are plo .. phi (none: phi < 0): the sinks', then from the first window, or from the
+// drafted tokens where that is behind them, to the last token.
+template <int STEP>
+__device__ __forceinline__ Steps<STEP> tree_steps(int32_t plo, int32_t phi, int32_t base, int32_t len, int32_t cap, int32_t window,
+                                                  int32_t sinks) {
+  const int64_t most = (int64_t)max(base, 0) + window - 1;
+  return cache_steps<STEP>((int32_t)min((int64_t)plo, most), phi < 0 ? -1 : len - 1, cap, window, sinks);
+}
+
 template <typename T, bool ONCE>
 __device__ __forceinline__ T read_codes(const uint8_t* p) {
   typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
@@ -101,7 +137,8 @@ __device__ __forceinline__ T read_codes(const uint8_t* p) {
 // ONCE: every code is read by one workgroup of the call alone and the cache is larger than the 256 MB behind the L2s: the
 // loads are marked as streaming (64 sequences of 8k tokens, 8 heads of 128: 128 -> 119 us; with several row tiles per
 // sequence 46 -> 49 us, with 67 MB of codes, which the next call finds there again, 21.8 -> 22.5 us).
-template <int D, int MT, bool ONCE>
+// TREE: drafted tokens by masks.  A step's places that no row of the tile sees are found by ballots over its rows.
+template <int D, int MT, bool ONCE, bool TREE>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   constexpr int KX = D / 64, CB = D / 16, ROWS = 16 * MT;  // 16-byte loads per K row and lane; d values per lane of V
   constexpr float NEG_INF = -__builtin_inff();
@@ -122,8 +159,22 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   const int32_t nrows = rt.count * a.group;
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
   const int32_t pos0 = len - rt.count;  // position of the sequence's first new token
-  const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
-  const Steps<32> steps = cache_steps<32>(plo, phi, cap, a.window, a.sinks);
+  int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
+  if constexpr (TREE) {
+    plo = INT32_MAX;
+    phi = -1;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int32_t p = a.positions[rt.t0 + min(rt.row0 + 16 * mt + l16, last_row) / a.group];
+      plo = min(plo, p < 0 ? INT32_MAX : p);
+      phi = max(phi, p);
+    }
+    position_range<16>(plo, phi);
+    plo = uniform(plo);
+    phi = uniform(phi);
+  }
+  const Steps<32> steps = TREE ? tree_steps<32>(plo, phi, pos0, len, cap, a.window, a.sinks)
+                               : cache_steps<32>(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
   const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
   if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
@@ -140,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   for (int mt = 0; mt < MT; ++mt) {
     const int32_t r = min(rt.row0 + 16 * mt + l16, nrows - 1);
     const int32_t t = r / a.group;
-    pos[mt] = pos0 + t;
+    pos[mt] = TREE ? a.positions[rt.t0 + t] : pos0 + t;
     const __bf16* qp = a.q + (int64_t)(rt.t0 + t) * a.q_stride + (int64_t)(g * a.group + (r - t * a.group)) * D + 16 * grp;
 #pragma unroll
     for (int x = 0; x < KX; ++x) {
@@ -149,7 +200,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     }
   }
   const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
-  const int32_t top = min(phi, cap - 1);  // last token any row sees
+  const int32_t top = min(TREE ? len - 1 : phi, cap - 1);  // last token any row sees
+  const bool live = !TREE || __builtin_amdgcn_ballot_w64(MT == 1 ? pos[0] < 0 : pos[0] < 0 || pos[MT - 1] < 0) == 0;
 
   struct Tokens {
     uint4 k[2][KX];
@@ -224,7 +276,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     const int32_t sinks = s < steps.sinks ? min(a.sinks, steps.win0) : a.sinks;
     const int32_t near = s < steps.sinks ? 0 : a.window;
     // every row of the tile sees every token of the step
-    const bool all = x.held[0] && x.held[1] && jl <= plo && (phi - x.j0 < near || jl < sinks);
+    const bool all = x.held[0] && x.held[1] && (TREE ? live && jl < pos0 : jl <= plo) && (phi - x.j0 < near || jl < sinks);
+    uint64_t rows[TREE ? 8 : 1] = {};  // rows that see each of the lanes' tokens
+    int32_t drafted[TREE ? 8 : 1];     // and its position, of a drafted one
+    if constexpr (TREE) {
+      if (jl >= pos0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          drafted[e] = a.window == INT32_MAX ? 0 : drafted_position(a, rt, x.j0 + 16 * (e >> 2) + 4 * grp + (e & 3) - pos0);
+      }
+    }
     // V's scale: its power of two goes into the conversion of the codes, what is left of it (1 for the scales that an
     // append makes) into P
     float vpow[2], vrest[2];
@@ -244,12 +305,28 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
         for (int kk = 0; kk < 2 * KX; ++kk) sc[half] = mfma16(kf[half][kk], qf[mt][kk], sc[half]);
       const float sl[2] = {fmaxf(x.ks[0] * a.scale_log2, 1.17549435e-38f), fmaxf(x.ks[1] * a.scale_log2, 1.17549435e-38f)};
       if (!all) {
+        uint32_t bits = 0;  // the row's mask, of the step's tokens
+        if constexpr (TREE) {
+          if (jl >= pos0) {
+            const int32_t t = min(rt.row0 + 16 * mt + l16, nrows - 1) / a.group;
+            bits = (uint32_t)mask_bits(a.mask + (int64_t)(rt.t0 + t) * a.words, a.words, x.j0 - pos0);
+          }
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int32_t j = x.j0 + 16 * half + 4 * grp + e;
-            const bool see = j <= pos[mt] && (pos[mt] - j < near || j < sinks) && x.held[half];
+            bool see;
+            if constexpr (TREE) {
+              const bool before = j < pos0;
+              const int32_t at = before ? j : drafted[4 * half + e];
+              see = (before | (bits >> (16 * half + 4 * grp + e) & 1)) & (pos[mt] >= 0) & (j <= top) & x.held[half] &
+                    ((a.window == INT32_MAX && near) | (pos[mt] - at < near) | (at < sinks));
+              rows[4 * half + e] |= __builtin_amdgcn_ballot_w64(see);
+            } else {
+              see = j <= pos[mt] && (pos[mt] - j < near || j < sinks) && x.held[half];
+            }
             if (!see) sc[half][e] = NEG_INF;
           }
       }
@@ -288,7 +365,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     VT v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) v[y] = x.v[y];
-    if (jl > top || !x.held[0] || !x.held[1] || steps.edge(s)) {  // P is 0 there, V whatever the page holds
+    if (TREE && !all) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((rows[4 * half + e] >> (16 * grp) & 0xFFFF) == 0) v[4 * half + e] = VT{};
+        // (of sixteen tokens that no row sees the page's scale may be anything too)
+        if ((rows[4 * half] | rows[4 * half + 1] | rows[4 * half + 2] | rows[4 * half + 3]) == 0) vpow[half] = 1.f;
+      }
+    }
+    if (!TREE && (jl > top || !x.held[0] || !x.held[1] || steps.edge(s))) {  // P is 0 there, V whatever the page holds
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
         const int32_t j = x.j0 + 16 * (y >> 2) + 4 * grp + (y & 3);
@@ -419,13 +506,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
 // 32x32x16 products S^T = K Q^T, O^T += V^T P^T with V^T by transpose reads.  P is rounded to bf16 for the second product,
 // as in the window kernels.  2048 rows x 8 heads over 30000 tokens, head_dim 128: 680 us, 765 TFLOP/s (a step's products,
 // exponentials and decoding add up in a wave: matrix cores 0.31 busy).  head_dim 64: three workgroups per CU (185 -> 167 us).
-template <int D>
+template <int D, bool TREE>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
   constexpr int KB = 64, CPR = D / 8, TILE = KB * D, ROWS = kChunkRows, U = D / 64;  // U: runs of 16 codes per thread
   constexpr float NEG_INF = -__builtin_inff(), TINY = 1.17549435e-38f;
   constexpr float RESCALE_SLACK = 8.f;
   __shared__ __attribute__((aligned(16))) __bf16 tiles[2][2][TILE];  // [slot][K, V]
   __shared__ __attribute__((aligned(16))) float scales[2][2][4];     // [slot][K's times the softmax's, V's rest][16 tokens]
+  __shared__ uint32_t named[TREE ? 2 * kMaxMaskWords : 1];           // drafted tokens that some row of the tile names
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -439,8 +527,24 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
   const int32_t nrows = rt.count * a.group;
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
   const int32_t pos0 = len - rt.count;
-  const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
-  const Steps<KB> steps = cache_steps<KB>(plo, phi, cap, a.window, a.sinks);
+  // this lane's query
+  const int32_t row = min(rt.row0 + 32 * w + l32, last_row), tok = row / a.group;
+  int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
+  if constexpr (TREE) {
+    plo = INT32_MAX;
+    phi = -1;
+#pragma unroll
+    for (int r = 0; r < ROWS; r += 64) {
+      const int32_t p = a.positions[rt.t0 + min(rt.row0 + r + lane, last_row) / a.group];
+      plo = min(plo, p < 0 ? INT32_MAX : p);
+      phi = max(phi, p);
+    }
+    position_range<64>(plo, phi);
+    plo = uniform(plo);
+    phi = uniform(phi);
+  }
+  const Steps<KB> steps = TREE ? tree_steps<KB>(plo, phi, pos0, len, cap, a.window, a.sinks)
+                               : cache_steps<KB>(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
   const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
   if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
@@ -449,12 +553,30 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       a.part_lse[((int64_t)split * a.total_q + rt.t0 + t) * a.heads_q + g * a.group + (r - t * a.group)] = NEG_INF;
     return;
   }
-  // this lane's query, and the first and last position of the wave's
+  // its position, and the first and last position of the wave's
   const bool busy = rt.row0 + 32 * w <= last_row;
-  const int32_t row = min(rt.row0 + 32 * w + l32, last_row), tok = row / a.group;
-  const int32_t pos = pos0 + tok;
-  const int32_t wlo = pos0 + min(rt.row0 + 32 * w, last_row) / a.group;
-  const int32_t whi = pos0 + min(rt.row0 + 32 * w + 31, last_row) / a.group;
+  const int32_t pos = TREE ? a.positions[rt.t0 + tok] : pos0 + tok;
+  int32_t wlo = pos0 + min(rt.row0 + 32 * w, last_row) / a.group;
+  int32_t whi = pos0 + min(rt.row0 + 32 * w + 31, last_row) / a.group;
+  if constexpr (TREE) {
+    wlo = pos < 0 ? INT32_MAX : pos;
+    whi = pos;
+    position_range<32>(wlo, whi);
+    wlo = uniform(wlo);
+    whi = uniform(whi);
+    // (the first barrier comes before the first of them is read)
+    for (int i = tid; i < 2 * a.words; i += 256) named[i] = 0;
+    __syncthreads();
+    const int32_t first = rt.row0 / a.group, count = last_row / a.group - first + 1;
+    for (int i = tid; i < count * a.words; i += 256) {
+      const int32_t t = i / a.words, x = i - t * a.words;
+      const uint64_t m = a.mask[(int64_t)(rt.t0 + first + t) * a.words + x];
+      if ((uint32_t)m) atomicOr(&named[2 * x], (uint32_t)m);
+      if (m >> 32) atomicOr(&named[2 * x + 1], (uint32_t)(m >> 32));
+    }
+    __syncthreads();
+  }
+  const bool live = !TREE || __builtin_amdgcn_ballot_w64(pos < 0) == 0;
   const int h = g * a.group + (row - tok * a.group);
   bf16x8 qf[D / 16];
   {
@@ -463,7 +585,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
     for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
   }
   const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
-  const int32_t top = min(phi, cap - 1);  // last token any row sees
+  const int32_t top = min(TREE ? len - 1 : phi, cap - 1);  // last token any row sees
 
   // Thread's codes of a step: of the 64 tokens those of 16-token group group_of(u) (one page each), 16 codes of a token.
   auto group_of = [&](int u) { return D == 64 ? w : (w >> 1) + 2 * u; };
@@ -519,7 +641,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       const int token = 16 * group_of(u) + slot_in;
       const int32_t j = steps.first(s) + token;
       float vpow = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
-      if (j > top || !x.held[u] || (steps.edge(s) && !steps.seen(a.sinks, j, j))) {  // anything may be there
+      bool unseen = j > top || !x.held[u] || (steps.edge(s) && !steps.seen(a.sinks, j, j));
+      if (TREE && j >= pos0) unseen |= j - pos0 >= 64 * a.words || !(named[(j - pos0) >> 5] >> ((j - pos0) & 31) & 1);
+      if (unseen) {  // anything may be there
         x.k[u] = x.v[u] = uint4{0, 0, 0, 0};
         vpow = 1.f;
       }
@@ -558,8 +682,23 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
     const int32_t near = s < steps.sinks ? 0 : a.window;
     const bool held = sl[0] > 0.f && sl[1] > 0.f && sl[2] > 0.f && sl[3] > 0.f;
     // every row of the wave sees every token of the step
-    const bool all = __builtin_amdgcn_ballot_w64(!held) == 0 && j0 + KB - 1 <= wlo && (whi - j0 < near || j0 + KB - 1 < sinks);
-    if (!all) {
+    const bool all = __builtin_amdgcn_ballot_w64(!held) == 0 && (TREE ? live && j0 + KB - 1 < pos0 : j0 + KB - 1 <= wlo) &&
+                     (whi - j0 < near || j0 + KB - 1 < sinks);
+    if (TREE && !all) {
+      const uint64_t bits = j0 + KB > pos0 ? mask_bits(a.mask + (int64_t)(rt.t0 + tok) * a.words, a.words, j0 - pos0) : 0;
+      const bool far = a.window == INT32_MAX && near;
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int32_t x = 32 * nb + c_row(j, hi), t = j0 + x;
+          const bool before = t < pos0;
+          const int32_t at = before || far ? t : drafted_position(a, rt, t - pos0);
+          const bool see = (before | (bits >> x & 1)) & (pos >= 0) & (t <= top) & (sl[2 * nb + (j >> 3)] > 0.f) &
+                           (far | (pos - at < near) | (at < sinks));
+          sc[nb][j] = see ? sc[nb][j] : NEG_INF;
+        }
+    } else if (!all) {
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -623,7 +762,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       if (more) load(s + 1, next, x);
       next = look_up(s + 2);
       const int32_t j0 = steps.first(s);
-      if (busy && j0 <= whi && (s < steps.sinks || j0 + KB - 1 >= max(wlo, 0) - (a.window - 1) || j0 < a.sinks)) compute(s, slot);
+      const bool some = s < steps.sinks || j0 + KB - 1 >= max(wlo, 0) - (a.window - 1) || j0 < a.sinks;
+      if (busy && (TREE ? some || j0 + KB > pos0 : j0 <= whi && some)) compute(s, slot);
       if (more) store(s + 1, x, slot ^ 1);
       hsap_lds_barrier();
     }
@@ -752,31 +892,20 @@ static hsap_status check_attn_rows(const hsap_cache_desc& d, int32_t heads_q, in
   return HSAP_OK;
 }
 
-template <int D>
+template <int D, bool TREE>
 static void launch_cache_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
-  if (c.rows == kChunkRows) hipLaunchKernelGGL(cache_chunk_kernel<D>, grid, block, 0, s, a);
-  else if (c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false>), grid, block, 0, s, a);
-  else if (c.once) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false>), grid, block, 0, s, a);
+  if (c.rows == kChunkRows) hipLaunchKernelGGL((cache_chunk_kernel<D, TREE>), grid, block, 0, s, a);
+  else if (c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false, TREE>), grid, block, 0, s, a);
+  else if (c.once) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true, TREE>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false, TREE>), grid, block, 0, s, a);
 }
 
-}  // namespace hsap
-
-using namespace hsap;
-
-extern "C" int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
-  clear_error();
-  if (check_cache_desc(desc, false) != HSAP_OK || check_attn_rows(*desc, heads_q, total_q) != HSAP_OK) return -1;
-  const CacheCut c = cache_cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
-  return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
-}
-
-extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
-                                       int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
-                                       int64_t total_q, void* o_out, float* lse_out, void* workspace, int64_t workspace_bytes,
-                                       void* hip_stream) {
-  clear_error();
+// A call's rows, without or with a tree's masks and positions.
+static hsap_status attend(const char* name, const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q,
+                          float softmax_scale, int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
+                          int64_t total_q, bool tree, const uint64_t* mask, int32_t words, const int32_t* positions, void* o_out,
+                          float* lse_out, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   hsap_status st = check_cache(desc, cache);
   if (st != HSAP_OK) return st;
   const int d = desc->head_dim;
@@ -787,8 +916,11 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   if (!cu_new && total_q != desc->num_seqs)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "without cu_new every sequence has one row: total_q %lld, num_seqs %d", (long long)total_q,
               desc->num_seqs);
+  if (tree && (words < 1 || words > kMaxMaskWords)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "mask_words %d: 1 to %d", words, kMaxMaskWords);
   if (total_q == 0 || desc->num_seqs == 0) return HSAP_OK;
   if (!q || !o_out || !workspace) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
+  if (tree && (!mask || !positions || ((uintptr_t)mask & 7)))
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "a tree's mask (8-byte aligned) and positions are needed");
   if (((uintptr_t)q | (uintptr_t)o_out | (uintptr_t)workspace) & 15)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "q, o_out and workspace must be 16-byte aligned");
   if (q_stride % 8 || q_stride < (int64_t)heads_q * d)
@@ -816,13 +948,21 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
   a.sinks = sinks;
   a.splits = c.splits;
   a.scale_log2 = softmax_scale * 1.44269504088896340736f;
+  a.mask = mask;
+  a.positions = positions;
+  a.words = words;
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
-  if (d == 128) launch_cache_attn<128>(a, c, blocks, s);
-  else launch_cache_attn<64>(a, c, blocks, s);
+  if (tree) {
+    if (d == 128) launch_cache_attn<128, true>(a, c, blocks, s);
+    else launch_cache_attn<64, true>(a, c, blocks, s);
+  } else {
+    if (d == 128) launch_cache_attn<128, false>(a, c, blocks, s);
+    else launch_cache_attn<64, false>(a, c, blocks, s);
+  }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn launch: %s", hipGetErrorString(e));
+  if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "%s launch: %s", name, hipGetErrorString(e));
   if (c.splits > 1) {
     const int64_t rows = total_q * heads_q;
     const dim3 few((unsigned)((rows * (d / 4) + 255) / 256)), many((unsigned)rows), block(256);
@@ -834,7 +974,41 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
       else hipLaunchKernelGGL(cache_join_many_kernel<64>, many, block, 0, s, a);
     }
     e = hipGetLastError();
-    if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_attn join launch: %s", hipGetErrorString(e));
+    if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "%s join launch: %s", name, hipGetErrorString(e));
   }
   return HSAP_OK;
+}
+
+}  // namespace hsap
+
+using namespace hsap;
+
+extern "C" int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
+  clear_error();
+  if (check_cache_desc(desc, false) != HSAP_OK || check_attn_rows(*desc, heads_q, total_q) != HSAP_OK) return -1;
+  const CacheCut c = cache_cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
+  return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
+}
+
+extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
+                                       int32_t window, int32_t sinks, const void* q, int64_t q_stride, const int32_t* cu_new,
+                                       int64_t total_q, void* o_out, float* lse_out, void* workspace, int64_t workspace_bytes,
+                                       void* hip_stream) {
+  clear_error();
+  return attend("cache_attn", desc, cache, heads_q, softmax_scale, window, sinks, q, q_stride, cu_new, total_q, false, nullptr, 0,
+                nullptr, o_out, lse_out, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" int64_t hsap_cache_tree_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
+  return hsap_cache_attn_workspace(desc, heads_q, total_q, one_each);
+}
+
+extern "C" hsap_status hsap_cache_tree_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q,
+                                            float softmax_scale, int32_t window, int32_t sinks, const void* q, int64_t q_stride,
+                                            const int32_t* cu_new, int64_t total_q, const uint64_t* mask, int32_t mask_words,
+                                            const int32_t* positions, void* o_out, float* lse_out, void* workspace,
+                                            int64_t workspace_bytes, void* hip_stream) {
+  clear_error();
+  return attend("cache_tree_attn", desc, cache, heads_q, softmax_scale, window, sinks, q, q_stride, cu_new, total_q, true, mask,
+                mask_words, positions, o_out, lse_out, workspace, workspace_bytes, hip_stream);
 }

@@ -1,0 +1,164 @@
+// Kept tokens of every sequence moved together, in place or into fresh pages.
+//
+// Token i of a sequence's list goes to place first + i.  A page's moved codes come from pages of other scales: the new scale
+// is the smallest that holds their largest value (and at least the old one where the page keeps tokens before them), and every
+// code is multiplied by old over new scale, powers of two: exact but for what falls under e4m3's smallest normal number.
+//
+// In place one workgroup takes a sequence's pages of one head in order: a list is ascending, so no place is written before
+// what it held has been read.  Into fresh pages every page is a workgroup's own.  Bound by memory: codes read and written
+// once.  A thread holds 16 codes of a token.
+#include <algorithm>
+
+#include "cache.h"
+#include "cache_codes.h"
+#include "hsap_internal.h"
+
+namespace hsap {
+
+hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c);
+
+struct CompactArgs {
+  hsap_cache_desc d;
+  hsap_cache c;
+  const int32_t* keep;
+  const int32_t* cu;
+  int64_t total;
+  const int32_t* first;  // may be NULL: 0
+  const int32_t* dst_table;
+  int32_t* new_lens;  // may be NULL
+};
+
+// Largest finite magnitude of 16 codes (times their scale, which is positive).
+__device__ __forceinline__ float codes_max(const uint4& w) {
+  const uint32_t c[4] = {w.x, w.y, w.z, w.w};
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+    // (fmaxf takes the other operand of a NaN)
+    m = fmaxf(fmaxf(m, fabsf(lo[0])), fmaxf(fabsf(lo[1]), fmaxf(fabsf(hi[0]), fabsf(hi[1]))));
+  }
+  return m;
+}
+
+// PER: units of 16 codes of a page per thread.
+template <int D, int PER, bool FRESH>
+__global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs a) {
+  constexpr int UNITS = D / 16;
+  __shared__ float wave_max[4], old_scale;
+  const int tid = threadIdx.x;
+  const bool is_v = blockIdx.x & 1;
+  const int32_t pair = (int32_t)(blockIdx.x >> 1);
+  const int h = pair % a.d.heads_kv;
+  const int64_t item = pair / a.d.heads_kv;
+  const int32_t ps = a.d.page_size;
+  int32_t s = 0;
+  if constexpr (FRESH) {
+    int32_t r = a.d.num_seqs;
+    while (r - s > 1) {
+      const int32_t mid = (s + r) >> 1;
+      if (item_base(a.cu[mid], 1, ps, 2, mid) <= item) s = mid;
+      else r = mid;
+    }
+  } else {
+    s = (int32_t)item;
+  }
+  const int32_t i0 = a.cu[s];
+  const int64_t count = min((int64_t)a.cu[s + 1], a.total) - i0;
+  const int32_t first = a.first ? max(a.first[s], 0) : 0;
+  const int64_t nth = FRESH ? item - item_base(i0, 1, ps, 2, s) : 0;  // page of the list's
+  if (a.new_lens && h == 0 && !is_v && nth == 0 && tid == 0) a.new_lens[s] = first + (int32_t)max(count, (int64_t)0);
+  if (count <= 0) return;
+  const int32_t* row = a.c.page_table + (int64_t)s * a.d.table_width;
+  const int32_t* out_row = FRESH ? a.dst_table + (int64_t)s * a.d.table_width : row;
+  uint8_t* all = is_v ? a.c.v_codes : a.c.k_codes;
+  float* scales = is_v ? a.c.v_scale : a.c.k_scale;
+  const int64_t end = (int64_t)first + count;
+  int64_t at = first / ps + nth;
+  for (int64_t lo = max((int64_t)first, at * ps); lo < end; lo = ++at * ps) {
+    const int64_t hi = min(end, (at + 1) * ps);
+    const int32_t page = lo <= INT32_MAX ? cache_page(out_row, a.d.table_width, a.d.num_pages, ps, (int32_t)lo) : -1;
+    const int32_t slot0 = (int32_t)(lo - at * ps), units = (int32_t)(hi - lo) * UNITS;
+    uint4 w[PER];
+    float scale[PER], amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int unit = tid + 256 * i;
+      w[i] = uint4{0, 0, 0, 0};
+      scale[i] = 0.f;
+      if (unit < units) {
+        const int32_t src = a.keep[i0 + (lo - first) + unit / UNITS];
+        const int32_t from = cache_page(row, a.d.table_width, a.d.num_pages, ps, src);
+        if (from >= 0) {
+          scale[i] = scales[(int64_t)from * a.d.heads_kv + h];
+          w[i] = *(const uint4*)(all + cache_row(from, a.d.heads_kv, h, ps, src & (ps - 1), D) + 16 * (unit % UNITS));
+        }
+        amax = fmaxf(amax, codes_max(w[i]) * scale[i]);
+      }
+    }
+    if (page >= 0 && tid == 0) old_scale = slot0 > 0 ? scales[(int64_t)page * a.d.heads_kv + h] : 0.f;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+    if ((tid & 63) == 0) wave_max[tid >> 6] = amax;
+    __syncthreads();  // (everything that this page's places held has been read)
+    amax = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+    float inv, ratio;
+    const float now = page_scale(amax, slot0 > 0, old_scale, inv, ratio);
+    __syncthreads();
+    if (page >= 0) {
+      uint8_t* codes = all + cache_row(page, a.d.heads_kv, h, ps, 0, D);
+      if (ratio != 1.f)
+        for (int e = tid; e < slot0 * UNITS; e += 256) recode16(codes + 16 * e, ratio);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int unit = tid + 256 * i;
+        if (unit < units) {
+          // (a code that is not 0 has at most 448 2^9 times the new scale; a page of zeros may have had any)
+          const float by = fminf(scale[i] * inv, 0x1p20f);
+          *(uint4*)(codes + (slot0 * UNITS + unit) * 16) = by == 1.f ? w[i] : recoded16(w[i], by);
+        }
+      }
+      if (tid == 0) scales[(int64_t)page * a.d.heads_kv + h] = now;
+    }
+    if (FRESH) break;
+  }
+}
+
+template <int D, bool FRESH>
+static void launch_compact(const CompactArgs& a, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(256);
+  const int per = a.d.page_size * (D / 16) / 256;
+  if (per <= 1) hipLaunchKernelGGL((cache_compact_kernel<D, 1, FRESH>), grid, block, 0, s, a);
+  else if (per == 2) hipLaunchKernelGGL((cache_compact_kernel<D, 2, FRESH>), grid, block, 0, s, a);
+  else if constexpr (D == 128) hipLaunchKernelGGL((cache_compact_kernel<D, 4, FRESH>), grid, block, 0, s, a);
+}
+
+}  // namespace hsap
+
+using namespace hsap;
+
+extern "C" hsap_status hsap_cache_compact(const hsap_cache_desc* desc, const hsap_cache* cache, const int32_t* keep,
+                                          const int32_t* cu_keep, int64_t total_keep, const int32_t* first, const int32_t* dst_table,
+                                          int32_t* new_lens, void* hip_stream) {
+  clear_error();
+  const hsap_status st = check_cache(desc, cache);
+  if (st != HSAP_OK) return st;
+  if (total_keep < 0 || total_keep > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_keep %lld", (long long)total_keep);
+  if (desc->num_seqs == 0) return HSAP_OK;
+  if (!cu_keep || (total_keep && !keep)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
+  CompactArgs a{*desc, *cache, keep, cu_keep, total_keep, first, dst_table, new_lens};
+  const int64_t items = dst_table ? item_base(total_keep, 1, desc->page_size, 2, desc->num_seqs) : desc->num_seqs;
+  const int64_t blocks = items * desc->heads_kv * 2;
+  if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens x heads");
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (dst_table) {
+    if (desc->head_dim == 128) launch_compact<128, true>(a, blocks, s);
+    else launch_compact<64, true>(a, blocks, s);
+  } else {
+    if (desc->head_dim == 128) launch_compact<128, false>(a, blocks, s);
+    else launch_compact<64, false>(a, blocks, s);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "cache_compact launch: %s", hipGetErrorString(e));
+  return HSAP_OK;
+}

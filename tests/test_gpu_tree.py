@@ -1,0 +1,430 @@
+"""Trees of drafted tokens over the paged cache on the GPU: masks and positions exactly, attention within the oracle's derived
+bounds; ragged, idle and empty sequences, long trees, any masks, windows, unseen and bad places, both kernels and split
+contexts, replays, streams, and the run of a serving step that drafts, verifies and goes on."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as C
+from oracle import pages as P
+from oracle import tree as T
+from paper_2606_30460_amd import _lib as L
+from test_gpu_cache import Pages, _bits, _cos_sin
+
+pytestmark = pytest.mark.gpu
+
+
+def _parents(new, rng, chain=False):
+    return np.array([j - 1 if chain else rng.integers(max(-1, j - 6), j) for n in new for j in range(int(n))], dtype=np.int32)
+
+
+def _cu(new):
+    return np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _masks(parents, cu, lens, words, pad=0):
+    n = int(cu[-1])
+    mask = torch.full((n + pad, words), 7, dtype=torch.int64, device="cuda")
+    positions = torch.full((n + pad,), 7, dtype=torch.int32, device="cuda")
+    up = np.concatenate([parents, np.zeros(pad, np.int32)]).astype(np.int32)
+    L.tree_masks(_dev(np.asarray(lens, np.int32)), _dev(cu), _dev(up), mask, positions)
+    torch.cuda.synchronize()
+    return mask, positions
+
+
+@pytest.mark.parametrize("new,words", [([1], 1), ([5, 0, 64, 1], 1), ([65, 3], 2), ([200, 128, 129, 1], 4), ([1024, 700], 16), ([70, 64], 1),
+                                       ([300], 3)])
+def test_masks(new, words):
+    print(new, words, flush=True)
+    rng = np.random.default_rng(len(new))
+    for chain in (False, True):
+        parents, cu, lens = _parents(new, rng, chain), _cu(new), np.asarray(new) + 1000 * np.arange(len(new))
+        bad = rng.random(len(parents)) < 0.05            # none: its own number, a later one, far below 0
+        parents[bad] = rng.choice([2 ** 31 - 1, 1024, -2 ** 31], int(bad.sum()))
+        mask, positions = _masks(parents, cu, lens, words, pad=3)
+        named, place = T.masks(parents, cu, lens, words)
+        assert np.array_equal(_bits(mask)[:-3], T.words_of(named)) and np.array_equal(_bits(positions)[:-3], place)
+        assert bool((mask[-3:] == 7).all()) and bool((positions[-3:] == 7).all())
+
+
+def test_masks_of_one_token_each():
+    lens = torch.tensor([5, 1, 0, 2 ** 31 - 1, 77], dtype=torch.int32, device="cuda")
+    mask = torch.full((5, 2), 9, dtype=torch.int64, device="cuda")
+    positions = torch.empty(5, dtype=torch.int32, device="cuda")
+    L.tree_masks(lens, None, None, mask, positions)
+    torch.cuda.synchronize()
+    assert mask.tolist() == [[1, 0]] * 5 and positions.tolist() == [4, 0, -1, 2 ** 31 - 2, 76]
+
+
+def _check(held, new, size, hq, hkv, d, window=L.MAX_WINDOW, sinks=0, seed=0, pad=0, width=None, pages=None, scale=None, strided=False,
+           lse=True, chain=False, named=None, positions=None, words=None, one=False, fill=True):
+    held, new = np.asarray(held), np.asarray(new)
+    lens = held + new
+    p = pages or Pages(np.maximum(lens, 0), size, hkv, d, seed, width=width).fill(np.maximum(lens, 0), seed + 1)
+    n, cu = int(new.sum()), _cu(new)
+    rng = np.random.default_rng(seed)
+    words = words or max(1, -(-int(new.max()) // 64))
+    if named is None:
+        named, place = T.masks(_parents(new, rng, chain), cu, lens, words)
+        positions = place if positions is None else positions
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randn(n + pad, hq + (3 if strided else 0), d, generator=g).to(torch.bfloat16).cuda()
+    q = q[:, 1:1 + hq] if strided else q
+    cache = p.device(lens)
+    o = torch.full((n + pad, hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ls = torch.full((hq, n + pad), 7.0, device="cuda") if lse else None
+    ws = torch.full((L.cache_tree_attn_workspace(cache, hq, n + pad),), 0xFF, dtype=torch.uint8, device="cuda")
+    scale = scale or 1 / math.sqrt(d)
+    mask = _dev(np.concatenate([T.words_of(named), np.full((pad, words), -1)]).astype(np.int64))
+    at = _dev(np.concatenate([positions, np.full(pad, 5)]).astype(np.int32))
+    L.cache_tree_attn(cache, hq, scale, q, None if one else _dev(cu), mask, at, o, ls, ws, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    want, tol, want_l, tol_l = T.attention(q[:n].float().double().cpu().numpy(), p.codes["k"], p.scales["k"], p.codes["v"],
+                                           p.scales["v"], p.table, lens, cu, named, positions, window, sinks, scale)
+    err = np.abs(o[:n].float().cpu().numpy() - want)
+    assert (err <= tol + 1e-9).all(), float(np.nanmax(err / (tol + 1e-9)))
+    assert bool((o[n:] == 7.0).all())
+    if lse:
+        got = ls.cpu().numpy()
+        none = np.isinf(want_l)
+        assert np.array_equal(got[:, :n][none], want_l[none])
+        assert (np.abs(got[:, :n] - np.where(none, 0, want_l))[~none] <= tol_l[~none]).all()
+        assert (got[:, n:] == 7.0).all()
+    return o
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [16, 32, 64, 128])
+def test_ragged(size, d):
+    print(size, d, flush=True)
+    held = [0, 1, 15, 16, 17, 31, 33, 100, 129, 600, 50]
+    new = [1, 2, 16, 7, 40, 1, 64, 65, 0, 24, 3]
+    _check(held, new, size, 8, 2, d, seed=size, pad=3)
+    _check(held, new, size, 3, 3, d, seed=size + 1, strided=True, lse=False)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 1), (16, 1), (40, 1), (24, 8), (6, 3)])
+def test_groups(hq, hkv):
+    print(hq, hkv, flush=True)
+    _check([70, 300], [12, 3], 32, hq, hkv, 128, seed=hq)
+    _check([70, 300], [1, 33], 32, hq, hkv, 64, seed=hq)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (3, 2), (16, 4), (33, 40), (100, 0), (1000, 5), (50, 1000)])
+def test_windows_and_sinks(window, sinks):
+    print(window, sinks, flush=True)
+    _check([1, 40, 130, 333, 700, 2], [5, 30, 64, 9, 1, 20], 16, 4, 1, 64, window, sinks, seed=window)
+    _check([10, 40, 130, 333, 700], [10, 1, 0, 50, 129], 64, 4, 2, 128, window, sinks, pad=1, seed=sinks, chain=True)
+    # more drafted tokens than a window: some do not see their path's beginning
+    _check([30, 5], [200, 90], 32, 2, 2, 64, window, sinks, chain=True, seed=4)
+
+
+def test_one_token_each():
+    held = np.array([0, 1, 16, 40, 130, 333, 700, -1])
+    for one in (True, False):
+        _check(held, np.ones(8, int), 16, 4, 2, 64, 50, 3, one=one, seed=1)
+        _check(held, np.ones(8, int), 64, 40, 2, 128, one=one, seed=2, width=30)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_split_contexts(d):
+    print(d, flush=True)
+    _check([5000], [8], 64, 4, 2, d, seed=1)
+    _check([4097, 1, 300], [5, 1, 70], 16, 8, 2, d, seed=2)
+    _check([3000], [20], 128, 4, 1, d, window=700, sinks=4, seed=3, width=100)
+
+
+CHUNKS = [([700, 77, 300, 0, 130], [120, 5, 64, 0, 130]), ([3000, 5], [200, 9])]
+
+
+@pytest.mark.parametrize("d,size", [(64, 16), (64, 64), (128, 32), (128, 128)])
+@pytest.mark.parametrize("held,new", CHUNKS)
+@pytest.mark.parametrize("window,sinks", [(L.MAX_WINDOW, 0), (1, 0), (70, 3), (500, 17)])
+def test_many_rows(held, new, window, sinks, d, size):
+    print(held, window, sinks, d, size, flush=True)
+    _check(held, new, size, 16, 8, d, window, sinks, width=12800 // size, pad=3, strided=size == 64, seed=size)
+
+
+def test_many_rows_in_one_part():
+    _check([100, 250], [200, 312], 32, 128, 8, 64, window=100, sinks=5, width=32)
+
+
+def _random(held, new, words, rng, dead=0.2):
+    """Masks of any bits and positions of any order, some below 0 (named by nobody)."""
+    n = int(np.sum(new))
+    named = rng.random((n, 64 * words)) < rng.choice([0.0, 0.1, 0.5, 1.0], (n, 1))
+    positions = np.repeat(held, new) + rng.integers(0, 60, n)
+    gone = rng.random(n) < dead
+    positions[gone] = -rng.integers(1, 100, int(gone.sum()))
+    at = 0
+    for m in new:
+        named[at:at + m, :m] &= ~gone[None, at:at + m][:, :64 * words]
+        at += m
+    return named, positions
+
+
+@pytest.mark.parametrize("window,sinks", [(L.MAX_WINDOW, 0), (1, 0), (20, 5), (300, 0)])
+@pytest.mark.parametrize("held,new,size,hq,hkv,d,width", [
+    ([0, 3, 200, 77], [20, 64, 1, 50], 16, 4, 2, 64, None), ([0, 3, 200, 77], [20, 64, 1, 50], 64, 4, 2, 128, None),
+    ([500, 0, 90], [100, 60, 128], 32, 16, 8, 128, 400), ([500, 0, 90], [100, 60, 128], 16, 16, 8, 64, 800)])
+def test_any_masks_and_positions(held, new, size, hq, hkv, d, width, window, sinks):
+    print(held, new, size, d, width, window, flush=True)
+    words = 2
+    named, positions = _random(held, new, words, np.random.default_rng(size), 0.2)
+    _check(held, new, size, hq, hkv, d, window, sinks, named=named, positions=positions, words=words, width=width, seed=3)
+
+
+def test_more_drafted_tokens_than_the_mask_names():
+    named, positions = T.masks(_parents([100, 70], np.random.default_rng(0), True), [0, 100, 170], [150, 90], 1)
+    _check([50, 20], [100, 70], 16, 4, 2, 64, named=named, positions=positions, words=1)
+
+
+def test_rows_without_anything():
+    for d, hq, width in ((64, 2, None), (128, 16, 800)):
+        new = [64, 70]
+        named, positions = np.zeros((134, 128), bool), np.zeros(134, np.int64)
+        _check([0, 0], new, 16, hq, hq // 2, d, named=named, positions=positions, words=2, width=width)     # no bits
+        named[:] = True
+        _check([30, 0], new, 16, hq, hq // 2, d, named=named & False, positions=positions - 1, words=2, width=width)  # no positions
+    _check([-3, 5], [5, 3], 16, 4, 2, 64)           # more drafted tokens than tokens: the first have no place
+
+
+def test_more_tokens_than_the_table():
+    p = Pages([64], 16, 1, 64, seed=2).fill([64])
+    _check([50], [30], 16, 2, 1, 64, pages=p)
+    _check([70], [30], 16, 2, 1, 64, pages=p)
+
+
+def test_bad_pages():
+    p = Pages([300, 200], 16, 2, 64, seed=9).fill([300, 200])
+    p.table[0, 2:12] = [2 ** 31 - 1, -2 ** 31, -5, 10 ** 6] * 2 + [-1, -1]        # handed back by the window
+    _check([280, 180], [20, 20], 16, 4, 2, 64, window=50, sinks=20, pages=p)
+    p.table[1, 4], p.table[1, 11] = 10 ** 6, -1                                   # no pages: before the drafts and among them
+    _check([280, 180], [20, 20], 16, 4, 2, 64, pages=p)
+
+
+def test_other_scales():
+    for d, size, width in ((64, 16, None), (128, 64, 200)):
+        p = Pages([260, 190], size, 8, d, seed=15, width=width).fill([260, 190])
+        rng = np.random.default_rng(1)
+        for x in "kv":
+            p.scales[x] *= rng.uniform(0.3, 3.0, p.scales[x].shape).astype(np.float32)
+        _check([200, 90], [60, 100], size, 16, 8, d, pages=p, seed=15)
+
+
+@pytest.mark.parametrize("d,size,width", [(64, 16, None), (128, 64, None), (64, 16, 800), (128, 64, 200)])
+@pytest.mark.parametrize("window,sinks", [(L.MAX_WINDOW, 0), (20, 0), (40, 17)])
+def test_places_that_no_row_sees_may_hold_anything(window, sinks, d, size, width):
+    # NaN codes and scales where no row sees a token, drafted ones that nobody names among them
+    print(window, sinks, d, size, width, flush=True)
+    held, new, hq, hkv = np.array([300, 77, 3, 160]), np.array([70, 64, 5, 60]), 16, 8
+    lens, cu = held + new, _cu(new)
+    named, positions = _random(held, new, 2, np.random.default_rng(1), 0.3)
+    at = 0
+    for m in new:                                 # whole stretches of drafted tokens that nobody names
+        named[at:at + m, m // 4:m // 2 + 20] = False
+        at += m
+    got = []
+    for poison in (False, True):
+        p = Pages(lens, size, hkv, d, seed=size, width=width).fill(lens)
+        for s, n in enumerate(lens if poison else []):
+            seen = np.zeros(n, bool)
+            for t in range(cu[s], cu[s + 1]):
+                # (a token that a mask names is finite, whatever the window)
+                seen[T.visible(n, new[s], named, positions, cu[s], t, window, sinks, 10 ** 9)] = True
+                seen[held[s]:] |= named[t, :new[s]] if positions[t] >= -10 ** 9 else False
+            for page in range(-(-n // size)):
+                here = seen[page * size:(page + 1) * size]
+                for x in "kv":
+                    if not here.any():
+                        p.scales[x][p.table[s, page]] = np.nan
+                    p.codes[x][p.table[s, page], :, np.flatnonzero(~here)] = 0xFF
+        cache = p.device(lens)
+        q = torch.randn(int(cu[-1]), hq, d, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+        o = torch.empty_like(q)
+        ws = torch.empty(L.cache_tree_attn_workspace(cache, hq, len(q)), dtype=torch.uint8, device="cuda")
+        L.cache_tree_attn(cache, hq, 0.1, q, _dev(cu), _dev(T.words_of(named)), _dev(positions.astype(np.int32)), o, None, ws,
+                          window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        got.append(o)
+    assert torch.equal(got[0], got[1]) and bool(torch.isfinite(got[0]).all())
+
+
+def test_large_scores():
+    p = Pages([90], 16, 1, 64, seed=5).fill([90], spread=4.0)
+    _check([70], [20], 16, 4, 1, 64, pages=p, seed=5)
+    _check([70], [20], 16, 4, 1, 64, seed=6, scale=1.5)
+
+
+def test_a_chain_is_the_causal_attention():
+    """Bit for bit, where both take the same kernel."""
+    for held, new, hq, hkv, d, width in (([300, 40], [9, 30], 8, 2, 128, None), ([500, 90], [150, 100], 16, 8, 64, 800)):
+        lens, cu = np.add(held, new), _cu(new)
+        p = Pages(lens, 16, hkv, d, seed=1, width=width).fill(lens)
+        cache = p.device(lens)
+        n = int(cu[-1])
+        q = torch.randn(n, hq, d, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+        outs = [(torch.empty_like(q), torch.empty(hq, n, device="cuda")) for _ in range(2)]
+        ws = torch.empty(L.cache_tree_attn_workspace(cache, hq, n), dtype=torch.uint8, device="cuda")
+        for window, sinks in ((L.MAX_WINDOW, 0), (37, 4)):
+            mask, positions = _masks(_parents(new, None, True), cu, lens, 3)
+            L.cache_attn(cache, hq, 0.1, q, _dev(cu), *outs[0], ws, window=window, sinks=sinks)
+            L.cache_tree_attn(cache, hq, 0.1, q, _dev(cu), mask, positions, *outs[1], ws, window=window, sinks=sinks)
+            torch.cuda.synchronize()
+            want, tol, _, _ = C.attention(q.float().double().cpu().numpy(), p.codes["k"], p.scales["k"], p.codes["v"], p.scales["v"],
+                                          p.table, lens, cu, window, sinks, 0.1)
+            for o, _ in outs:
+                assert (np.abs(o.float().cpu().numpy() - want) <= tol + 1e-9).all()
+
+
+def test_replays_follow_masks_and_lengths():
+    held, hq, hkv, d = np.array([700, 90, 400]), 8, 2, 128
+    p = Pages(held + 60, 32, hkv, d, seed=11, spare=0).fill(held + 60)
+    cache = p.device(held + 20)
+    n, most = 40, 64
+    new = [np.array([20, 15, 5]), np.array([1, 39, 0]), np.array([13, 13, 14])]
+    cu, parents = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    q = torch.randn(n, hq, d, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    ws = torch.empty(L.cache_tree_attn_workspace(cache, hq, n), dtype=torch.uint8, device="cuda")
+    out = {x: torch.zeros(*shape, dtype=dt, device="cuda") for x, shape, dt in (
+        ("mask", (n, 1), torch.int64), ("positions", (n,), torch.int32), ("o", (n, hq, d), torch.bfloat16), ("lse", (hq, n), torch.float32))}
+
+    def step():
+        L.tree_masks(cache.seq_lens, cu, parents, out["mask"], out["positions"])
+        L.cache_tree_attn(cache, hq, 0.1, q, cu, out["mask"], out["positions"], out["o"], out["lse"], ws, window=300, sinks=4)
+
+    def load(turn):
+        cu.copy_(torch.from_numpy(_cu(new[turn])))
+        parents[:int(new[turn].sum())] = torch.from_numpy(_parents(new[turn], np.random.default_rng(turn))).cuda()
+        cache.seq_lens.copy_(torch.from_numpy((held + new[turn]).astype(np.int32)))
+
+    load(0)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in (0, 1, 2, 1):
+        load(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {x: t.clone() for x, t in out.items()}
+        step()
+        torch.cuda.synchronize()
+        m = int(new[turn].sum())
+        for x, t in out.items():
+            a, b = (got[x][:, :m], t[:, :m]) if x == "lse" else (got[x][:m], t[:m])
+            assert torch.equal(a, b), (turn, x)
+
+
+def test_two_streams():
+    """Calls on two streams, each with its own workspace."""
+    held, new, hq, hkv, d = np.array([3000, 500]), np.array([20, 33]), 8, 2, 128
+    p = Pages(held + new, 64, hkv, d, seed=3).fill(held + new)
+    cache, cu = p.device(), _cu(new)
+    mask, positions = _masks(_parents(new, np.random.default_rng(0)), cu, held + new, 1)
+    q = [torch.randn(53, hq, d, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).cuda() for i in range(2)]
+    size, cu = L.cache_tree_attn_workspace(cache, hq, 53), _dev(cu)
+    want = []
+    for x in q:
+        o = torch.empty_like(x)
+        L.cache_tree_attn(cache, hq, 0.1, x, cu, mask, positions, o, None, torch.empty(size, dtype=torch.uint8, device="cuda"))
+        want.append(o)
+    torch.cuda.synchronize()
+    streams, ws = [torch.cuda.Stream() for _ in q], [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in q]
+    got = [torch.empty_like(x) for x in q]
+    for _ in range(5):
+        for st, x, o, w in zip(streams, q, got, ws):
+            L.cache_tree_attn(cache, hq, 0.1, x, cu, mask, positions, o, None, w, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_drafting_run():
+    """A server's steps: prompts into pages, each with three branches; every step drafts a tree per branch, appends it at its
+    positions, verifies it, keeps an accepted path and gives the rest of its pages back."""
+    hq, hkv, d, size, layers, steps = 4, 2, 64, 16, 2, 5
+    rows, prompts = 6, np.array([37, 0, 0, 52, 0, 0])
+    source = np.array([0, 0, 0, 3, 3, 3])
+    num, width = 60, 12
+    g, rng = torch.Generator().manual_seed(0), np.random.default_rng(0)
+    table, refs = torch.full((rows, width), -1, dtype=torch.int32, device="cuda"), torch.zeros(num, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    caches = [L.KVCache(torch.full((num, hkv, size, d), 0x7F, dtype=torch.uint8, device="cuda"),
+                        torch.full((num, hkv, size, d), 0x7F, dtype=torch.uint8, device="cuda"),
+                        torch.full((num, hkv), float("nan"), device="cuda"), torch.full((num, hkv), float("nan"), device="cuda"),
+                        table, lens) for _ in range(layers)]
+    rotation = L.Rotation(_cos_sin(300, d), np.arange(d // 2) % 3)
+    pairs, missing = torch.empty(rows, 2, dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+
+    def reserve(cu, total):
+        ws = torch.empty(L.pages_reserve_workspace(caches[0], total), dtype=torch.uint8, device="cuda")
+        L.pages_reserve(caches[0], refs, cu, total, pairs, missing, ws)
+        for c in caches:
+            L.cache_copy_pages(c, pairs)
+
+    def tokens(n):
+        return torch.randn(n, hq + 2 * hkv, d, generator=g).to(torch.bfloat16).cuda()
+
+    # what every row's tokens are, per layer: dequantised at each append, moved along with the rows
+    cu = _cu(prompts)
+    lens.copy_(torch.from_numpy(prompts.astype(np.int32)))
+    reserve(_dev(cu), int(cu[-1]))
+    place = torch.from_numpy(np.concatenate([np.arange(n) for n in prompts]).astype(np.int32)).cuda()
+    for c in caches:
+        x = tokens(int(cu[-1]))
+        L.cache_append_at(c, x[:, hq:hq + hkv], x[:, hq + hkv:], _dev(cu), rotation, torch.stack([place] * 3))
+    L.pages_fork(caches[0], refs, _dev(source.astype(np.int32)))
+    committed = prompts[source]
+    assert lens.tolist() == committed.tolist()
+    for step in range(steps):
+        new = rng.integers(1, 20, rows)
+        cu, total = _cu(new), int(new.sum())
+        parents = _parents(new, rng)
+        lens.copy_(torch.from_numpy((committed + new).astype(np.int32)))
+        reserve(_dev(cu), total)
+        assert int(missing) == 0
+        mask = torch.empty(total, 1, dtype=torch.int64, device="cuda")
+        positions = torch.empty(total, dtype=torch.int32, device="cuda")
+        L.tree_masks(lens, _dev(cu), _dev(parents), mask, positions)
+        named, at = T.masks(parents, cu, committed + new, 1)
+        for c in caches:
+            x, q = tokens(total), torch.empty(total, hq, d, dtype=torch.bfloat16, device="cuda")
+            L.cache_append_at(c, x[:, hq:hq + hkv], x[:, hq + hkv:], _dev(cu), rotation, torch.stack([positions] * 3), q=x[:, :hq],
+                              q_out=q)
+            o, lse = torch.empty_like(q), torch.empty(hq, total, device="cuda")
+            ws = torch.empty(L.cache_tree_attn_workspace(c, hq, total), dtype=torch.uint8, device="cuda")
+            L.cache_tree_attn(c, hq, 0.125, q, _dev(cu), mask, positions, o, lse, ws)
+            torch.cuda.synchronize()
+            codes = [_bits(t) for t in c.tensors[:4]]
+            want, tol, want_l, tol_l = T.attention(q.float().double().cpu().numpy(), codes[0], codes[2], codes[1], codes[3],
+                                                   _bits(table), committed + new, cu, named, at, 2 ** 31 - 1, 0, 0.125)
+            assert (np.abs(o.float().cpu().numpy() - want) <= tol + 1e-9).all(), step
+            assert (np.abs(lse.cpu().numpy() - want_l) <= tol_l).all(), step
+        # one path of every tree is accepted
+        kept = [np.flatnonzero(named[rng.integers(cu[s], cu[s + 1])]) for s in range(rows)]
+        count = np.array([len(k) for k in kept])
+        keep = np.concatenate([committed[s] + k for s, k in enumerate(kept)]).astype(np.int32)
+        first, cu_keep = _dev(committed.astype(np.int32)), _dev(_cu(count))
+        before = [[_bits(t).copy() for t in c.tensors[:4]] for c in caches]
+        for i, c in enumerate(caches):
+            L.cache_compact(c, _dev(keep), cu_keep, first=first, new_lens=lens if i == layers - 1 else None)
+        torch.cuda.synchronize()
+        for c, (ck, cv, sk, sv) in zip(caches, before):
+            for codes, scales, a, b in ((ck, sk, c.k_codes, c.k_scale), (cv, sv, c.v_codes, c.v_scale)):
+                P.compact(codes, scales, _bits(table), _bits(table), keep, _cu(count), committed)
+                assert np.array_equal(_bits(a), codes) and np.array_equal(_bits(b), scales, equal_nan=True), step
+        committed = committed + count
+        assert lens.tolist() == committed.tolist()
+        # rows of a prompt go on from its first now and then, else pages behind the lengths are given back
+        to = source if step % 2 else np.arange(rows)
+        L.pages_fork(caches[0], refs, _dev(to.astype(np.int32)) if step % 2 else None)
+        committed = committed[to]
+        t, r = _bits(table), _bits(refs)
+        assert np.array_equal(r, P.counts(t, num)) and lens.tolist() == committed.tolist()
+        assert [(x >= 0).sum() for x in t] == [-(-n // size) for n in committed]
