@@ -17,115 +17,13 @@
 // and turned in registers, two codes of two tokens at a time (v_perm, then the conversion to bf16, which e4m3 fits
 // exactly).  P is rounded to bf16 for the second product (2^-8 relative at most, summed in fp32), O once at the end.
 #include <algorithm>
-#include <type_traits>
 
-#include "cache.h"
-#include "hsap_internal.h"
-#include "mfma.h"
-#include "window.h"
+#include "cache_attn.h"
 
 namespace hsap {
 
 hsap_status check_cache_desc(const hsap_cache_desc* d, bool pages);
 hsap_status check_cache(const hsap_cache_desc* d, const hsap_cache* c);
-
-struct CacheAttnArgs {
-  hsap_cache_desc d;
-  hsap_cache c;
-  const __bf16* q;
-  int64_t q_stride;
-  const int32_t* cu;
-  int64_t total_q;
-  __bf16* o;
-  float* lse;      // may be NULL
-  float* part_o;   // [splits, total_q, Hq, d], normalised
-  float* part_lse; // [splits, total_q, Hq], log2 units
-  int32_t heads_q;
-  int32_t group;
-  int32_t page_shift;  // log2 of the page size
-  int32_t window;
-  int32_t sinks;
-  int32_t splits;
-  float scale_log2;
-  const uint64_t* mask;      // TREE kernels: [total_q, words]
-  const int32_t* positions;  // TREE kernels: [total_q]
-  int32_t words;
-};
-
-// Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
-__device__ __forceinline__ int32_t steps_per_split(int32_t total, int32_t splits) { return (total + splits - 1) / splits; }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// four e4m3 codes times a power of two to bf16 (exact within bf16's range)
-__device__ __forceinline__ void decode4(uint32_t w, float pow2, bf16x2& lo, bf16x2& hi) {
-  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, false);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, true);
-}
-
-__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-// The sequence, first row and rows of a row tile; false where the tile is empty.
-struct RowTile {
-  int32_t seq, t0, count, row0;  // row0: first row (token * group + head) of the tile within the sequence
-};
-__device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, int rows, RowTile& t) {
-  if (!a.cu) {
-    const int32_t per = (a.group + rows - 1) / rows;
-    t.seq = tile / per;
-    t.t0 = t.seq;
-    t.count = 1;
-    t.row0 = (tile - t.seq * per) * rows;
-    return t.seq < a.d.num_seqs;
-  }
-  int32_t s = 0, r = a.d.num_seqs;
-  while (r - s > 1) {
-    const int32_t mid = (s + r) >> 1;
-    if (item_base(a.cu[mid], a.group, rows, 1, mid) <= tile) s = mid;
-    else r = mid;
-  }
-  t.seq = s;
-  t.t0 = a.cu[s];
-  t.count = (int32_t)min((int64_t)a.cu[s + 1], a.total_q) - t.t0;
-  const int64_t row0 = (tile - item_base(t.t0, a.group, rows, 1, s)) * rows;
-  t.row0 = (int32_t)row0;
-  return t.count > 0 && row0 < (int64_t)t.count * a.group;
-}
-
-// Trees.  A row sees the tokens before the drafted ones, from `base` places on, by its position (window, sinks) and the
-// drafted ones that its mask names.  Bits of drafted tokens from .. from + 63 (from may be below 0) of a row's mask:
-__device__ __forceinline__ uint64_t mask_bits(const uint64_t* mask, int32_t words, int32_t from) {
-  if (from <= -64) return 0;
-  if (from < 0) return mask[0] << -from;
-  const int32_t w = from >> 6, sh = from & 63;
-  uint64_t x = w < words ? mask[w] >> sh : 0;
-  if (sh && w + 1 < words) x |= mask[w + 1] << (64 - sh);
-  return x;
-}
-// Position of drafted token x of the sequence whose first is t0 (x may be any number: it is not used then).
-__device__ __forceinline__ int32_t drafted_position(const CacheAttnArgs& a, const RowTile& rt, int32_t x) {
-  return a.positions[rt.t0 + min(max(x, 0), rt.count - 1)];
-}
-// Least and largest position of the rows that see anything (a position below 0 sees nothing): over the lanes that differ in
-// the bits of LANES.
-template <int LANES>
-__device__ __forceinline__ void position_range(int32_t& lo, int32_t& hi) {
-#pragma unroll
-  for (int o = 1; o < LANES; o <<= 1) {
-    lo = min(lo, __shfl_xor(lo, o));
-    hi = max(hi, __shfl_xor(hi, o));
-  }
-}
-// Steps of a tile whose rows' positions are plo .. phi (none: phi < 0): the sinks', then from the first window, or from the
-// drafted tokens where that is behind them, to the last token.
-template <int STEP>
-__device__ __forceinline__ Steps<STEP> tree_steps(int32_t plo, int32_t phi, int32_t base, int32_t len, int32_t cap, int32_t window,
-                                                  int32_t sinks) {
-  const int64_t most = (int64_t)max(base, 0) + window - 1;
-  return cache_steps<STEP>((int32_t)min((int64_t)plo, most), phi < 0 ? -1 : len - 1, cap, window, sinks);
-}
 
 template <typename T, bool ONCE>
 __device__ __forceinline__ T read_codes(const uint8_t* p) {
@@ -173,6 +71,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     plo = uniform(plo);
     phi = uniform(phi);
   }
+  const bool deep = TREE && drafts_end(a, rt, phi, lane);
   const Steps<32> steps = TREE ? tree_steps<32>(plo, phi, pos0, len, cap, a.window, a.sinks)
                                : cache_steps<32>(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
@@ -277,13 +176,18 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     const int32_t near = s < steps.sinks ? 0 : a.window;
     // every row of the tile sees every token of the step
     const bool all = x.held[0] && x.held[1] && (TREE ? live && jl < pos0 : jl <= plo) && (phi - x.j0 < near || jl < sinks);
-    uint64_t rows[TREE ? 8 : 1] = {};  // rows that see each of the lanes' tokens
-    int32_t drafted[TREE ? 8 : 1];     // and its position, of a drafted one
+    uint32_t sees[TREE ? MT : 1], some = 0;  // the step's tokens that the lane's rows see, that any row does
     if constexpr (TREE) {
-      if (jl >= pos0) {
+      if (__builtin_expect(!all, 0)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          drafted[e] = a.window == INT32_MAX ? 0 : drafted_position(a, rt, x.j0 + 16 * (e >> 2) + 4 * grp + (e & 3) - pos0);
+        for (int mt = 0; mt < MT; ++mt) {
+          const int32_t t = min(rt.row0 + 16 * mt + l16, nrows - 1) / a.group;
+          sees[mt] = (uint32_t)seen_bits(a, rt, a.mask + (int64_t)(rt.t0 + t) * a.words, pos[mt], pos0, x.j0, top, deep, lane);
+          sees[mt] &= (x.held[0] ? 0xFFFFu : 0u) | (x.held[1] ? 0xFFFF0000u : 0u);
+          some |= sees[mt];
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) some |= __shfl_xor(some, o);
       }
     }
     // V's scale: its power of two goes into the conversion of the codes, what is left of it (1 for the scales that an
@@ -304,29 +208,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
 #pragma unroll
         for (int kk = 0; kk < 2 * KX; ++kk) sc[half] = mfma16(kf[half][kk], qf[mt][kk], sc[half]);
       const float sl[2] = {fmaxf(x.ks[0] * a.scale_log2, 1.17549435e-38f), fmaxf(x.ks[1] * a.scale_log2, 1.17549435e-38f)};
-      if (!all) {
-        uint32_t bits = 0;  // the row's mask, of the step's tokens
-        if constexpr (TREE) {
-          if (jl >= pos0) {
-            const int32_t t = min(rt.row0 + 16 * mt + l16, nrows - 1) / a.group;
-            bits = (uint32_t)mask_bits(a.mask + (int64_t)(rt.t0 + t) * a.words, a.words, x.j0 - pos0);
-          }
-        }
+      if (TREE ? __builtin_expect(!all, 0) : !all) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int32_t j = x.j0 + 16 * half + 4 * grp + e;
-            bool see;
-            if constexpr (TREE) {
-              const bool before = j < pos0;
-              const int32_t at = before ? j : drafted[4 * half + e];
-              see = (before | (bits >> (16 * half + 4 * grp + e) & 1)) & (pos[mt] >= 0) & (j <= top) & x.held[half] &
-                    ((a.window == INT32_MAX && near) | (pos[mt] - at < near) | (at < sinks));
-              rows[4 * half + e] |= __builtin_amdgcn_ballot_w64(see);
-            } else {
-              see = j <= pos[mt] && (pos[mt] - j < near || j < sinks) && x.held[half];
-            }
+            const bool see = TREE ? (sees[TREE ? mt : 0] >> (4 * grp)) & (1u << (16 * half + e))
+                                  : j <= pos[mt] && (pos[mt] - j < near || j < sinks) && x.held[half];
             if (!see) sc[half][e] = NEG_INF;
           }
       }
@@ -365,14 +254,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     VT v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) v[y] = x.v[y];
-    if (TREE && !all) {
+    if (TREE && __builtin_expect(!all, 0)) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if ((rows[4 * half + e] >> (16 * grp) & 0xFFFF) == 0) v[4 * half + e] = VT{};
+          if (!((some >> (4 * grp)) & (1u << (16 * half + e)))) v[4 * half + e] = VT{};
         // (of sixteen tokens that no row sees the page's scale may be anything too)
-        if ((rows[4 * half] | rows[4 * half + 1] | rows[4 * half + 2] | rows[4 * half + 3]) == 0) vpow[half] = 1.f;
+        if (!(some & (0xFFFFu << (16 * half)))) vpow[half] = 1.f;
       }
     }
     if (!TREE && (jl > top || !x.held[0] || !x.held[1] || steps.edge(s))) {  // P is 0 there, V whatever the page holds
@@ -506,14 +395,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
 // 32x32x16 products S^T = K Q^T, O^T += V^T P^T with V^T by transpose reads.  P is rounded to bf16 for the second product,
 // as in the window kernels.  2048 rows x 8 heads over 30000 tokens, head_dim 128: 680 us, 765 TFLOP/s (a step's products,
 // exponentials and decoding add up in a wave: matrix cores 0.31 busy).  head_dim 64: three workgroups per CU (185 -> 167 us).
-template <int D, bool TREE>
+template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
   constexpr int KB = 64, CPR = D / 8, TILE = KB * D, ROWS = kChunkRows, U = D / 64;  // U: runs of 16 codes per thread
   constexpr float NEG_INF = -__builtin_inff(), TINY = 1.17549435e-38f;
   constexpr float RESCALE_SLACK = 8.f;
   __shared__ __attribute__((aligned(16))) __bf16 tiles[2][2][TILE];  // [slot][K, V]
   __shared__ __attribute__((aligned(16))) float scales[2][2][4];     // [slot][K's times the softmax's, V's rest][16 tokens]
-  __shared__ uint32_t named[TREE ? 2 * kMaxMaskWords : 1];           // drafted tokens that some row of the tile names
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -527,24 +415,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
   const int32_t nrows = rt.count * a.group;
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
   const int32_t pos0 = len - rt.count;
-  // this lane's query
-  const int32_t row = min(rt.row0 + 32 * w + l32, last_row), tok = row / a.group;
-  int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
-  if constexpr (TREE) {
-    plo = INT32_MAX;
-    phi = -1;
-#pragma unroll
-    for (int r = 0; r < ROWS; r += 64) {
-      const int32_t p = a.positions[rt.t0 + min(rt.row0 + r + lane, last_row) / a.group];
-      plo = min(plo, p < 0 ? INT32_MAX : p);
-      phi = max(phi, p);
-    }
-    position_range<64>(plo, phi);
-    plo = uniform(plo);
-    phi = uniform(phi);
-  }
-  const Steps<KB> steps = TREE ? tree_steps<KB>(plo, phi, pos0, len, cap, a.window, a.sinks)
-                               : cache_steps<KB>(plo, phi, cap, a.window, a.sinks);
+  const int32_t plo = pos0 + rt.row0 / a.group, phi = pos0 + last_row / a.group;
+  const Steps<KB> steps = cache_steps<KB>(plo, phi, cap, a.window, a.sinks);
   const int32_t per = steps_per_split(steps.total, a.splits);
   const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
   if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
@@ -553,30 +425,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       a.part_lse[((int64_t)split * a.total_q + rt.t0 + t) * a.heads_q + g * a.group + (r - t * a.group)] = NEG_INF;
     return;
   }
-  // its position, and the first and last position of the wave's
+  // this lane's query, and the first and last position of the wave's
   const bool busy = rt.row0 + 32 * w <= last_row;
-  const int32_t pos = TREE ? a.positions[rt.t0 + tok] : pos0 + tok;
-  int32_t wlo = pos0 + min(rt.row0 + 32 * w, last_row) / a.group;
-  int32_t whi = pos0 + min(rt.row0 + 32 * w + 31, last_row) / a.group;
-  if constexpr (TREE) {
-    wlo = pos < 0 ? INT32_MAX : pos;
-    whi = pos;
-    position_range<32>(wlo, whi);
-    wlo = uniform(wlo);
-    whi = uniform(whi);
-    // (the first barrier comes before the first of them is read)
-    for (int i = tid; i < 2 * a.words; i += 256) named[i] = 0;
-    __syncthreads();
-    const int32_t first = rt.row0 / a.group, count = last_row / a.group - first + 1;
-    for (int i = tid; i < count * a.words; i += 256) {
-      const int32_t t = i / a.words, x = i - t * a.words;
-      const uint64_t m = a.mask[(int64_t)(rt.t0 + first + t) * a.words + x];
-      if ((uint32_t)m) atomicOr(&named[2 * x], (uint32_t)m);
-      if (m >> 32) atomicOr(&named[2 * x + 1], (uint32_t)(m >> 32));
-    }
-    __syncthreads();
-  }
-  const bool live = !TREE || __builtin_amdgcn_ballot_w64(pos < 0) == 0;
+  const int32_t row = min(rt.row0 + 32 * w + l32, last_row), tok = row / a.group;
+  const int32_t pos = pos0 + tok;
+  const int32_t wlo = pos0 + min(rt.row0 + 32 * w, last_row) / a.group;
+  const int32_t whi = pos0 + min(rt.row0 + 32 * w + 31, last_row) / a.group;
   const int h = g * a.group + (row - tok * a.group);
   bf16x8 qf[D / 16];
   {
@@ -585,7 +439,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
     for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
   }
   const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
-  const int32_t top = min(TREE ? len - 1 : phi, cap - 1);  // last token any row sees
+  const int32_t top = min(phi, cap - 1);  // last token any row sees
 
   // Thread's codes of a step: of the 64 tokens those of 16-token group group_of(u) (one page each), 16 codes of a token.
   auto group_of = [&](int u) { return D == 64 ? w : (w >> 1) + 2 * u; };
@@ -641,9 +495,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       const int token = 16 * group_of(u) + slot_in;
       const int32_t j = steps.first(s) + token;
       float vpow = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
-      bool unseen = j > top || !x.held[u] || (steps.edge(s) && !steps.seen(a.sinks, j, j));
-      if (TREE && j >= pos0) unseen |= j - pos0 >= 64 * a.words || !(named[(j - pos0) >> 5] >> ((j - pos0) & 31) & 1);
-      if (unseen) {  // anything may be there
+      if (j > top || !x.held[u] || (steps.edge(s) && !steps.seen(a.sinks, j, j))) {  // anything may be there
         x.k[u] = x.v[u] = uint4{0, 0, 0, 0};
         vpow = 1.f;
       }
@@ -682,23 +534,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
     const int32_t near = s < steps.sinks ? 0 : a.window;
     const bool held = sl[0] > 0.f && sl[1] > 0.f && sl[2] > 0.f && sl[3] > 0.f;
     // every row of the wave sees every token of the step
-    const bool all = __builtin_amdgcn_ballot_w64(!held) == 0 && (TREE ? live && j0 + KB - 1 < pos0 : j0 + KB - 1 <= wlo) &&
-                     (whi - j0 < near || j0 + KB - 1 < sinks);
-    if (TREE && !all) {
-      const uint64_t bits = j0 + KB > pos0 ? mask_bits(a.mask + (int64_t)(rt.t0 + tok) * a.words, a.words, j0 - pos0) : 0;
-      const bool far = a.window == INT32_MAX && near;
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int32_t x = 32 * nb + c_row(j, hi), t = j0 + x;
-          const bool before = t < pos0;
-          const int32_t at = before || far ? t : drafted_position(a, rt, t - pos0);
-          const bool see = (before | (bits >> x & 1)) & (pos >= 0) & (t <= top) & (sl[2 * nb + (j >> 3)] > 0.f) &
-                           (far | (pos - at < near) | (at < sinks));
-          sc[nb][j] = see ? sc[nb][j] : NEG_INF;
-        }
-    } else if (!all) {
+    const bool all = __builtin_amdgcn_ballot_w64(!held) == 0 && j0 + KB - 1 <= wlo && (whi - j0 < near || j0 + KB - 1 < sinks);
+    if (!all) {
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -762,8 +599,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_kernel(Cache
       if (more) load(s + 1, next, x);
       next = look_up(s + 2);
       const int32_t j0 = steps.first(s);
-      const bool some = s < steps.sinks || j0 + KB - 1 >= max(wlo, 0) - (a.window - 1) || j0 < a.sinks;
-      if (busy && (TREE ? some || j0 + KB > pos0 : j0 <= whi && some)) compute(s, slot);
+      if (busy && j0 <= whi && (s < steps.sinks || j0 + KB - 1 >= max(wlo, 0) - (a.window - 1) || j0 < a.sinks)) compute(s, slot);
       if (more) store(s + 1, x, slot ^ 1);
       hsap_lds_barrier();
     }
@@ -892,13 +728,29 @@ static hsap_status check_attn_rows(const hsap_cache_desc& d, int32_t heads_q, in
   return HSAP_OK;
 }
 
-template <int D, bool TREE>
+template <typename Cut>
+static int64_t workspace_of(Cut cut, const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
+  clear_error();
+  if (check_cache_desc(desc, false) != HSAP_OK || check_attn_rows(*desc, heads_q, total_q) != HSAP_OK) return -1;
+  const CacheCut c = cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
+  return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
+}
+
+template <int D>
 static void launch_cache_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
-  if (c.rows == kChunkRows) hipLaunchKernelGGL((cache_chunk_kernel<D, TREE>), grid, block, 0, s, a);
-  else if (c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false, TREE>), grid, block, 0, s, a);
-  else if (c.once) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true, TREE>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false, TREE>), grid, block, 0, s, a);
+  if (c.rows == kChunkRows) hipLaunchKernelGGL(cache_chunk_kernel<D>, grid, block, 0, s, a);
+  else if (c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<D, 2, false, false>), grid, block, 0, s, a);
+  else if (c.once) hipLaunchKernelGGL((cache_attn_kernel<D, 1, true, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false, false>), grid, block, 0, s, a);
+}
+
+template <int D>
+static void launch_tree_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(256);
+  if (c.rows >= 64) launch_tree(a, c, blocks, s);
+  else if (D == 128 && c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<128, 2, false, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false, true>), grid, block, 0, s, a);
 }
 
 // A call's rows, without or with a tree's masks and positions.
@@ -926,7 +778,12 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
   if (q_stride % 8 || q_stride < (int64_t)heads_q * d)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "q_stride %lld must be a multiple of 8 and at least %lld", (long long)q_stride,
               (long long)heads_q * d);
-  const CacheCut c = cache_cut(*desc, heads_q, total_q, !cu_new, (int64_t)desc->table_width * desc->page_size);
+  const int64_t tokens = (int64_t)desc->table_width * desc->page_size;
+  CacheCut c = (tree ? tree_cut : cache_cut)(*desc, heads_q, total_q, !cu_new, tokens);
+  if (tree) {  // (fewer splits where a window leaves little: the workspace is for any window)
+    const int64_t near = std::min(tokens, (int64_t)window + sinks + 64 * words);
+    c.splits = std::min(c.splits, tree_cut(*desc, heads_q, total_q, !cu_new, near).splits);
+  }
   const int64_t need = cache_workspace(c, heads_q, total_q, d);
   if (workspace_bytes < need)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
@@ -955,11 +812,11 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;
   if (tree) {
-    if (d == 128) launch_cache_attn<128, true>(a, c, blocks, s);
-    else launch_cache_attn<64, true>(a, c, blocks, s);
+    if (d == 128) launch_tree_attn<128>(a, c, blocks, s);
+    else launch_tree_attn<64>(a, c, blocks, s);
   } else {
-    if (d == 128) launch_cache_attn<128, false>(a, c, blocks, s);
-    else launch_cache_attn<64, false>(a, c, blocks, s);
+    if (d == 128) launch_cache_attn<128>(a, c, blocks, s);
+    else launch_cache_attn<64>(a, c, blocks, s);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) HSAP_FAIL(HSAP_ERR_HIP, "%s launch: %s", name, hipGetErrorString(e));
@@ -984,10 +841,7 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
 using namespace hsap;
 
 extern "C" int64_t hsap_cache_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
-  clear_error();
-  if (check_cache_desc(desc, false) != HSAP_OK || check_attn_rows(*desc, heads_q, total_q) != HSAP_OK) return -1;
-  const CacheCut c = cache_cut(*desc, heads_q, total_q, one_each != 0, (int64_t)desc->table_width * desc->page_size);
-  return std::max<int64_t>(16, cache_workspace(c, heads_q, total_q, desc->head_dim));
+  return workspace_of(cache_cut, desc, heads_q, total_q, one_each);
 }
 
 extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q, float softmax_scale,
@@ -1000,7 +854,7 @@ extern "C" hsap_status hsap_cache_attn(const hsap_cache_desc* desc, const hsap_c
 }
 
 extern "C" int64_t hsap_cache_tree_attn_workspace(const hsap_cache_desc* desc, int32_t heads_q, int64_t total_q, int32_t one_each) {
-  return hsap_cache_attn_workspace(desc, heads_q, total_q, one_each);
+  return workspace_of(tree_cut, desc, heads_q, total_q, one_each);
 }
 
 extern "C" hsap_status hsap_cache_tree_attn(const hsap_cache_desc* desc, const hsap_cache* cache, int32_t heads_q,

@@ -1,4 +1,4 @@
-// Masks and positions of drafted tokens from each one's parent.
+// Trees of drafted tokens: masks and positions from each one's parent, and the attention of many rows.
 //
 // A token's mask names itself and its ancestors among the drafted tokens of its sequence, its position is that of its
 // depth: the drafted tokens stand behind `base` tokens, a token without a parent at position base.  A thread walks one
@@ -6,8 +6,7 @@
 // of LDS as the tree is deep.
 #include <algorithm>
 
-#include "cache.h"
-#include "hsap_internal.h"
+#include "cache_attn.h"
 
 namespace hsap {
 
@@ -38,6 +37,315 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* seq_lens
     mask[(int64_t)(t0 + j) * words + x] = bits;
     if (x == 0) positions[t0 + j] = j < named ? base + depth - 1 : -1;
   }
+}
+
+// Many rows of a sequence's tree against its tokens: every code is decoded once for the 32 RB rows of a workgroup.  A step's
+// codes come to registers a step ahead and go as bf16 (which e4m3 fits exactly; V times its scale's power of two) into LDS;
+// then every wave takes 32 rows and 32 tokens (two waves share a row's tokens where RB = 2): 32x32x16 products
+// S^T = K Q^T, O^T += V^T P^T with V^T by transpose reads, Q from LDS too.  One copy of the tiles and few registers, so that
+// three workgroups share a compute unit and decode, multiply and wait at different times.  P is rounded to bf16 for the second
+// product (2^-8 relative at most, summed in fp32), O once at the end.  Steps before the drafted tokens and inside every row's
+// window have no masks; the others (few) form a row's bits once.
+template <int D, int RB>
+__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheAttnArgs a) {
+  constexpr int KB = RB == 4 ? 32 : 64;                          // tokens of a step: a block of 32 for every wave
+  constexpr int CPR = D / 8, ROWS = 32 * RB, U = KB * D / 4096;  // U: runs of 16 codes per thread
+  constexpr int SLOT = (2 + D / 2) * 64;                         // floats of a wave's results
+  constexpr float NEG_INF = -__builtin_inff(), TINY = 1.17549435e-38f;
+  constexpr float RESCALE_SLACK = 8.f;
+  __shared__ __attribute__((aligned(16))) union {
+    struct {
+      __bf16 k[KB * D], v[KB * D], q[ROWS * D];
+    };
+    float join[2 * SLOT];
+  } lds;
+  __shared__ __attribute__((aligned(16))) float scales[2][4];        // [K's times the softmax's, V's rest][16 tokens]
+  __shared__ uint32_t named[2 * kMaxMaskWords];                      // drafted tokens that some row of the tile names
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = blockIdx.x % a.d.heads_kv;
+  const int32_t rest = blockIdx.x / a.d.heads_kv;
+  const int32_t split = rest % a.splits, tile = rest / a.splits;
+  RowTile rt;
+  if (!row_tile(a, tile, ROWS, rt)) return;
+  const int32_t len = max(0, a.c.seq_lens[rt.seq]);
+  const int32_t ps = a.d.page_size, cap = a.d.table_width * ps;
+  const int32_t nrows = rt.count * a.group;
+  const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
+  const int32_t base = len - rt.count;  // place of the sequence's first drafted token
+  int32_t plo = INT32_MAX, phi = -1;    // positions of the tile's rows
+#pragma unroll
+  for (int r = 0; r < ROWS; r += 64) {
+    const int32_t p = a.positions[rt.t0 + min(rt.row0 + r + lane, last_row) / a.group];
+    plo = min(plo, p < 0 ? INT32_MAX : p);
+    phi = max(phi, p);
+  }
+  position_range<64>(plo, phi);
+  plo = uniform(plo);
+  phi = uniform(phi);
+  const bool deep = drafts_end(a, rt, phi, lane);
+  const Steps<KB> steps = tree_steps<KB>(plo, phi, base, len, cap, a.window, a.sinks);
+  const int32_t per = steps_per_split(steps.total, a.splits);
+  const int32_t s_begin = split * per, s_end = min(steps.total, s_begin + per);
+  if (s_begin >= s_end && a.splits > 1) {  // nothing here for the join
+    const int32_t r = rt.row0 + tid, t = r / a.group;
+    if (tid < ROWS && r < nrows)
+      a.part_lse[((int64_t)split * a.total_q + rt.t0 + t) * a.heads_q + g * a.group + (r - t * a.group)] = NEG_INF;
+    return;
+  }
+  // the wave's rows, and its first block of a step's tokens
+  const int rb = RB == 2 ? w & 1 : w, b0 = RB == 2 ? w >> 1 : 0;
+  const bool busy = rt.row0 + 32 * rb <= last_row;
+  const int32_t row = min(rt.row0 + 32 * rb + l32, last_row), tok = row / a.group;
+  const int32_t pos = a.positions[rt.t0 + tok];
+  int32_t wlo = pos < 0 ? INT32_MAX : pos, whi = pos;
+  position_range<32>(wlo, whi);
+  wlo = uniform(wlo);
+  whi = uniform(whi);
+  const bool live = __builtin_amdgcn_ballot_w64(pos < 0) == 0;
+  const int h = g * a.group + (row - tok * a.group);
+#pragma unroll
+  for (int i = 0; i < ROWS * CPR / 256; ++i) {
+    const int at = tid + 256 * i, r = min(rt.row0 + at / CPR, last_row), t = r / a.group;
+    *(bf16x8*)(lds.q + swz<CPR>(at / CPR, 8 * (at % CPR))) =
+        *(const bf16x8*)(a.q + (int64_t)(rt.t0 + t) * a.q_stride + (int64_t)(g * a.group + (r - t * a.group)) * D + 8 * (at % CPR));
+  }
+  const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
+  const int32_t top = min(len - 1, cap - 1);  // last token any row sees
+
+  // Thread's codes of a step: of the 64 tokens those of 16-token group group_of(u) (one page each), 16 codes of a token.
+  auto group_of = [&](int u) { return D == 64 ? w : (w >> 1) + 2 * u; };
+  const int slot_in = D == 64 ? (lane >> 2) : 8 * (w & 1) + (lane >> 3);  // token within the group
+  const int column = 16 * (D == 64 ? lane & 3 : lane & 7);
+  // Pages and scales are read as vectors: a scalar load, which may come back out of order, would make every wait for an LDS
+  // read a wait for memory.
+  int zero;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+  struct Codes {
+    uint4 k[U], v[U];
+    float ks[U], vs[U];
+    bool held[U];  // the group lies in a page
+  };
+  struct Where {
+    int32_t page[U];
+  };
+  // Steps behind the last are its own again, so that no load depends on a branch (a wait would take it for the youngest one).
+  auto look_up = [&](int32_t s) __attribute__((always_inline)) {
+    Where x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = steps.first(min(s, s_end - 1)) + 16 * group_of(u);
+      const bool any = steps.looked_up(a.sinks, j, top);
+      x.page[u] = table[(any ? j >> a.page_shift : 0) + zero];
+      if (!any) x.page[u] = -1;
+    }
+    return x;
+  };
+  auto load = [&](int32_t s, const Where& where, Codes& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = steps.first(min(s, s_end - 1)) + 16 * group_of(u);
+      const int32_t page = uniform(where.page[u]);
+      x.held[u] = (uint32_t)page < (uint32_t)a.d.num_pages;
+      const int64_t at = (int64_t)(x.held[u] ? page : 0) * a.d.heads_kv + g;
+      x.ks[u] = (a.c.k_scale + at)[zero];
+      x.vs[u] = (a.c.v_scale + at)[zero];
+      const int64_t first = ((at << a.page_shift) + (j & (ps - 1)) + slot_in) * D + column;
+      x.k[u] = *(const uint4*)(a.c.k_codes + first);
+      x.v[u] = *(const uint4*)(a.c.v_codes + first);
+    }
+  };
+  auto decode = [&](const uint4& c, float pow2, __bf16* out0, __bf16* out1) __attribute__((always_inline)) {
+    bf16x2 p[8];
+    decode4(c.x, pow2, p[0], p[1]);
+    decode4(c.y, pow2, p[2], p[3]);
+    decode4(c.z, pow2, p[4], p[5]);
+    decode4(c.w, pow2, p[6], p[7]);
+    *(bf16x8*)out0 = bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+    *(bf16x8*)out1 = bf16x8{p[4][0], p[4][1], p[5][0], p[5][1], p[6][0], p[6][1], p[7][0], p[7][1]};
+  };
+  auto store = [&](int32_t s, Codes& x) __attribute__((always_inline)) {
+    const int32_t j0 = steps.first(s);
+    bool whole = j0 >= steps.lo && j0 + KB <= base;  // every place is some row's
+#pragma unroll
+    for (int u = 0; u < U; ++u) whole &= x.held[u];
+    float vpow[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) vpow[u] = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
+    if (__builtin_expect(!whole, 0)) {  // places that no row sees may hold anything
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int32_t j = j0 + 16 * group_of(u) + slot_in;
+        bool unseen = (j > top) | !x.held[u] | ((j < steps.lo) & (j >= a.sinks));
+        if (j >= base) unseen |= j - base >= 64 * a.words || !(named[(j - base) >> 5] >> ((j - base) & 31) & 1);
+        if (unseen) {
+          x.k[u] = x.v[u] = uint4{0, 0, 0, 0};
+          vpow[u] = 1.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int token = 16 * group_of(u) + slot_in;
+      const int at0 = swz<CPR>(token, column), at1 = swz<CPR>(token, column + 8);
+      decode(x.k[u], 1.f, lds.k + at0, lds.k + at1);
+      decode(x.v[u], vpow[u], lds.v + at0, lds.v + at1);
+      // (a scale of 0 stands for no page; at least the smallest normal number, so that -inf times it stays -inf)
+      if (lane == 0) {
+        scales[0][group_of(u)] = x.held[u] ? fmaxf(x.ks[u] * a.scale_log2, TINY) : 0.f;
+        scales[1][group_of(u)] = __uint_as_float((__float_as_uint(x.vs[u]) & 0x007FFFFFu) | 0x3F800000u);
+      }
+    }
+  };
+
+  TileReads<D> rd;
+  rd.init(lane);
+  float m_run = NEG_INF, l_run = 0.f;
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
+
+  auto compute = [&](int32_t s) __attribute__((always_inline)) {
+    const int32_t j0 = steps.first(s);
+    const int32_t jb = j0 + 32 * b0;
+    float sl[2], vrest[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      sl[q] = scales[0][2 * b0 + q];
+      vrest[q] = scales[1][2 * b0 + q];
+    }
+    f32x16 sc{};
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(rd.rows(lds.k + 32 * b0 * D, kk), rd.rows(lds.q + 32 * rb * D, kk), sc);
+    // every row of the wave sees every token of the block
+    const bool all = live && jb + 31 < base && (s < steps.sinks ? jb + 31 < a.sinks : whi - jb < a.window || jb + 31 < a.sinks) &&
+                     __builtin_amdgcn_ballot_w64(fminf(sl[0], sl[1]) > 0.f) == ~uint64_t(0);
+    if (__builtin_expect(!all, 0)) {
+      const uint32_t m = (uint32_t)seen_bits(a, rt, a.mask + (int64_t)(rt.t0 + tok) * a.words, pos, base, jb, top, deep, lane) &
+                         ((sl[0] > 0.f ? 0xFFFFu : 0u) | (sl[1] > 0.f ? 0xFFFF0000u : 0u));
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sc[j] = (m >> (4 * hi)) & (1u << c_row(j, 0)) ? sc[j] : NEG_INF;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) sl[q] = fmaxf(sl[q], TINY);
+    }
+    float mx = NEG_INF;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float x = sc[8 * q];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) x = fmaxf(x, sc[8 * q + j]);
+      mx = fmaxf(mx, x * sl[q]);
+    }
+    // (the two lanes of a row join their maxima only when some row's rose by more than the slack)
+    if (__builtin_amdgcn_ballot_w64(mx > m_run + RESCALE_SLACK) != 0) {
+      const float m_new = fmaxf(m_run, pair_max(mx));
+      const float alpha = m_run == NEG_INF ? 0.f : fast_exp2(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == NEG_INF ? 0.f : m_run;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float p = fast_exp2(__builtin_fmaf(sc[j], sl[j >> 3], -m_use));
+      l_run += p;
+      sc[j] = p;
+    }
+    if (__builtin_amdgcn_ballot_w64(vrest[0] != 1.f || vrest[1] != 1.f) != 0) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sc[j] *= vrest[j >> 3];
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      bf16x8 pb;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pb[j] = (__bf16)sc[8 * q + j];
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) o[mb] = mfma32(rd.turned(lds.v + 16 * (2 * b0 + q) * D, mb), pb, o[mb]);
+    }
+  };
+
+  // (the first barrier comes before the first of them is read)
+  for (int i = tid; i < 2 * a.words; i += 256) named[i] = 0;
+  if (s_begin < s_end) {
+    Codes x;
+    load(s_begin, look_up(s_begin), x);
+    Where next = look_up(s_begin + 1);
+    __syncthreads();
+    const int32_t first = rt.row0 / a.group, count = last_row / a.group - first + 1;
+    for (int i = tid; i < count * a.words; i += 256) {
+      const int32_t t = i / a.words, at = i - t * a.words;
+      const uint64_t m = a.mask[(int64_t)(rt.t0 + first + t) * a.words + at];
+      if ((uint32_t)m) atomicOr(&named[2 * at], (uint32_t)m);
+      if (m >> 32) atomicOr(&named[2 * at + 1], (uint32_t)(m >> 32));
+    }
+    __syncthreads();
+    for (int32_t s = s_begin; s < s_end; ++s) {
+      store(s, x);
+      const Where after = look_up(s + 2);
+      load(s + 1, next, x);
+      next = after;
+      hsap_lds_barrier();
+      const int32_t j0 = steps.first(s);
+      if (busy && (s < steps.sinks || j0 + KB - 1 >= wlo - (a.window - 1) || j0 < a.sinks || j0 + KB > base)) compute(s);
+      hsap_lds_barrier();
+    }
+  }
+  l_run = pair_sum(l_run);
+  if constexpr (RB == 2) {  // the second block's wave hands its results to the first's
+    float* join = lds.join + rb * SLOT + lane;
+    __syncthreads();  // (without steps nobody has waited for Q's rows)
+    if (b0 == 1) {
+      join[0] = m_run;
+      join[64] = l_run;
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) join[64 * (2 + 16 * mb + e)] = o[mb][e];
+    }
+    __syncthreads();
+    if (b0 == 1) return;
+    const float m2 = join[0], l2 = join[64], m = fmaxf(m_run, m2), m_use = m == NEG_INF ? 0.f : m;
+    const float f1 = fast_exp2(m_run - m_use), f2 = fast_exp2(m2 - m_use);
+    l_run = l_run * f1 + l2 * f2;
+    m_run = m;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[mb][e] = o[mb][e] * f1 + join[64 * (2 + 16 * mb + e)] * f2;
+  }
+  if (rt.row0 + 32 * rb + l32 > last_row) return;
+  const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+  const float lse2 = l_run > 0.f ? m_run + __log2f(l_run) : NEG_INF;
+  const int64_t out = (int64_t)(rt.t0 + tok) * a.heads_q + h;
+  if (a.splits == 1) {
+    __bf16* op = a.o + out * D + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(bf16x4*)(op + 32 * mb + 8 * q) = bf16x4{(__bf16)(o[mb][4 * q] * inv), (__bf16)(o[mb][4 * q + 1] * inv),
+                                                  (__bf16)(o[mb][4 * q + 2] * inv), (__bf16)(o[mb][4 * q + 3] * inv)};
+    if (hi == 0 && a.lse) a.lse[(int64_t)h * a.total_q + rt.t0 + tok] = lse2 * 0.69314718055994530942f;
+  } else {
+    const int64_t at = (int64_t)split * a.total_q * a.heads_q + out;
+    float* op = a.part_o + at * D + 4 * hi;
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(op + 32 * mb + 8 * q) = f32x4{o[mb][4 * q] * inv, o[mb][4 * q + 1] * inv, o[mb][4 * q + 2] * inv, o[mb][4 * q + 3] * inv};
+    if (hi == 0) a.part_lse[at] = lse2;
+  }
+}
+
+void launch_tree(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(256);
+  if (a.d.head_dim == 64) hipLaunchKernelGGL((cache_tree_kernel<64, 2>), grid, block, 0, s, a);
+  else if (c.rows == 64) hipLaunchKernelGGL((cache_tree_kernel<128, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_tree_kernel<128, 4>), grid, block, 0, s, a);
 }
 
 }  // namespace hsap
