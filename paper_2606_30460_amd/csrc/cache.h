@@ -140,28 +140,27 @@ inline CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tot
   return c;
 }
 
-// A tree call's cut: 16 or 32 rows (cache_attn_kernel), 64 or 128 (cache_tree_kernel).  Measured, us, 32 -> 64 -> 128 rows
-// at each one's best splits; rows of a sequence on average:
-//   head_dim 128:  30 rows 58 -> 63 -> 72 (16 sequences of 8k tokens), 60 rows 84 -> 80 -> 81 (32 of 4k), 80 rows 100 -> 95 -> 82
-//     (16 of 8k) and 196 -> 180 -> 150 (64 of 8k), 160 rows 284 -> 248 -> 203 (8 of 32k)
-//   head_dim 64:   30 rows 44 -> 37 -> 46, 60 rows 65 -> 54 -> 60, 250 rows 78 -> 56 -> 59
-// Splits: as many as fill the chip about once (three or four workgroups of a compute unit), but not shorter than their
-// beginning, end and partials are worth (16 sequences of 80 rows over 8k tokens: four splits 107, eight 82, sixteen 98).
+// A tree call's cut: 16 or 32 rows (cache_attn_kernel), or cache_tree_kernel's, 128 at head_dim 128 and 64 at 64.  Measured at
+// each one's best splits, us, by the rows of a sequence on average:
+//   head_dim 128, 32 -> 128 rows:  30 rows 58 -> 64 (16 sequences of 8k tokens), 60 rows 83 -> 78 (32 of 4k), 80 rows 98 -> 79 (16
+//     of 8k) and 189 -> 150 (64 of 8k), 160 rows 265 -> 198 (8 of 32k)
+//   head_dim 64, 32 -> 64 rows:  30 rows 44 -> 34 (16 of 8k), 60 rows 65 -> 53 (64 of 2k), 250 rows 78 -> 56 (4 of 16k)
+// Splits: as many as fill the chip about once, but not shorter than their beginning, end and partials are worth (16 sequences
+// of 80 rows over 8k tokens: four splits 102, eight 79, sixteen 97).
+constexpr int64_t kTreeGrid128 = 1024, kTreeGrid64 = 768;
 inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
+  CacheCut c;
+  const bool narrow = d.head_dim == 64;
   const int64_t group = heads_q / d.heads_kv;
   const int64_t rows = one_each ? group : (total_q * group + d.num_seqs - 1) / std::max(d.num_seqs, 1);
-  CacheCut c;
   c.once = false;
-  c.rows = rows <= 16 ? 16 : d.head_dim == 64 ? 64 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  c.rows = rows <= 16 ? 16 : narrow ? 64 : rows <= 32 ? 32 : 128;
   c.tiles = one_each ? (int64_t)d.num_seqs * ((group + c.rows - 1) / c.rows) : item_base(total_q, group, c.rows, 1, d.num_seqs);
-  if (c.rows <= 32) {
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / 256));
-    c.splits = (int32_t)std::min(most, std::max<int64_t>(1, kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv)));
-  } else {
-    const int64_t full = one_each ? c.tiles * d.heads_kv : (total_q * group + c.rows - 1) / c.rows * d.heads_kv;  // workgroups that do something
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, tokens / (c.rows == 64 ? 512 : 1024)));
-    c.splits = (int32_t)std::min(most, std::max<int64_t>(1, (c.rows == 64 ? 768 : 1024) / std::max<int64_t>(1, full)));
-  }
+  // (workgroups that do something: c.tiles counts a tile more per sequence)
+  const int64_t full = std::max<int64_t>(1, (one_each ? c.tiles : (total_q * group + c.rows - 1) / c.rows) * d.heads_kv);
+  const int64_t grid = c.rows <= 32 ? kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv) : (narrow ? kTreeGrid64 : kTreeGrid128) / full;
+  const int64_t shortest = c.rows <= 32 ? 256 : narrow ? 512 : 1024;
+  c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxSplits, tokens / shortest), grid));
   return c;
 }
 

@@ -137,7 +137,7 @@ __device__ __forceinline__ Steps<STEP> tree_steps(int32_t plo, int32_t phi, int3
   return cache_steps<STEP>((int32_t)min((int64_t)plo, most), phi < 0 ? -1 : len - 1, cap, window, sinks);
 }
 
-// The kernels for many rows of a tree (cache_tree.hip): c.rows 64 or 128.
-void launch_tree(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s);
+// The kernels for many rows of a tree (cache_tree.hip): tiles of 128 rows at head_dim 128, 64 at 64.
+void launch_tree(const CacheAttnArgs& a, int64_t blocks, hipStream_t s);
 
 }  // namespace hsap

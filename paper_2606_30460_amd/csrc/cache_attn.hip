@@ -748,7 +748,7 @@ static void launch_cache_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t
 template <int D>
 static void launch_tree_attn(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
-  if (c.rows >= 64) launch_tree(a, c, blocks, s);
+  if (c.rows >= 64) launch_tree(a, blocks, s);
   else if (D == 128 && c.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<128, 2, false, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_attn_kernel<D, 1, false, true>), grid, block, 0, s, a);
 }
@@ -780,10 +780,9 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
               (long long)heads_q * d);
   const int64_t tokens = (int64_t)desc->table_width * desc->page_size;
   CacheCut c = (tree ? tree_cut : cache_cut)(*desc, heads_q, total_q, !cu_new, tokens);
-  if (tree) {  // (fewer splits where a window leaves little: the workspace is for any window)
-    const int64_t near = std::min(tokens, (int64_t)window + sinks + 64 * words);
-    c.splits = std::min(c.splits, tree_cut(*desc, heads_q, total_q, !cu_new, near).splits);
-  }
+  // (fewer splits where a window leaves little: the workspace is for any window)
+  const int64_t near = std::min(tokens, (int64_t)window + sinks + 64 * words);
+  if (tree) c.splits = std::min(c.splits, tree_cut(*desc, heads_q, total_q, !cu_new, near).splits);
   const int64_t need = cache_workspace(c, heads_q, total_q, d);
   if (workspace_bytes < need)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);

@@ -46,6 +46,20 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* seq_lens
 // three workgroups share a compute unit and decode, multiply and wait at different times.  P is rounded to bf16 for the second
 // product (2^-8 relative at most, summed in fp32), O once at the end.  Steps before the drafted tokens and inside every row's
 // window have no masks; the others (few) form a row's bits once.
+// Order of N products with two LDS reads each: the reads of three are under way before the first.  (Left to itself the
+// compiler, short of registers, waits for each product's reads.)
+template <int N>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int READ = 0x100, PRODUCT = 0x8;
+  __builtin_amdgcn_sched_group_barrier(READ, 6, 0);
+#pragma unroll
+  for (int i = 0; i < N - 3; ++i) {
+    __builtin_amdgcn_sched_group_barrier(PRODUCT, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(PRODUCT, 3, 0);
+}
+
 template <int D, int RB>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheAttnArgs a) {
   constexpr int KB = RB == 4 ? 32 : 64;                          // tokens of a step: a block of 32 for every wave
@@ -74,13 +88,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   const int32_t nrows = rt.count * a.group;
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;
   const int32_t base = len - rt.count;  // place of the sequence's first drafted token
-  int32_t plo = INT32_MAX, phi = -1;    // positions of the tile's rows
+  int32_t plo = INT32_MAX, phi = -1, least = INT32_MAX;  // positions of the tile's rows
 #pragma unroll
   for (int r = 0; r < ROWS; r += 64) {
     const int32_t p = a.positions[rt.t0 + min(rt.row0 + r + lane, last_row) / a.group];
+    least = min(least, p);
     plo = min(plo, p < 0 ? INT32_MAX : p);
     phi = max(phi, p);
   }
+  const bool plive = __builtin_amdgcn_ballot_w64(least < 0) == 0;  // all of them see something
   position_range<64>(plo, phi);
   plo = uniform(plo);
   phi = uniform(phi);
@@ -99,11 +115,6 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   const bool busy = rt.row0 + 32 * rb <= last_row;
   const int32_t row = min(rt.row0 + 32 * rb + l32, last_row), tok = row / a.group;
   const int32_t pos = a.positions[rt.t0 + tok];
-  int32_t wlo = pos < 0 ? INT32_MAX : pos, whi = pos;
-  position_range<32>(wlo, whi);
-  wlo = uniform(wlo);
-  whi = uniform(whi);
-  const bool live = __builtin_amdgcn_ballot_w64(pos < 0) == 0;
   const int h = g * a.group + (row - tok * a.group);
 #pragma unroll
   for (int i = 0; i < ROWS * CPR / 256; ++i) {
@@ -114,14 +125,23 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   const int32_t* table = a.c.page_table + (int64_t)rt.seq * a.d.table_width;
   const int32_t top = min(len - 1, cap - 1);  // last token any row sees
 
-  // Thread's codes of a step: of the 64 tokens those of 16-token group group_of(u) (one page each), 16 codes of a token.
+  // Steps whose places are all some row's, and every row's: behind the sinks' and every window's beginning, before the drafts.
+  const int64_t inside = max((int64_t)phi - a.window + 1, (int64_t)steps.win0) - steps.win0;
+  const int32_t hot0 = steps.sinks + (int32_t)min((inside + KB - 1) / KB, (int64_t)steps.total);
+  const int32_t hot1 = plive ? steps.sinks + max(base - steps.win0, 0) / KB : 0;
+
+  // Thread's codes of a step: those of 16-token group group_of(u) (one page each), 16 codes of a token.  What is formed of a
+  // page's number is formed on the vector units, which have its multiplication and addition in one, and which do not make
+  // every wait for LDS one for memory, as scalar loads would.
   auto group_of = [&](int u) { return D == 64 ? w : (w >> 1) + 2 * u; };
   const int slot_in = D == 64 ? (lane >> 2) : 8 * (w & 1) + (lane >> 3);  // token within the group
   const int column = 16 * (D == 64 ? lane & 3 : lane & 7);
-  // Pages and scales are read as vectors: a scalar load, which may come back out of order, would make every wait for an LDS
-  // read a wait for memory.
   int zero;
   asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+  const uint32_t page_bytes = (uint32_t)a.d.heads_kv << a.page_shift;  // (times D)
+  const int64_t first_row = ((int64_t)g << a.page_shift) + slot_in;
+  const uint8_t* k_at = a.c.k_codes + first_row * D + column;
+  const uint8_t* v_at = a.c.v_codes + first_row * D + column;
   struct Codes {
     uint4 k[U], v[U];
     float ks[U], vs[U];
@@ -130,7 +150,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   struct Where {
     int32_t page[U];
   };
-  // Steps behind the last are its own again, so that no load depends on a branch (a wait would take it for the youngest one).
+  // (steps behind the last are its own again)
   auto look_up = [&](int32_t s) __attribute__((always_inline)) {
     Where x;
 #pragma unroll
@@ -146,14 +166,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int32_t j = steps.first(min(s, s_end - 1)) + 16 * group_of(u);
-      const int32_t page = uniform(where.page[u]);
-      x.held[u] = (uint32_t)page < (uint32_t)a.d.num_pages;
-      const int64_t at = (int64_t)(x.held[u] ? page : 0) * a.d.heads_kv + g;
-      x.ks[u] = (a.c.k_scale + at)[zero];
-      x.vs[u] = (a.c.v_scale + at)[zero];
-      const int64_t first = ((at << a.page_shift) + (j & (ps - 1)) + slot_in) * D + column;
-      x.k[u] = *(const uint4*)(a.c.k_codes + first);
-      x.v[u] = *(const uint4*)(a.c.v_codes + first);
+      x.held[u] = (uint32_t)where.page[u] < (uint32_t)a.d.num_pages;
+      const uint32_t page = x.held[u] ? where.page[u] : 0;
+      const uint64_t scale = (uint64_t)page * (uint32_t)a.d.heads_kv + g;
+      x.ks[u] = a.c.k_scale[scale];
+      x.vs[u] = a.c.v_scale[scale];
+      const uint64_t at = ((uint64_t)page * page_bytes + (uint32_t)(j & (ps - 1))) * D;
+      x.k[u] = *(const uint4*)(k_at + at);
+      x.v[u] = *(const uint4*)(v_at + at);
     }
   };
   auto decode = [&](const uint4& c, float pow2, __bf16* out0, __bf16* out1) __attribute__((always_inline)) {
@@ -166,17 +186,16 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
     *(bf16x8*)out1 = bf16x8{p[4][0], p[4][1], p[5][0], p[5][1], p[6][0], p[6][1], p[7][0], p[7][1]};
   };
   auto store = [&](int32_t s, Codes& x) __attribute__((always_inline)) {
-    const int32_t j0 = steps.first(s);
-    bool whole = j0 >= steps.lo && j0 + KB <= base;  // every place is some row's
+    bool held = true;
 #pragma unroll
-    for (int u = 0; u < U; ++u) whole &= x.held[u];
+    for (int u = 0; u < U; ++u) held &= x.held[u];
     float vpow[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) vpow[u] = __uint_as_float(__float_as_uint(x.vs[u]) & 0x7F800000u);
-    if (__builtin_expect(!whole, 0)) {  // places that no row sees may hold anything
+    if (__builtin_expect(s < hot0 || s >= hot1 || __builtin_amdgcn_ballot_w64(!held) != 0, 0)) {  // places that no row sees may hold anything
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int32_t j = j0 + 16 * group_of(u) + slot_in;
+        const int32_t j = steps.first(s) + 16 * group_of(u) + slot_in;
         bool unseen = (j > top) | !x.held[u] | ((j < steps.lo) & (j >= a.sinks));
         if (j >= base) unseen |= j - base >= 64 * a.words || !(named[(j - base) >> 5] >> ((j - base) & 31) & 1);
         if (unseen) {
@@ -207,8 +226,6 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
 
   auto compute = [&](int32_t s) __attribute__((always_inline)) {
-    const int32_t j0 = steps.first(s);
-    const int32_t jb = j0 + 32 * b0;
     float sl[2], vrest[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -218,10 +235,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
     f32x16 sc{};
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) sc = mfma32(rd.rows(lds.k + 32 * b0 * D, kk), rd.rows(lds.q + 32 * rb * D, kk), sc);
-    // every row of the wave sees every token of the block
-    const bool all = live && jb + 31 < base && (s < steps.sinks ? jb + 31 < a.sinks : whi - jb < a.window || jb + 31 < a.sinks) &&
-                     __builtin_amdgcn_ballot_w64(fminf(sl[0], sl[1]) > 0.f) == ~uint64_t(0);
-    if (__builtin_expect(!all, 0)) {
+    reads_ahead<D / 16>();
+    if (__builtin_expect(s < hot0 || s >= hot1 || __builtin_amdgcn_ballot_w64(!(fminf(sl[0], sl[1]) > 0.f)) != 0, 0)) {
+      const int32_t jb = steps.first(s) + 32 * b0;
       const uint32_t m = (uint32_t)seen_bits(a, rt, a.mask + (int64_t)(rt.t0 + tok) * a.words, pos, base, jb, top, deep, lane) &
                          ((sl[0] > 0.f ? 0xFFFFu : 0u) | (sl[1] > 0.f ? 0xFFFF0000u : 0u));
 #pragma unroll
@@ -265,6 +281,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
 #pragma unroll
       for (int mb = 0; mb < D / 32; ++mb) o[mb] = mfma32(rd.turned(lds.v + 16 * (2 * b0 + q) * D, mb), pb, o[mb]);
     }
+    reads_ahead<D / 16>();
   };
 
   // (the first barrier comes before the first of them is read)
@@ -288,8 +305,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
       load(s + 1, next, x);
       next = after;
       hsap_lds_barrier();
-      const int32_t j0 = steps.first(s);
-      if (busy && (s < steps.sinks || j0 + KB - 1 >= wlo - (a.window - 1) || j0 < a.sinks || j0 + KB > base)) compute(s);
+      if (busy) compute(s);
       hsap_lds_barrier();
     }
   }
@@ -341,10 +357,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   }
 }
 
-void launch_tree(const CacheAttnArgs& a, const CacheCut& c, int64_t blocks, hipStream_t s) {
+void launch_tree(const CacheAttnArgs& a, int64_t blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(256);
   if (a.d.head_dim == 64) hipLaunchKernelGGL((cache_tree_kernel<64, 2>), grid, block, 0, s, a);
-  else if (c.rows == 64) hipLaunchKernelGGL((cache_tree_kernel<128, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_tree_kernel<128, 4>), grid, block, 0, s, a);
 }
 
