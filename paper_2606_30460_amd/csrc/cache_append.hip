@@ -36,6 +36,7 @@ struct AppendArgs {
   __bf16* q_out;
   int32_t heads_q;
   int32_t kv_blocks;  // workgroups of the cache's part; the others rotate Q
+  int32_t q_lanes;    // AT: rows of Q that a wave takes at a time
 };
 
 // Values of a row that are rotated as halves.
@@ -100,8 +101,42 @@ __device__ __forceinline__ float unit_max(const Unit& r) {
   return m;
 }
 
+// AT: a wave takes a token's Q rows, several tokens' where it has few heads.
+template <int D>
+__device__ __forceinline__ void rotate_q_at(const AppendArgs& a, int64_t wave) {
+  constexpr int UNITS = D / 16, G = 64 / UNITS;
+  const int lane = threadIdx.x & 63, u = lane % UNITS, g = lane / UNITS;
+  const int per = G / a.q_lanes, sub = g & (a.q_lanes - 1);
+  const int64_t first = wave * per, t = first + g / a.q_lanes;
+  if (first >= a.total_new) return;
+  int64_t pos;
+  if (a.cu) {
+    int32_t s = sequence_of(a.cu, a.d.num_seqs, 1, 1, 0, first);  // cu[s] <= first
+    if (t >= a.total_new || t >= a.cu[a.d.num_seqs]) return;      // (behind the last sequence: not read)
+    if (t >= a.cu[s + 1]) {
+      int32_t r = a.d.num_seqs;
+      while (r - s > 1) {
+        const int32_t mid = (s + r) >> 1;
+        if (a.cu[mid] <= t) s = mid;
+        else r = mid;
+      }
+    }
+    pos = (int64_t)a.c.seq_lens[s] - (a.cu[s + 1] - t);
+  } else {
+    if (t >= a.total_new) return;
+    pos = (int64_t)a.c.seq_lens[t] - 1;
+  }
+  Place at;
+  if (pos < 0 || !place_of(a.turn, t, at)) return;
+  const UnitTurn by = load_turn<D>(a.turn, at, u);
+  const int rot = halves(a, true);
+  turn_heads<D, 2>(
+      a.turn, by, a.heads_q, sub, a.q_lanes, u, [&](int h) { return load_bf16<D>(a.q + t * a.q_stride + (int64_t)h * D, rot, u); },
+      [&](int h, const Unit& r) { store_bf16<D>(a.q_out + (t * a.heads_q + h) * D, rot, u, r); });
+}
+
 // One rotated Q row unit per thread.
-template <int D, bool AT>
+template <int D>
 __device__ __forceinline__ void rotate_q(const AppendArgs& a, int64_t item) {
   constexpr int UNITS = D / 16;
   const int u = (int)(item % UNITS);
@@ -124,8 +159,8 @@ __device__ __forceinline__ void rotate_q(const AppendArgs& a, int64_t item) {
     pos = (int64_t)a.c.seq_lens[t] - 1;
   }
   Place at;
-  if (!place<D, AT>(a, t, pos, at)) return;
-  if (a.turn.rot) x = turned_unit<D, AT>(a, at, pos, u, x);
+  if (!place<D, false>(a, t, pos, at)) return;
+  if (a.turn.rot) x = turned_unit<D, false>(a, at, pos, u, x);
   store_bf16<D>(a.q_out + (t * a.heads_q + h) * D, rot, u, x);
 }
 
@@ -134,7 +169,9 @@ template <int D, bool AT>
 __global__ __launch_bounds__(256) void cache_append_one_kernel(AppendArgs a) {
   constexpr int UNITS = D / 16;
   if ((int)blockIdx.x >= a.kv_blocks) {
-    rotate_q<D, AT>(a, (int64_t)(blockIdx.x - a.kv_blocks) * 256 + threadIdx.x);
+    const int64_t block = blockIdx.x - a.kv_blocks;
+    if constexpr (AT) rotate_q_at<D>(a, block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    else rotate_q<D>(a, block * 256 + threadIdx.x);
     return;
   }
   const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -178,7 +215,9 @@ template <int D, int PER, bool AT>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   constexpr int UNITS = D / 16;
   if ((int)blockIdx.x >= a.kv_blocks) {
-    rotate_q<D, AT>(a, (int64_t)(blockIdx.x - a.kv_blocks) * 256 + threadIdx.x);
+    const int64_t block = blockIdx.x - a.kv_blocks;
+    if constexpr (AT) rotate_q_at<D>(a, block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    else rotate_q<D>(a, block * 256 + threadIdx.x);
     return;
   }
   __shared__ float wave_max[4], old_scale;
@@ -189,12 +228,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   const int64_t item = pair / a.d.heads_kv;
   const int32_t ps = a.d.page_size;
   // the sequence whose pages this item is one of
-  int32_t s = 0, r = a.d.num_seqs;
-  while (r - s > 1) {
-    const int32_t mid = (s + r) >> 1;
-    if (item_base(a.cu[mid], 1, ps, 2, mid) <= item) s = mid;
-    else r = mid;
-  }
+  const int32_t s = sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item);
   const int32_t t0 = a.cu[s], count = a.cu[s + 1] - t0, len = a.c.seq_lens[s];
   if (count <= 0 || len <= 0) return;
   const int64_t pos0 = (int64_t)len - count;  // position of the first new token
@@ -325,7 +359,9 @@ static hsap_status append(const hsap_cache_desc* desc, const hsap_cache* cache, 
   const int64_t units = d / 16;
   const int64_t kv = cu_new ? (item_base(total_new, 1, desc->page_size, 2, desc->num_seqs)) * desc->heads_kv * 2
                             : ((int64_t)desc->num_seqs * desc->heads_kv * 2 * units + 255) / 256;
-  const int64_t blocks = kv + (q ? (total_new * heads_q * units + 255) / 256 : 0);
+  a.q_lanes = rows_at_a_time(heads_q, d);
+  const int64_t q_tokens = 4 * (64 / units / a.q_lanes);  // AT: of a workgroup
+  const int64_t blocks = kv + (!q ? 0 : turn.positions ? (total_new + q_tokens - 1) / q_tokens : (total_new * heads_q * units + 255) / 256);
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens x heads");
   a.kv_blocks = (int32_t)kv;
   hipStream_t s = (hipStream_t)hip_stream;

@@ -780,12 +780,13 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
               (long long)heads_q * d);
   const int64_t tokens = (int64_t)desc->table_width * desc->page_size;
   CacheCut c = (tree ? tree_cut : cache_cut)(*desc, heads_q, total_q, !cu_new, tokens);
-  // (fewer splits where a window leaves little: the workspace is for any window)
-  const int64_t near = std::min(tokens, (int64_t)window + sinks + 64 * words);
-  if (tree) c.splits = std::min(c.splits, tree_cut(*desc, heads_q, total_q, !cu_new, near).splits);
   const int64_t need = cache_workspace(c, heads_q, total_q, d);
   if (workspace_bytes < need)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+  if (tree) {  // fewer splits where a window leaves little
+    const int64_t near = std::min(tokens, (int64_t)window + sinks + 64 * words);
+    c.splits = std::min(c.splits, tree_cut(*desc, heads_q, total_q, !cu_new, near).splits);
+  }
   CacheAttnArgs a{};
   a.d = *desc;
   a.c = *cache;

@@ -41,84 +41,88 @@ __device__ __forceinline__ float codes_max(const uint4& w) {
   return m;
 }
 
-// PER: units of 16 codes of a page per thread.
+// A workgroup moves K's and V's codes of a page and head, whose tokens it looks up once (16 sequences of 8k tokens, half of
+// them into fresh pages: 49 us with one each, XXX with both).  PER: units of 16 codes of a page per thread.
 template <int D, int PER, bool FRESH>
 __global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs a) {
   constexpr int UNITS = D / 16;
-  __shared__ float wave_max[4], old_scale;
+  __shared__ float wave_max[2][4], old_scale[2];
   const int tid = threadIdx.x;
-  const bool is_v = blockIdx.x & 1;
-  const int32_t pair = (int32_t)(blockIdx.x >> 1);
-  const int h = pair % a.d.heads_kv;
-  const int64_t item = pair / a.d.heads_kv;
+  const int h = blockIdx.x % a.d.heads_kv;
+  const int64_t item = blockIdx.x / a.d.heads_kv;
   const int32_t ps = a.d.page_size;
-  int32_t s = 0;
-  if constexpr (FRESH) {
-    int32_t r = a.d.num_seqs;
-    while (r - s > 1) {
-      const int32_t mid = (s + r) >> 1;
-      if (item_base(a.cu[mid], 1, ps, 2, mid) <= item) s = mid;
-      else r = mid;
-    }
-  } else {
-    s = (int32_t)item;
-  }
+  const int32_t s = FRESH ? sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item) : (int32_t)item;
   const int32_t i0 = a.cu[s];
   const int64_t count = min((int64_t)a.cu[s + 1], a.total) - i0;
   const int32_t first = a.first ? max(a.first[s], 0) : 0;
   const int64_t nth = FRESH ? item - item_base(i0, 1, ps, 2, s) : 0;  // page of the list's
-  if (a.new_lens && h == 0 && !is_v && nth == 0 && tid == 0) a.new_lens[s] = first + (int32_t)max(count, (int64_t)0);
+  if (a.new_lens && h == 0 && nth == 0 && tid == 0) a.new_lens[s] = first + (int32_t)max(count, (int64_t)0);
   if (count <= 0) return;
   const int32_t* row = a.c.page_table + (int64_t)s * a.d.table_width;
   const int32_t* out_row = FRESH ? a.dst_table + (int64_t)s * a.d.table_width : row;
-  uint8_t* all = is_v ? a.c.v_codes : a.c.k_codes;
-  float* scales = is_v ? a.c.v_scale : a.c.k_scale;
+  uint8_t* const all[2] = {a.c.k_codes, a.c.v_codes};
+  float* const scales[2] = {a.c.k_scale, a.c.v_scale};
   const int64_t end = (int64_t)first + count;
   int64_t at = first / ps + nth;
   for (int64_t lo = max((int64_t)first, at * ps); lo < end; lo = ++at * ps) {
     const int64_t hi = min(end, (at + 1) * ps);
     const int32_t page = lo <= INT32_MAX ? cache_page(out_row, a.d.table_width, a.d.num_pages, ps, (int32_t)lo) : -1;
     const int32_t slot0 = (int32_t)(lo - at * ps), units = (int32_t)(hi - lo) * UNITS;
-    uint4 w[PER];
-    float scale[PER], amax = 0.f;
+    uint4 w[2][PER];
+    float scale[2][PER], amax[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int unit = tid + 256 * i;
-      w[i] = uint4{0, 0, 0, 0};
-      scale[i] = 0.f;
+      w[0][i] = w[1][i] = uint4{0, 0, 0, 0};
+      scale[0][i] = scale[1][i] = 0.f;
       if (unit < units) {
         const int32_t src = a.keep[i0 + (lo - first) + unit / UNITS];
         const int32_t from = cache_page(row, a.d.table_width, a.d.num_pages, ps, src);
         if (from >= 0) {
-          scale[i] = scales[(int64_t)from * a.d.heads_kv + h];
-          w[i] = *(const uint4*)(all + cache_row(from, a.d.heads_kv, h, ps, src & (ps - 1), D) + 16 * (unit % UNITS));
+          const int64_t of = (int64_t)from * a.d.heads_kv + h;
+          const int64_t place = cache_row(from, a.d.heads_kv, h, ps, src & (ps - 1), D) + 16 * (unit % UNITS);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            scale[x][i] = scales[x][of];
+            w[x][i] = *(const uint4*)(all[x] + place);
+          }
         }
-        amax = fmaxf(amax, codes_max(w[i]) * scale[i]);
       }
     }
-    if (page >= 0 && tid == 0) old_scale = slot0 > 0 ? scales[(int64_t)page * a.d.heads_kv + h] : 0.f;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-    if ((tid & 63) == 0) wave_max[tid >> 6] = amax;
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) amax[x] = fmaxf(amax[x], codes_max(w[x][i]) * scale[x][i]);
+      if (page >= 0 && tid == 0) old_scale[x] = slot0 > 0 ? scales[x][(int64_t)page * a.d.heads_kv + h] : 0.f;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) amax[x] = fmaxf(amax[x], __shfl_xor(amax[x], o));
+      if ((tid & 63) == 0) wave_max[x][tid >> 6] = amax[x];
+    }
     __syncthreads();  // (everything that this page's places held has been read)
-    amax = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
-    float inv, ratio;
-    const float now = page_scale(amax, slot0 > 0, old_scale, inv, ratio);
-    __syncthreads();
-    if (page >= 0) {
-      uint8_t* codes = all + cache_row(page, a.d.heads_kv, h, ps, 0, D);
-      if (ratio != 1.f)
-        for (int e = tid; e < slot0 * UNITS; e += 256) recode16(codes + 16 * e, ratio);
+    float now[2], inv[2], ratio[2];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int unit = tid + 256 * i;
-        if (unit < units) {
-          // (a code that is not 0 has at most 448 2^9 times the new scale; a page of zeros may have had any)
-          const float by = fminf(scale[i] * inv, 0x1p20f);
-          *(uint4*)(codes + (slot0 * UNITS + unit) * 16) = by == 1.f ? w[i] : recoded16(w[i], by);
+    for (int x = 0; x < 2; ++x) {
+      const float m = fmaxf(fmaxf(wave_max[x][0], wave_max[x][1]), fmaxf(wave_max[x][2], wave_max[x][3]));
+      now[x] = page_scale(m, slot0 > 0, old_scale[x], inv[x], ratio[x]);
+    }
+    if (!FRESH) __syncthreads();  // (the next page's come to the same places)
+    if (page >= 0) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint8_t* codes = all[x] + cache_row(page, a.d.heads_kv, h, ps, 0, D);
+        if (ratio[x] != 1.f)
+          for (int e = tid; e < slot0 * UNITS; e += 256) recode16(codes + 16 * e, ratio[x]);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int unit = tid + 256 * i;
+          if (unit < units) {
+            // (a code that is not 0 has at most 448 2^9 times the new scale; a page of zeros may have had any)
+            const float by = fminf(scale[x][i] * inv[x], 0x1p20f);
+            *(uint4*)(codes + (slot0 * UNITS + unit) * 16) = by == 1.f ? w[x][i] : recoded16(w[x][i], by);
+          }
         }
+        if (tid == 0) scales[x][(int64_t)page * a.d.heads_kv + h] = now[x];
       }
-      if (tid == 0) scales[(int64_t)page * a.d.heads_kv + h] = now;
     }
     if (FRESH) break;
   }
@@ -148,7 +152,7 @@ extern "C" hsap_status hsap_cache_compact(const hsap_cache_desc* desc, const hsa
   if (!cu_keep || (total_keep && !keep)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
   CompactArgs a{*desc, *cache, keep, cu_keep, total_keep, first, dst_table, new_lens};
   const int64_t items = dst_table ? item_base(total_keep, 1, desc->page_size, 2, desc->num_seqs) : desc->num_seqs;
-  const int64_t blocks = items * desc->heads_kv * 2;
+  const int64_t blocks = items * desc->heads_kv;
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens x heads");
   hipStream_t s = (hipStream_t)hip_stream;
   if (dst_table) {

@@ -29,6 +29,7 @@ struct PagesArgs {
   int32_t window;
   int32_t sinks;
   int32_t columns;
+  int32_t with_lens;
 };
 
 __device__ __forceinline__ bool is_page(const hsap_cache_desc& d, int32_t p) { return p >= 0 && p < d.num_pages; }
@@ -40,23 +41,31 @@ __device__ __forceinline__ int32_t source_of(const PagesArgs& a, int32_t s) {
 }
 
 constexpr int kForkEntries = 16384;  // of the table, that a workgroup holds: columns for all rows
+constexpr int kForkThreads = 512;
 
-// A workgroup takes some columns of all rows, so that rows can change places.
-__global__ __launch_bounds__(256) void pages_fork_kernel(PagesArgs a) {
+// A workgroup takes some columns of all rows, so that rows can change places.  One that takes them all writes the lengths too
+// (a second launch would: 8 rows of 63 pages 4.1 us in two, XXX in one).
+__global__ __launch_bounds__(kForkThreads) void pages_fork_kernel(PagesArgs a) {
   extern __shared__ int32_t held[];
   const int32_t c0 = (int32_t)blockIdx.x * a.columns, width = min(a.columns, a.d.table_width - c0);
   const int32_t n = a.d.num_seqs * width, ps = a.d.page_size;
-  for (int32_t i = threadIdx.x; i < n; i += 256) {
+  const int32_t* lens = a.lens;
+  if (a.with_lens) {
+    int32_t* lens_held = held + n;
+    for (int32_t s = threadIdx.x; s < a.d.num_seqs; s += kForkThreads) lens_held[s] = a.lens[s];
+    lens = lens_held;
+  }
+  for (int32_t i = threadIdx.x; i < n; i += kForkThreads) {
     const int32_t s = i / width, c = i - s * width;
     held[i] = a.table[(int64_t)s * a.d.table_width + c0 + c];
   }
   __syncthreads();
-  for (int32_t i = threadIdx.x; i < n; i += 256) {
+  for (int32_t i = threadIdx.x; i < n; i += kForkThreads) {
     const int32_t s = i / width, c = i - s * width;
     const int32_t from = source_of(a, s), old = held[i];
     int32_t now = -1;
     if (from >= 0) {
-      const int64_t len = a.lens[from], first = (int64_t)(c0 + c) * ps;
+      const int64_t len = lens[from], first = (int64_t)(c0 + c) * ps;
       // (the next token is at position len)
       const bool seen = len - (first + ps - 1) < a.window || first < a.sinks;
       if (first < len && seen) now = held[from * width + c];
@@ -67,6 +76,11 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(PagesArgs a) {
     if (now >= 0) atomicAdd(a.refs + now, 1);
     a.table[(int64_t)s * a.d.table_width + c0 + c] = now;
   }
+  if (a.with_lens)
+    for (int32_t s = threadIdx.x; s < a.d.num_seqs; s += kForkThreads) {
+      const int32_t from = source_of(a, s);
+      a.lens[s] = from < 0 ? 0 : lens[from];
+    }
 }
 
 // The lengths of the rows, after the pages (whose kernel reads the old ones).
@@ -86,6 +100,18 @@ struct Item {
   int64_t entry;  // in the table
   bool part;      // the page holds older tokens of the sequence
 };
+// Page nth of those that the `count` new tokens from t0 on of sequence s, len tokens long, are written to; false: there is none.
+__device__ __forceinline__ bool place_of(const PagesArgs& a, int32_t s, int32_t t0, int32_t count, int32_t len, int64_t nth, Item& x) {
+  const int32_t ps = a.d.page_size;
+  if (count <= 0 || len <= 0) return false;
+  const int64_t pos0 = (int64_t)len - count, first = max(pos0, (int64_t)0), at = first / ps + nth;
+  const int64_t lo = max(first, at * ps), end = min(min((int64_t)len, (at + 1) * ps), pos0 + a.total - t0);
+  if (lo >= end || at >= a.d.table_width) return false;
+  x.s = s;
+  x.entry = (int64_t)s * a.d.table_width + at;
+  x.part = lo > at * ps;
+  return true;
+}
 __device__ __forceinline__ bool item_of(const PagesArgs& a, int64_t item, Item& x) {
   const int32_t ps = a.d.page_size;
   int32_t s = 0, t0, count;
@@ -105,15 +131,7 @@ __device__ __forceinline__ bool item_of(const PagesArgs& a, int64_t item, Item& 
     t0 = s;
     count = 1;
   }
-  const int32_t len = a.lens[s];
-  if (count <= 0 || len <= 0) return false;
-  const int64_t pos0 = (int64_t)len - count, first = max(pos0, (int64_t)0), at = first / ps + nth;
-  const int64_t lo = max(first, at * ps), end = min(min((int64_t)len, (at + 1) * ps), pos0 + a.total - t0);
-  if (lo >= end || at >= a.d.table_width) return false;
-  x.s = s;
-  x.entry = (int64_t)s * a.d.table_width + at;
-  x.part = lo > at * ps;
-  return true;
+  return place_of(a, s, t0, count, a.lens[s], nth, x);
 }
 
 __device__ __forceinline__ int32_t count_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -221,6 +239,106 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
   }
 }
 
+// The same where every thread has one item at most: sequences and lengths in LDS, places held in registers, and the sequences
+// that write a shared page found by comparison, so that nothing is written before it is known that the free pages are enough.
+constexpr int kFewItems = 1024;
+__global__ __launch_bounds__(1024) void pages_reserve_few_kernel(PagesArgs a) {
+  __shared__ int32_t waves[16], cu[kFewItems + 1], lens[kFewItems], list[kFewItems];
+  __shared__ int32_t shared[kFewItems];  // each item's page where it is shared, else -1
+  const int tid = threadIdx.x, ps = a.d.page_size;
+  const int32_t n = a.d.num_seqs, items = (int32_t)a.items;
+  // (free pages of the first stretch, under way while the places are found)
+  uint32_t free = 0;
+  const int32_t p0 = 16 * tid;
+  const bool wide = ((uintptr_t)a.refs & 15) == 0;
+  int4 r[4];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    const int32_t p = p0 + 4 * y;
+    r[y] = int4{1, 1, 1, 1};
+    if (wide && p + 3 < a.d.num_pages) r[y] = *(const int4*)(a.refs + p);
+    else {
+      if (p < a.d.num_pages) r[y].x = a.refs[p];
+      if (p + 1 < a.d.num_pages) r[y].y = a.refs[p + 1];
+      if (p + 2 < a.d.num_pages) r[y].z = a.refs[p + 2];
+      if (p + 3 < a.d.num_pages) r[y].w = a.refs[p + 3];
+    }
+  }
+  if (tid < n) {
+    lens[tid] = a.lens[tid];
+    a.pairs[2 * tid] = a.pairs[2 * tid + 1] = -1;
+  }
+  if (a.cu)
+    for (int32_t i = tid; i <= n; i += 1024) cu[i] = a.cu[i];
+  __syncthreads();
+  Item x{};
+  int32_t page = -1, count = 0;
+  bool mine = false;
+  if (tid < items) {
+    int32_t s = tid, t0 = tid, new_count = 1;
+    int64_t nth = 0;
+    if (a.cu) {
+      int32_t hi = n;
+      s = 0;
+      while (hi - s > 1) {
+        const int32_t mid = (s + hi) >> 1;
+        if (item_base(cu[mid], 1, ps, 2, mid) <= tid) s = mid;
+        else hi = mid;
+      }
+      t0 = cu[s];
+      new_count = cu[s + 1] - t0;
+      nth = tid - item_base(t0, 1, ps, 2, s);
+    }
+    mine = place_of(a, s, t0, new_count, lens[s], nth, x);
+    if (mine) {
+      page = a.table[x.entry];
+      if (is_page(a.d, page)) count = a.refs[page];
+      else page = -1;
+    }
+  }
+  shared[tid] = count > 1 ? page : -1;
+  __syncthreads();
+  bool need = mine && page < 0;
+  if (count > 1) {
+    int32_t writers = 0;
+    bool last = true;
+    for (int32_t i = 0; i < items; ++i) {
+      const bool same = shared[i] == page;
+      writers += same;
+      last &= !same || i <= tid;
+    }
+    need = writers < count || !last;
+  }
+  int32_t wanted, total;
+  const int32_t nth = block_scan(need, waves, wanted);
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+    free |= (uint32_t)((r[y].x == 0) | (r[y].y == 0) << 1 | (r[y].z == 0) << 2 | (r[y].w == 0) << 3) << (4 * y);
+  int32_t at = block_scan(__popc(free), waves, total), found = total;
+  for (int64_t p = p0;;) {
+    for (; free && at < wanted; free &= free - 1) list[at++] = (int32_t)p + __ffs(free) - 1;
+    p += 1024 * 16;
+    if (found >= wanted || p - p0 >= a.d.num_pages) break;
+    free = 0;
+#pragma unroll
+    for (int y = 0; y < 16; ++y)
+      if (p + y < a.d.num_pages && a.refs[p + y] == 0) free |= 1u << y;
+    at = found + block_scan(__popc(free), waves, total);
+    found += total;
+  }
+  __syncthreads();
+  if (tid == 0) *a.missing = max(0, wanted - found);
+  if (found < wanted || !need) return;
+  const int32_t to = list[nth];
+  if (page >= 0) atomicAdd(a.refs + page, -1);
+  a.refs[to] = 1;
+  a.table[x.entry] = to;
+  if (x.part && page >= 0) {
+    a.pairs[2 * x.s] = page;
+    a.pairs[2 * x.s + 1] = to;
+  }
+}
+
 constexpr int kCopyBytes = 16384;  // of a page, per workgroup
 
 __global__ __launch_bounds__(256) void copy_pages_kernel(hsap_cache_desc d, hsap_cache c, const int32_t* pairs, int32_t parts) {
@@ -287,11 +405,14 @@ extern "C" hsap_status hsap_pages_fork(const hsap_cache_desc* desc, int32_t* pag
   a.source = source;
   a.window = window;
   a.sinks = sinks;
-  a.columns = std::min(std::min(32, desc->table_width), kForkEntries / desc->num_seqs);
+  const int64_t all = (int64_t)desc->num_seqs * desc->table_width;
+  a.columns = std::min(all <= kForkEntries / 4 ? desc->table_width : std::min(32, desc->table_width), kForkEntries / desc->num_seqs);
+  a.with_lens = source && a.columns == desc->table_width && desc->num_seqs <= kForkEntries / 4;
   hipStream_t s = (hipStream_t)hip_stream;
   const unsigned blocks = (unsigned)((desc->table_width + a.columns - 1) / a.columns);
-  hipLaunchKernelGGL(pages_fork_kernel, dim3(blocks), dim3(256), (size_t)desc->num_seqs * a.columns * 4, s, a);
-  if ((st = launched("pages_fork")) != HSAP_OK || !source) return st;
+  const size_t lds = (size_t)desc->num_seqs * (a.columns + a.with_lens) * 4;
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(blocks), dim3(kForkThreads), lds, s, a);
+  if ((st = launched("pages_fork")) != HSAP_OK || !source || a.with_lens) return st;
   hipLaunchKernelGGL(pages_lens_kernel, dim3(1), dim3(256), (size_t)desc->num_seqs * 4, s, a);
   return launched("pages_fork lengths");
 }
@@ -327,7 +448,9 @@ extern "C" hsap_status hsap_pages_reserve(const hsap_cache_desc* desc, int32_t* 
   a.items = desc->num_seqs ? reserve_items(*desc, !cu_new, total_new) : 0;
   if (workspace_bytes < 8 * a.items)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)(8 * a.items));
-  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
+  if (a.items <= kFewItems && desc->num_seqs <= kFewItems)
+    hipLaunchKernelGGL(pages_reserve_few_kernel, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
+  else hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
   return launched("pages_reserve");
 }
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ void store_row(const hsap_token_rows& x, int64_t at, 
 
 template <int D>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
-  constexpr int UNITS = D / 16, G = 64 / UNITS, FLIGHT = 4;
+  constexpr int UNITS = D / 16, G = 64 / UNITS;
   const int lane = threadIdx.x & 63, u = lane % UNITS, g = lane / UNITS;
   const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int sub = g & (a.lanes - 1);
@@ -59,20 +59,9 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const hsap_token_rows& x = a.x[n];
-    for (int h0 = sub; h0 < x.heads; h0 += FLIGHT * a.lanes) {
-      Unit r[FLIGHT];
-#pragma unroll
-      for (int y = 0; y < FLIGHT; ++y) {
-        const int h = h0 + y * a.lanes;
-        if (h < x.heads) r[y] = load_row<D>(x, t * x.in_stride + (int64_t)h * D, rot, u);
-      }
-#pragma unroll
-      for (int y = 0; y < FLIGHT; ++y) {
-        const int h = h0 + y * a.lanes;
-        if (h < x.heads)
-          store_row<D>(x, t * x.out_stride + (int64_t)h * D, rot, u, turn<D>(a.turn.rot, a.turn.interleaved, u, turned, r[y]));
-      }
-    }
+    turn_heads<D, 4>(
+        a.turn, turned, x.heads, sub, a.lanes, u, [&](int h) { return load_row<D>(x, t * x.in_stride + (int64_t)h * D, rot, u); },
+        [&](int h, const Unit& r) { store_row<D>(x, t * x.out_stride + (int64_t)h * D, rot, u, r); });
   }
 }
 
@@ -130,9 +119,8 @@ extern "C" hsap_status hsap_rotate(const hsap_rotation* rotation, int32_t head_d
   if (k) a.x[1] = *k;
   a.total = total;
   a.inverse = inverse != 0;
-  const int32_t most = 64 / (head_dim / 16), heads = q->heads > a.x[1].heads ? q->heads : a.x[1].heads;
-  a.lanes = 1;
-  while (a.lanes < most && a.lanes < heads) a.lanes *= 2;
+  const int32_t most = 64 / (head_dim / 16);
+  a.lanes = rows_at_a_time(q->heads > a.x[1].heads ? q->heads : a.x[1].heads, head_dim);
   const int64_t per = 4 * (most / a.lanes), blocks = (total + per - 1) / per;
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many tokens");
   hipStream_t s = (hipStream_t)hip_stream;

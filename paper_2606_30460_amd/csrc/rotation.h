@@ -134,6 +134,27 @@ __device__ __forceinline__ void store_bf16(__bf16* row, int rot, int u, const Un
   *(bf16x8*)(row + at[1]) = __builtin_convertvector(r.b, bf16x8);
 }
 
+// A token's rows of `heads` heads by one unit's cosines and sines, `lanes` rows of a wave at a time from `sub` on, FLIGHT of them
+// in flight: a lane forms them once for all heads.
+template <int D, int FLIGHT, typename Load, typename Store>
+__device__ __forceinline__ void turn_heads(const Turns& t, const UnitTurn& by, int heads, int sub, int lanes, int u, Load load, Store store) {
+  for (int h0 = sub; h0 < heads; h0 += FLIGHT * lanes) {
+    Unit r[FLIGHT];
+#pragma unroll
+    for (int y = 0; y < FLIGHT; ++y)
+      if (h0 + y * lanes < heads) r[y] = load(h0 + y * lanes);
+#pragma unroll
+    for (int y = 0; y < FLIGHT; ++y)
+      if (h0 + y * lanes < heads) store(h0 + y * lanes, turn<D>(t.rot, t.interleaved, u, by, r[y]));
+  }
+}
+// Rows of a token that a wave takes at a time: a power of two up to the rows that its lanes hold.
+inline int32_t rows_at_a_time(int32_t heads, int32_t head_dim) {
+  int32_t n = 1;
+  while (n < heads && n < 64 / (head_dim / 16)) n *= 2;
+  return n;
+}
+
 // Checks a rotation and fills in all of `out` but the positions (ops of hsap_rotate and hsap_cache_append_at).
 hsap_status check_rotation(const hsap_rotation* r, int32_t head_dim, Turns* out);
 
