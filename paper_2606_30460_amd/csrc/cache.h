@@ -80,6 +80,31 @@ HSAP_CACHE_HD Steps<STEP> cache_steps(int32_t plo, int32_t phi, int32_t cap, int
   return Steps<STEP>{ns, win0, lo, ns + (phi >= win0 ? (phi - win0) / STEP + 1 : 0)};
 }
 
+#if defined(__HIPCC__)
+// Last of n sequences whose items begin at `item` or before (item_base, rising with the sequence), with its tokens and its entry
+// of `values` (0 where that is NULL): 64 probes at a time, so that up to 64 sequences take one trip to memory.  `item` is the same
+// on every lane of a wave, and so is the result.
+struct Sequence {
+  int32_t s, begin, end, value;
+};
+__device__ __forceinline__ Sequence sequence_of(const int32_t* cu, int32_t n, int64_t num, int64_t den, int64_t add, int64_t item,
+                                                const int32_t* values) {
+  const int lane = threadIdx.x & 63;
+  int32_t lo = 0, len = n;
+  for (;;) {
+    const int32_t stride = (len + 63) >> 6, probe = min(lane * stride, len - 1);
+    const int32_t begin = cu[lo + probe], end = cu[lo + probe + 1], value = values ? values[lo + probe] : 0;
+    const bool below = lane * stride < len && item_base(begin, num, den, add, lo + probe) <= item;
+    const int32_t at = max(__popcll(__builtin_amdgcn_ballot_w64(below)) - 1, 0);
+    if (stride == 1)
+      return Sequence{__builtin_amdgcn_readfirstlane(lo + at), __builtin_amdgcn_readlane(begin, at), __builtin_amdgcn_readlane(end, at),
+                      __builtin_amdgcn_readlane(value, at)};
+    lo += at * stride;
+    len = min(stride, len - at * stride);
+  }
+}
+#endif
+
 constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
 constexpr int kMaxSplits = 128;  // of a row tile's tokens
 constexpr int kMaxMaskWords = HSAP_MAX_MASK_WORDS;
@@ -161,6 +186,7 @@ inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tota
   const int64_t grid = c.rows <= 32 ? kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv) : (narrow ? kTreeGrid64 : kTreeGrid128) / full;
   const int64_t shortest = c.rows <= 32 ? 256 : narrow ? 512 : 1024;
   c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxSplits, tokens / shortest), grid));
+  if (c.rows > 32 && 8 * full >= kTreeGrid128 / 2) c.splits = std::min(c.splits, 8);  // (more are joined by the slower kernel)
   return c;
 }
 

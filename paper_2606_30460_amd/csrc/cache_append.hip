@@ -111,17 +111,20 @@ __device__ __forceinline__ void rotate_q_at(const AppendArgs& a, int64_t wave) {
   if (first >= a.total_new) return;
   int64_t pos;
   if (a.cu) {
-    int32_t s = sequence_of(a.cu, a.d.num_seqs, 1, 1, 0, first);  // cu[s] <= first
-    if (t >= a.total_new || t >= a.cu[a.d.num_seqs]) return;      // (behind the last sequence: not read)
-    if (t >= a.cu[s + 1]) {
+    Sequence q = sequence_of(a.cu, a.d.num_seqs, 1, 1, 0, first, a.c.seq_lens);  // q.begin <= first
+    if (t >= a.total_new) return;
+    if (t >= q.end) {
       int32_t r = a.d.num_seqs;
-      while (r - s > 1) {
-        const int32_t mid = (s + r) >> 1;
-        if (a.cu[mid] <= t) s = mid;
+      if (t >= a.cu[r]) return;  // (behind the last sequence: not read)
+      while (r - q.s > 1) {
+        const int32_t mid = (q.s + r) >> 1;
+        if (a.cu[mid] <= t) q.s = mid;
         else r = mid;
       }
+      q.end = a.cu[q.s + 1];
+      q.value = a.c.seq_lens[q.s];
     }
-    pos = (int64_t)a.c.seq_lens[s] - (a.cu[s + 1] - t);
+    pos = (int64_t)q.value - (q.end - t);
   } else {
     if (t >= a.total_new) return;
     pos = (int64_t)a.c.seq_lens[t] - 1;
@@ -228,8 +231,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   const int64_t item = pair / a.d.heads_kv;
   const int32_t ps = a.d.page_size;
   // the sequence whose pages this item is one of
-  const int32_t s = sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item);
-  const int32_t t0 = a.cu[s], count = a.cu[s + 1] - t0, len = a.c.seq_lens[s];
+  const Sequence q = sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item, a.c.seq_lens);
+  const int32_t s = q.s, t0 = q.begin, count = q.end - t0, len = q.value;
   if (count <= 0 || len <= 0) return;
   const int64_t pos0 = (int64_t)len - count;  // position of the first new token
   const int64_t first = pos0 > 0 ? pos0 : 0;

@@ -51,6 +51,7 @@ __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const 
 // The sequence, first row and rows of a row tile; false where the tile is empty.
 struct RowTile {
   int32_t seq, t0, count, row0;  // row0: first row (token * group + head) of the tile within the sequence
+  int32_t len;                   // tokens of the sequence
 };
 __device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, int rows, RowTile& t) {
   if (!a.cu) {
@@ -59,18 +60,16 @@ __device__ __forceinline__ bool row_tile(const CacheAttnArgs& a, int32_t tile, i
     t.t0 = t.seq;
     t.count = 1;
     t.row0 = (tile - t.seq * per) * rows;
-    return t.seq < a.d.num_seqs;
+    if (t.seq >= a.d.num_seqs) return false;
+    t.len = max(0, a.c.seq_lens[t.seq]);
+    return true;
   }
-  int32_t s = 0, r = a.d.num_seqs;
-  while (r - s > 1) {
-    const int32_t mid = (s + r) >> 1;
-    if (item_base(a.cu[mid], a.group, rows, 1, mid) <= tile) s = mid;
-    else r = mid;
-  }
-  t.seq = s;
-  t.t0 = a.cu[s];
-  t.count = (int32_t)min((int64_t)a.cu[s + 1], a.total_q) - t.t0;
-  const int64_t row0 = (tile - item_base(t.t0, a.group, rows, 1, s)) * rows;
+  const Sequence q = sequence_of(a.cu, a.d.num_seqs, a.group, rows, 1, tile, a.c.seq_lens);
+  t.seq = q.s;
+  t.t0 = q.begin;
+  t.count = (int32_t)min((int64_t)q.end, a.total_q) - t.t0;
+  t.len = max(0, q.value);
+  const int64_t row0 = (tile - item_base(t.t0, a.group, rows, 1, q.s)) * rows;
   t.row0 = (int32_t)row0;
   return t.count > 0 && row0 < (int64_t)t.count * a.group;
 }

@@ -34,21 +34,6 @@ __device__ __forceinline__ uint4 recoded16(const uint4& w, float ratio) {
 }
 __device__ __forceinline__ void recode16(uint8_t* p, float ratio) { *(uint4*)p = recoded16(*(const uint4*)p, ratio); }
 
-// Last of n sequences whose items begin at `item` or before (cache.h's item_base, rising with the sequence): 64 probes at a
-// time, the same on every lane of a wave, as `item` has to be.
-__device__ __forceinline__ int32_t sequence_of(const int32_t* cu, int32_t n, int64_t num, int64_t den, int64_t add, int64_t item) {
-  const int lane = threadIdx.x & 63;
-  int32_t lo = 0, len = n;
-  while (len > 1) {
-    const int32_t stride = (len + 63) >> 6, probe = lane * stride;
-    const bool below = probe < len && item_base(cu[lo + probe], num, den, add, lo + probe) <= item;
-    const int32_t at = max(__popcll(__builtin_amdgcn_ballot_w64(below)) - 1, 0) * stride;
-    lo += at;
-    len = min(stride, len - at);
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
-}
-
 // The page's new scale; `kept` tokens before the new ones stay.  Sets inv to its reciprocal and ratio to what their codes
 // are multiplied by (1: they stay as they are).
 __device__ __forceinline__ float page_scale(float amax, bool kept, float old, float& inv, float& ratio) {

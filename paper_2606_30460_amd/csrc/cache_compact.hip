@@ -51,10 +51,19 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs a) {
   const int h = blockIdx.x % a.d.heads_kv;
   const int64_t item = blockIdx.x / a.d.heads_kv;
   const int32_t ps = a.d.page_size;
-  const int32_t s = FRESH ? sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item) : (int32_t)item;
-  const int32_t i0 = a.cu[s];
-  const int64_t count = min((int64_t)a.cu[s + 1], a.total) - i0;
-  const int32_t first = a.first ? max(a.first[s], 0) : 0;
+  int32_t s = (int32_t)item, i0, i1, first;
+  if constexpr (FRESH) {
+    const Sequence q = sequence_of(a.cu, a.d.num_seqs, 1, ps, 2, item, a.first);
+    s = q.s;
+    i0 = q.begin;
+    i1 = q.end;
+    first = max(q.value, 0);
+  } else {
+    i0 = a.cu[s];
+    i1 = a.cu[s + 1];
+    first = a.first ? max(a.first[s], 0) : 0;
+  }
+  const int64_t count = min((int64_t)i1, a.total) - i0;
   const int64_t nth = FRESH ? item - item_base(i0, 1, ps, 2, s) : 0;  // page of the list's
   if (a.new_lens && h == 0 && nth == 0 && tid == 0) a.new_lens[s] = first + (int32_t)max(count, (int64_t)0);
   if (count <= 0) return;

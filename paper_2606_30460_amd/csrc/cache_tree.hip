@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   const int32_t split = rest % a.splits, tile = rest / a.splits;
   RowTile rt;
   if (!row_tile(a, tile, ROWS, rt)) return;
-  const int32_t len = max(0, a.c.seq_lens[rt.seq]);
+  const int32_t len = rt.len;
   const int32_t ps = a.d.page_size, cap = a.d.table_width * ps;
   const int32_t nrows = rt.count * a.group;
   const int32_t last_row = min(rt.row0 + ROWS, nrows) - 1;

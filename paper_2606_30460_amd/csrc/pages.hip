@@ -41,7 +41,7 @@ __device__ __forceinline__ int32_t source_of(const PagesArgs& a, int32_t s) {
 }
 
 constexpr int kForkEntries = 16384;  // of the table, that a workgroup holds: columns for all rows
-constexpr int kForkThreads = 512;
+constexpr int kForkThreads = 1024;
 
 // A workgroup takes some columns of all rows, so that rows can change places.  One that takes them all writes the lengths too
 // (a second launch would: 8 rows of 63 pages 4.1 us in two, XXX in one).
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
 constexpr int kFewItems = 1024;
 __global__ __launch_bounds__(1024) void pages_reserve_few_kernel(PagesArgs a) {
   __shared__ int32_t waves[16], cu[kFewItems + 1], lens[kFewItems], list[kFewItems];
-  __shared__ int32_t shared[kFewItems];  // each item's page where it is shared, else -1
+  __shared__ __attribute__((aligned(16))) int32_t shared[kFewItems];  // each item's page where it is shared, else -1
   const int tid = threadIdx.x, ps = a.d.page_size;
   const int32_t n = a.d.num_seqs, items = (int32_t)a.items;
   // (free pages of the first stretch, under way while the places are found)
@@ -302,10 +302,16 @@ __global__ __launch_bounds__(1024) void pages_reserve_few_kernel(PagesArgs a) {
   if (count > 1) {
     int32_t writers = 0;
     bool last = true;
-    for (int32_t i = 0; i < items; ++i) {
-      const bool same = shared[i] == page;
-      writers += same;
-      last &= !same || i <= tid;
+#pragma unroll 4
+    for (int32_t i = 0; i < items; i += 4) {
+      const int4 x4 = *(const int4*)(shared + i);
+      const int32_t p4[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool same = p4[e] == page;
+        writers += same;
+        last &= !same | (i + e <= tid);
+      }
     }
     need = writers < count || !last;
   }
