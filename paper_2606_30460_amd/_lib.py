@@ -946,7 +946,18 @@ class Rotation:
 
 
 def _turned_rows(x, out, what: str, total: int, here: int) -> TokenRows:
-    f32 = [getattr(t, "dtype", None) is _dtypes["float32"] for t in (x, out)]
+    fp32, bf16 = _dtypes["float32"], _dtypes["bfloat16"]
+    f32 = x.dtype is fp32, getattr(out, "dtype", None) is fp32
+    try:  # (one pass over the attributes; what does not pass it is looked at again, for the message)
+        shape = x.shape
+        if (shape == out.shape and shape[0] == total > 1 and x.get_device() == here >= 0 and out.get_device() == here
+                and (f32[0] or x.dtype is bf16) and (f32[1] or out.dtype is bf16)):
+            _, heads, d = shape
+            (row, head, one), (out_row, out_head, out_one) = x.stride(), out.stride()
+            if one == out_one == 1 and (heads == 1 or head == out_head == d):
+                return TokenRows(x.data_ptr(), out.data_ptr(), row, out_row, heads, *f32)
+    except AttributeError:
+        pass
     d = x.shape[-1]
     src, in_stride = _token_rows(x, what, total, x.shape[1], d, here, "float32" if f32[0] else "bfloat16")
     dst, out_stride = _token_rows(out, what + "_out", total, x.shape[1], d, here, "float32" if f32[1] else "bfloat16")

@@ -42,7 +42,8 @@ __device__ __forceinline__ float codes_max(const uint4& w) {
 }
 
 // A workgroup moves K's and V's codes of a page and head, whose tokens it looks up once (16 sequences of 8k tokens, half of
-// them into fresh pages: 49 us with one each, XXX with both).  PER: units of 16 codes of a page per thread.
+// them into fresh pages: 49 us with a workgroup each, 46 with one for both, 39 since it holds no decoded values, so that seven
+// share a compute unit: 4.0 TB/s; a chain of list, table, codes and a maximum, four trips to memory).  PER: units of 16 codes of a page per thread.
 template <int D, int PER, bool FRESH>
 __global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs a) {
   constexpr int UNITS = D / 16;
@@ -101,7 +102,11 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs a) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) amax[x] = fmaxf(amax[x], codes_max(w[x][i]) * scale[x][i]);
+      for (int i = 0; i < PER; ++i) {
+        amax[x] = fmaxf(amax[x], codes_max(w[x][i]) * scale[x][i]);
+        // (decoded again below: sixteen values a unit, held until then, would take the registers of more workgroups)
+        asm volatile("" : "+v"(w[x][i].x), "+v"(w[x][i].y), "+v"(w[x][i].z), "+v"(w[x][i].w));
+      }
       if (page >= 0 && tid == 0) old_scale[x] = slot0 > 0 ? scales[x][(int64_t)page * a.d.heads_kv + h] : 0.f;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) amax[x] = fmaxf(amax[x], __shfl_xor(amax[x], o));
