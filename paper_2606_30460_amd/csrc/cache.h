@@ -171,8 +171,9 @@ inline CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tot
 //     of 8k) and 189 -> 150 (64 of 8k), 160 rows 265 -> 198 (8 of 32k)
 //   head_dim 64, 32 -> 64 rows:  30 rows 44 -> 34 (16 of 8k), 60 rows 65 -> 53 (64 of 2k), 250 rows 78 -> 56 (4 of 16k)
 // Splits: as many as fill the chip about once, but not shorter than their beginning, end and partials are worth (16 sequences
-// of 80 rows over 8k tokens: four splits 102, eight 79, sixteen 97).
-constexpr int64_t kTreeGrid128 = 1024, kTreeGrid64 = 768;
+// of 80 rows over 8k tokens: four splits 102, eight 79, sixteen 97); while there are few workgroups, down to 128 tokens (one of
+// 512 rows over 4k, two K/V heads: four splits 41, sixteen 24, 32 23; eight of 160 rows over 2k: two 47, four 35, eight 38).
+constexpr int64_t kTreeGrid128 = 1024, kTreeGrid64 = 768, kTreeFew = 320;
 inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
   const bool narrow = d.head_dim == 64;
@@ -186,7 +187,10 @@ inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tota
   const int64_t grid = c.rows <= 32 ? kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv) : (narrow ? kTreeGrid64 : kTreeGrid128) / full;
   const int64_t shortest = c.rows <= 32 ? 256 : narrow ? 512 : 1024;
   c.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxSplits, tokens / shortest), grid));
-  if (c.rows > 32 && 8 * full >= kTreeGrid128 / 2) c.splits = std::min(c.splits, 8);  // (more are joined by the slower kernel)
+  if (c.rows > 32) {
+    c.splits = (int32_t)std::max<int64_t>(c.splits, std::min(std::min<int64_t>(kMaxSplits, tokens / 128), kTreeFew / full));
+    if (8 * full >= kTreeGrid128 / 2) c.splits = std::min(c.splits, 8);  // (more are joined by the slower kernel)
+  }
   return c;
 }
 
