@@ -160,7 +160,7 @@ __device__ __forceinline__ int32_t block_scan(int32_t x, int32_t* waves, int32_t
 }
 
 // One workgroup.  Every place that is written and has a page takes its count off that page; where nobody else is left the
-// last of those sequences keeps it (refs holds -(s + 1) meanwhile), all others need a free one.
+// last of those places keeps it (refs holds -(item + 1) meanwhile), all others need a free one.
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
   __shared__ int32_t waves[16];
   constexpr int KEEP = -1, NONE = -2;  // of `work`: the place's page stays; nothing is written there
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
   for (int64_t i = tid; i < a.items; i += 1024) {
     Item x;
     if (item_of(a, i, x) && is_page(a.d, a.table[x.entry]) && count_now(a.refs + a.table[x.entry]) <= 0)
-      atomicMin(a.refs + a.table[x.entry], -(x.s + 1));
+      atomicMin(a.refs + a.table[x.entry], -(int32_t)(i + 1));
   }
   __syncthreads();
   int32_t need = 0;
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
     int32_t what = NONE;
     if (i < a.items && item_of(a, i, x)) {
       const int32_t page = a.table[x.entry];
-      what = is_page(a.d, page) && count_now(a.refs + page) == -(x.s + 1) ? KEEP : 0;
+      what = is_page(a.d, page) && count_now(a.refs + page) == -(int32_t)(i + 1) ? KEEP : 0;
     }
     int32_t total;
     const int32_t nth = block_scan(what == 0, waves, total);
@@ -413,9 +413,10 @@ extern "C" hsap_status hsap_pages_fork(const hsap_cache_desc* desc, int32_t* pag
   a.sinks = sinks;
   const int64_t all = (int64_t)desc->num_seqs * desc->table_width;
   a.columns = std::min(all <= kForkEntries / 4 ? desc->table_width : std::min(32, desc->table_width), kForkEntries / desc->num_seqs);
-  a.with_lens = source && a.columns == desc->table_width && desc->num_seqs <= kForkEntries / 4;
+  a.with_lens = source && a.columns == desc->table_width && desc->num_seqs <= (kForkEntries - all);
   hipStream_t s = (hipStream_t)hip_stream;
   const unsigned blocks = (unsigned)((desc->table_width + a.columns - 1) / a.columns);
+  if (blocks > kMaxBlocks256 / (kForkThreads / 256)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "table too wide for its rows");
   const size_t lds = (size_t)desc->num_seqs * (a.columns + a.with_lens) * 4;
   hipLaunchKernelGGL(pages_fork_kernel, dim3(blocks), dim3(kForkThreads), lds, s, a);
   if ((st = launched("pages_fork")) != HSAP_OK || !source || a.with_lens) return st;

@@ -93,6 +93,8 @@ static hsap_status check_token_rows(const char* what, const hsap_token_rows& x, 
   if (x.in_stride % 8 || x.out_stride % 8 || x.in_stride < x.heads * row || x.out_stride < x.heads * row)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "%s: row strides (%lld, %lld) must be multiples of 8 and at least %lld", what,
               (long long)x.in_stride, (long long)x.out_stride, (long long)(x.heads * row));
+  if (x.in == x.out && (x.in_stride != x.out_stride || !x.in_f32 != !x.out_f32))
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "%s: in place rows have one type and stride", what);
   return HSAP_OK;
 }
 

@@ -108,6 +108,8 @@ def test_bad_rotate_arguments():
     for over in (dict(heads=0), dict(src=0), dict(out=0), dict(src=4104), dict(out=4104), dict(in_stride=252), dict(out_stride=252),
                  dict(in_stride=192), dict(out_stride=248)):
         assert _rotate(q=_rows(**over)) == BAD and _rotate(k=_rows(**over)) == BAD, over
+    for over in (dict(in_f32=1), dict(out_f32=1), dict(out_stride=264)):         # in place, of two types or strides
+        assert _rotate(q=_rows(**over)) == BAD and "in place" in L.lib().hsap_last_error().decode()
     lib = L.lib()
     r, q = _rotation(), _rows()
     assert lib.hsap_rotate(None, 64, FAKE, 5, ctypes.byref(q), None, 0, None) == BAD
@@ -172,6 +174,7 @@ def test_bad_forks():
     assert _fork(window=0) == BAD and _fork(sinks=-1) == BAD
     for name in ("table", "lens", "refs"):
         assert _fork(**{name: None}) == BAD, name
+    assert _fork(d=_desc(num_seqs=16384, table_width=2 ** 27 - 1)) == BAD and "too wide" in L.lib().hsap_last_error().decode()
     assert _fork(d=_desc(num_seqs=16385)) == NONE and _fork(d=_desc(num_seqs=0)) == L.HSAP_OK
 
 

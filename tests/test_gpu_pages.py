@@ -69,7 +69,7 @@ def test_fork(size):
 
 def test_fork_of_tables_of_every_shape():
     rng = np.random.default_rng(0)
-    for rows, width in ((1, 1), (1, 1000), (300, 33), (600, 40), (2000, 7), (16384, 1)):
+    for rows, width in ((1, 1), (1, 1000), (300, 33), (512, 32), (4000, 1), (600, 40), (2000, 7), (8192, 1), (16384, 1)):
         lens = rng.integers(0, 16 * width + 1, rows)
         print(rows, width, flush=True)
         _check_fork(lens, width, 16, rng.integers(-1, rows, rows), seed=rows)
@@ -174,6 +174,26 @@ def test_reserve_shared_by_all_and_by_some():
     torch.cuda.synchronize()
     assert cache.page_table.tolist() == [[0, 4, 5], [1, 2, 3]] and pairs.tolist() == [[1, 0], [-1, -1]]
     assert r.tolist() == [1, 1, 1, 1, 1, 1, 0, 0, 0]
+
+
+@pytest.mark.parametrize("rows", [3, 1500])
+def test_reserve_of_a_page_twice_in_a_row(rows):
+    # one page at two places of the same sequence, both written: the last one keeps it
+    table = np.full((rows, 4), -1)
+    table[:, :3] = np.arange(rows)[:, None] * 2 + np.array([0, 1, 1])
+    refs = P.counts(table, 2 * rows + 9)
+    refs[-9:-7] = 1
+    lens, new = np.full(rows, 20), np.zeros(rows, int)
+    lens[[0, rows - 1]], new[[0, rows - 1]] = 40, 20                # places 20 .. 39: the second page, partly, and the third
+    cache, r = _cache(table, lens, len(refs)), _dev(refs)
+    pairs, missing = torch.empty(rows, 2, dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(L.pages_reserve_workspace(cache, 40), dtype=torch.uint8, device="cuda")
+    L.pages_reserve(cache, r, _dev(_cu(new)), 40, pairs, missing, ws)
+    torch.cuda.synchronize()
+    want, want_refs, want_pairs, short = P.reserve(table, lens, refs, _cu(new), 16)
+    assert int(missing) == short == 0 and np.array_equal(_bits(pairs), want_pairs)
+    got = _bits(cache.page_table)
+    assert np.array_equal(got, want) and np.array_equal(_bits(r), want_refs) and got[0, 1] != got[0, 2] == 1
 
 
 @pytest.mark.parametrize("size,hkv,d", [(16, 1, 64), (32, 3, 128), (128, 8, 128), (64, 5, 64), (128, 9, 128)])

@@ -278,6 +278,40 @@ def test_append_at_its_places_is_the_append(interleaved):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+def test_replays_follow_positions_and_lengths():
+    held, hkv, d, most = np.array([100, 3, 40]), 2, 128, 50
+    p = Pages(held + most, 32, hkv, d, seed=4).fill(held)
+    caches = [p.device(held) for _ in range(2)]
+    r = L.Rotation(_cos_sin(200, 96), np.arange(48) % 3)
+    n = most
+    g = torch.Generator().manual_seed(0)
+    q, k, v = (torch.randn(n, h, d, generator=g).to(torch.bfloat16).cuda() for h in (6, hkv, hkv))
+    at, cu = torch.zeros(3, n, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    outs = [[torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(k)] for _ in range(2)]
+
+    def step(which):
+        L.rotate(r, at, q, outs[which][0], inverse=True)
+        L.cache_append_at(caches[which], k, v, cu, r, at, q=q, q_out=outs[which][1], k_out=outs[which][2])
+
+    for which in (0, 1):                           # (all tokens rotated at 0, none appended: what a skipped one keeps)
+        step(which)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    for turn, new in enumerate(([20, 1, 29], [0, 50, 0], [17, 16, 16])):
+        cu.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)))
+        at.copy_(torch.randint(-2, 200, at.shape, generator=g, dtype=torch.int32))
+        for c in caches:
+            c.seq_lens.copy_(torch.from_numpy((held + new).astype(np.int32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(1)
+        torch.cuda.synchronize()
+        for x, y in zip(list(caches[0].tensors) + outs[0], list(caches[1].tensors) + outs[1]):
+            same = torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+            assert same, turn
+
+
 def test_refused_arguments():
     cs = _cos_sin(10, 64)
     for bad in (dict(pair_axis=[0] * 31), dict(pair_axis=[4] + [0] * 31), dict(pair_axis=[-1] + [0] * 31), dict(axes=5), dict(axes=0)):

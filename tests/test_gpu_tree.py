@@ -263,7 +263,7 @@ def test_large_scores():
 
 
 def test_a_chain_is_the_causal_attention():
-    """Bit for bit, where both take the same kernel."""
+    """Both against the causal oracle, on the same cache."""
     for held, new, hq, hkv, d, width in (([300, 40], [9, 30], 8, 2, 128, None), ([500, 90], [150, 100], 16, 8, 64, 800)):
         lens, cu = np.add(held, new), _cu(new)
         p = Pages(lens, 16, hkv, d, seed=1, width=width).fill(lens)
@@ -320,6 +320,72 @@ def test_replays_follow_masks_and_lengths():
         for x, t in out.items():
             a, b = (got[x][:, :m], t[:, :m]) if x == "lse" else (got[x][:m], t[:m])
             assert torch.equal(a, b), (turn, x)
+
+
+@pytest.mark.parametrize("d,hkv", [(128, 8), (64, 16)])
+def test_offsets_beyond_32_bits(d, hkv):
+    """Pages behind the first 2^32 bytes of the codes give what the same pages do at the beginning, for every number of rows;
+    an append at positions writes them."""
+    size = 128
+    pages = 2 ** 32 // (hkv * size * d) + 8
+    small = Pages([300], size, hkv, d, seed=1, spare=0).fill([300])
+    t = small.device()
+    codes = [torch.zeros((pages, hkv, size, d), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.ones((pages, hkv), device="cuda") for _ in range(2)]
+    far = pages - 3
+    for big, x in zip(codes + scales, t.tensors[:4]):
+        big[far:] = x
+    cache = L.KVCache(*codes, *scales, t.page_table + far, t.seq_lens)
+    for new, group in ((1, 2), (12, 2), (100, 2)):
+        n, hq, cu = new, hkv * group, _cu([new])
+        mask, positions = _masks(_parents([new], np.random.default_rng(0)), cu, [300], 2)
+        q = torch.randn(n, hq, d, generator=torch.Generator().manual_seed(new)).to(torch.bfloat16).cuda()
+        outs = [torch.empty_like(q) for _ in range(2)]
+        ws = torch.empty(L.cache_tree_attn_workspace(t, hq, n), dtype=torch.uint8, device="cuda")
+        for c, o in zip((t, cache), outs):
+            L.cache_tree_attn(c, hq, 0.1, q, _dev(cu), mask, positions, o, None, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(*outs) and bool(outs[0].any()), new
+    r = L.Rotation(_cos_sin(50, d), np.arange(d // 2) % 3)
+    k, v = (torch.randn(40, hkv, d, generator=torch.Generator().manual_seed(x)).to(torch.bfloat16).cuda() for x in (1, 2))
+    at = torch.arange(120, dtype=torch.int32, device="cuda").reshape(3, 40) % 50
+    for c in (t, cache):
+        L.cache_append_at(c, k, v, _dev(_cu([40])), r, at)
+        L.cache_append_at(c, k[:1], v[:1], None, r, at[:, :1].contiguous())
+    torch.cuda.synchronize()
+    for big, x in zip(codes + scales, t.tensors[:4]):
+        assert torch.equal(big[far:].view(torch.uint8), x.view(torch.uint8))
+
+
+def test_many_drafted_tokens():
+    # masks of sixteen words, drafts behind several pages, more of them than tokens before
+    _check([5, 700], [1024, 3], 128, 2, 2, 128, seed=1, chain=True)
+    _check([100], [1000], 32, 1, 1, 64, 200, 3, seed=2)
+
+
+def test_graphs_that_share_a_workspace():
+    held, new, hq, hkv, d = np.array([3000, 500]), np.array([20, 33]), 8, 2, 128
+    p = Pages(held + new, 64, hkv, d, seed=3).fill(held + new)
+    cache, cu = p.device(), _cu(new)
+    mask, positions = _masks(_parents(new, np.random.default_rng(0)), cu, held + new, 1)
+    qs = [torch.randn(53, hq, d, generator=torch.Generator().manual_seed(x)).to(torch.bfloat16).cuda() for x in range(2)]
+    outs, cu = [torch.empty_like(q) for q in qs], _dev(cu)
+    ws = torch.empty(L.cache_tree_attn_workspace(cache, hq, 53), dtype=torch.uint8, device="cuda")
+    want, graphs = [], []
+    for q, o in zip(qs, outs):
+        L.cache_tree_attn(cache, hq, 0.1, q, cu, mask, positions, o, None, ws)
+        torch.cuda.synchronize()
+        want.append(o.clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            L.cache_tree_attn(cache, hq, 0.1, q, cu, mask, positions, o, None, ws)
+    for turn in range(3):
+        for o in outs:
+            o.zero_()
+        for g in graphs[::1 if turn else -1]:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want)), turn
 
 
 def test_two_streams():
