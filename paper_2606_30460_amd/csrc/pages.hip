@@ -113,19 +113,19 @@ __device__ __forceinline__ bool place_of(const PagesArgs& a, int32_t s, int32_t 
   x.part = lo > at * ps;
   return true;
 }
-__device__ __forceinline__ bool item_of(const PagesArgs& a, int64_t item, Item& x) {
+__device__ __forceinline__ bool item_of(const PagesArgs& a, const int32_t* cu, int64_t item, Item& x) {
   const int32_t ps = a.d.page_size;
   int32_t s = 0, t0, count;
   int64_t nth = 0;
-  if (a.cu) {
+  if (cu) {
     int32_t r = a.d.num_seqs;
     while (r - s > 1) {
       const int32_t mid = (s + r) >> 1;
-      if (item_base(a.cu[mid], 1, ps, 2, mid) <= item) s = mid;
+      if (item_base(cu[mid], 1, ps, 2, mid) <= item) s = mid;
       else r = mid;
     }
-    t0 = a.cu[s];
-    count = a.cu[s + 1] - t0;
+    t0 = cu[s];
+    count = cu[s + 1] - t0;
     nth = item - item_base(t0, 1, ps, 2, s);
   } else {
     s = (int32_t)item;
@@ -160,21 +160,29 @@ __device__ __forceinline__ int32_t block_scan(int32_t x, int32_t* waves, int32_t
   return before + sum - x;
 }
 
+constexpr int kReserveSeqs = 8192;  // searched in LDS (one new token of each of 4000: 167 us from memory, 125)
+
 // One workgroup.  Every place that is written and has a page takes its count off that page; where nobody else is left the
 // last of those places keeps it (refs holds -(item + 1) meanwhile), all others need a free one.
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
-  __shared__ int32_t waves[16];
+  __shared__ int32_t waves[16], held[kReserveSeqs + 1];
   constexpr int KEEP = -1, NONE = -2;  // of `work`: the place's page stays; nothing is written there
   const int tid = threadIdx.x;
+  const int32_t* cu = a.cu;
+  if (a.cu && a.d.num_seqs <= kReserveSeqs) {
+    for (int32_t s = tid; s <= a.d.num_seqs; s += 1024) held[s] = a.cu[s];
+    cu = held;
+    __syncthreads();
+  }
   for (int32_t s = tid; s < 2 * a.d.num_seqs; s += 1024) a.pairs[s] = -1;
   for (int64_t i = tid; i < a.items; i += 1024) {
     Item x;
-    if (item_of(a, i, x) && is_page(a.d, a.table[x.entry])) atomicAdd(a.refs + a.table[x.entry], -1);
+    if (item_of(a, cu, i, x) && is_page(a.d, a.table[x.entry])) atomicAdd(a.refs + a.table[x.entry], -1);
   }
   __syncthreads();
   for (int64_t i = tid; i < a.items; i += 1024) {
     Item x;
-    if (item_of(a, i, x) && is_page(a.d, a.table[x.entry]) && count_now(a.refs + a.table[x.entry]) <= 0)
+    if (item_of(a, cu, i, x) && is_page(a.d, a.table[x.entry]) && count_now(a.refs + a.table[x.entry]) <= 0)
       atomicMin(a.refs + a.table[x.entry], -(int32_t)(i + 1));
   }
   __syncthreads();
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
     const int64_t i = i0 + tid;
     Item x;
     int32_t what = NONE;
-    if (i < a.items && item_of(a, i, x)) {
+    if (i < a.items && item_of(a, cu, i, x)) {
       const int32_t page = a.table[x.entry];
       what = is_page(a.d, page) && count_now(a.refs + page) == -(int32_t)(i + 1) ? KEEP : 0;
     }
@@ -212,19 +220,19 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(PagesArgs a) {
   if (short_of) {  // as if nothing had been asked
     for (int64_t i = tid; i < a.items; i += 1024) {
       Item x;
-      if (a.work[i] == KEEP && item_of(a, i, x)) atomicExch(a.refs + a.table[x.entry], 0);
+      if (a.work[i] == KEEP && item_of(a, cu, i, x)) atomicExch(a.refs + a.table[x.entry], 0);
     }
     __syncthreads();
     for (int64_t i = tid; i < a.items; i += 1024) {
       Item x;
-      if (a.work[i] != NONE && item_of(a, i, x) && is_page(a.d, a.table[x.entry])) atomicAdd(a.refs + a.table[x.entry], 1);
+      if (a.work[i] != NONE && item_of(a, cu, i, x) && is_page(a.d, a.table[x.entry])) atomicAdd(a.refs + a.table[x.entry], 1);
     }
     return;
   }
   for (int64_t i = tid; i < a.items; i += 1024) {
     const int32_t what = a.work[i];
     Item x;
-    if (what == NONE || !item_of(a, i, x)) continue;
+    if (what == NONE || !item_of(a, cu, i, x)) continue;
     const int32_t old = a.table[x.entry];
     if (what == KEEP) {
       atomicExch(a.refs + old, 1);

@@ -125,6 +125,12 @@ def test_windows_and_sinks(window, sinks):
     _check([30, 5], [200, 90], 32, 2, 2, 64, window, sinks, chain=True, seed=4)
 
 
+def test_more_heads_than_a_tile_has_rows():
+    for d in (64, 128):
+        _check([70, 300], [2, 5], 32, 160, 1, d, seed=d)
+        _check([70, 300, -1], [1, 1, 1], 32, 160, 1, d, one=True, seed=d, width=40)
+
+
 def test_one_token_each():
     held = np.array([0, 1, 16, 40, 130, 333, 700, -1])
     for one in (True, False):
