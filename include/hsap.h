@@ -1017,7 +1017,11 @@ hsap_status hsap_rotate(const hsap_rotation* rotation, int32_t head_dim, const i
  * hsap_cache_append_at -- hsap_cache_append with the rotation by positions given for every new token, device int32
  * [axes, total_new], instead of by its place in its sequence.  Where a token goes (its place, page and slot) follows
  * seq_lens and cu_new as there, and so does everything else; what is said there of cos_sin_rows holds for the positions.
- * Of a page whose first token is skipped the scale is that of the tokens that are not.
+ * A skipped token changes neither its place nor its page's scale: positions of -1 leave a sequence as it is, whose last place
+ * may hold a token already.  Of a page whose first place is among a call's and skipped, the scale is that of the call's tokens
+ * there that are not; where all of them are, the page keeps its scale, and a later call, whose tokens come behind, takes
+ * it for that of tokens before them, as any append does.  A caller that leaves a page's first places out for good, and not in
+ * the call that writes those behind them, sets the page's scales to 0 between the two.
  */
 hsap_status hsap_cache_append_at(const hsap_cache_desc* desc, const hsap_cache* cache, const void* k, int64_t k_stride,
                                  const void* v, int64_t v_stride, const int32_t* cu_new, int64_t total_new,

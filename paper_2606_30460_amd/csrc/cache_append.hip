@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void cache_append_one_kernel(AppendArgs a) {
   Unit x = load_bf16<D>(src + (int64_t)h * D, rot, u);
   const int32_t pos = a.c.seq_lens[s] - 1;
   Place at;
-  if (!place<D, AT>(a, s, pos, at)) return;
+  if (!place<D, AT>(a, s, pos, at)) return;  // (a place that may hold a token already: the page keeps its scale)
   if (!is_v && a.turn.rot) x = turned_unit<D, AT>(a, at, pos, u, x);
   if (!is_v && a.k_out) store_bf16<D>(a.k_out + (s * a.d.heads_kv + h) * D, rot, u, x);
   const int32_t page = cache_page(a.c.page_table + s * a.d.table_width, a.d.table_width, a.d.num_pages, a.d.page_size, pos);
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   if ((tid & 63) == 0) wave_max[tid >> 6] = amax;
   __syncthreads();
   amax = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
-  if (AT && amax < 0.f) return;
+  if (AT && amax < 0.f) return;  // (places that may hold tokens already: the page keeps its scale)
   float inv, ratio;
   const float now = page_scale(amax, slot0 > 0, old_scale, inv, ratio);
   if (ratio != 1.f)
