@@ -952,7 +952,8 @@ int64_t hsap_pages_reserve_workspace(const hsap_cache_desc* desc, int64_t total_
  *               through) is changed then: look at it before the append where that can be.
  *   workspace   device, 16-byte aligned, workspace_bytes >= hsap_pages_reserve_workspace; contents ignored.  Calls that
  *               overlap in time need workspaces of their own.
- * Places behind the table are left out, as by the append.  One launch on `stream`.
+ * Places behind the table are left out, as by the append.  Without sequences missing alone is written; the arrays may be NULL.
+ * One launch on `stream`.
  */
 hsap_status hsap_pages_reserve(const hsap_cache_desc* desc, int32_t* page_table, const int32_t* seq_lens, int32_t* refs,
                                const int32_t* cu_new, int64_t total_new, int32_t* pairs, int32_t* missing, void* workspace,

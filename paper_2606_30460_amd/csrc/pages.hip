@@ -462,6 +462,10 @@ extern "C" hsap_status hsap_pages_reserve(const hsap_cache_desc* desc, int32_t* 
   a.missing = missing;
   a.work = (int32_t*)workspace;
   a.items = desc->num_seqs ? reserve_items(*desc, !cu_new, total_new) : 0;
+  if (desc->num_seqs == 0) {  // (the kernel writes missing; arrays that may be NULL then are not read)
+    a.d.num_pages = 0;
+    a.cu = nullptr;
+  }
   if (workspace_bytes < 8 * a.items)
     HSAP_FAIL(HSAP_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)(8 * a.items));
   if (a.items <= kFewItems && desc->num_seqs <= kFewItems)
