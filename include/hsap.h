@@ -903,7 +903,7 @@ hsap_status hsap_cache_tree_attn(const hsap_cache_desc* desc, const hsap_cache* 
  *               and none of them holding a token to be moved; faster for long lists.  NULL: in place, in the pages of
  *               page_table, which then are the sequence's own from place first[s] on.
  *   new_lens    device int32 [num_seqs], or NULL: receives first[s] + the length of its list.  May be cache->seq_lens, which
- *               is not read.
+ *               is not read, but overlaps no input (first least of all, which is checked).
  * A page's scale is that of an append: the smallest power of two for the values moved into it, and at least the old one
  * where the page holds tokens before them (whose codes are encoded anew if it rises).  Moved codes are multiplied by the old
  * scale over the new in fp32 and rounded to nearest even, once: with powers of two exact but below e4m3's normal range.  Places

@@ -1059,7 +1059,7 @@ def cache_tree_attn(cache: KVCache, heads_q: int, softmax_scale: float, q, cu_ne
 def cache_compact(cache: KVCache, keep, cu_keep, first=None, dst_table=None, new_lens=None, stream=None) -> None:
     """hsap_cache_compact: of every sequence the tokens at places keep[cu_keep[s] ..] (int32, ascending) move to places
     first[s] .. (None: 0 ..), in place or into the pages of dst_table int32 [num_seqs, table_width]; new_lens int32
-    [num_seqs] takes the lengths (cache.seq_lens may be given)."""
+    [num_seqs] takes the lengths (cache.seq_lens may be given, but not what first is)."""
     here, c = _cache_here(cache), cache.desc
     _check(lib().hsap_cache_compact(
         *cache._refs, _arg(keep, "int32", "keep", None, here), _arg(cu_keep, "int32", "cu_keep", c.num_seqs + 1, here),

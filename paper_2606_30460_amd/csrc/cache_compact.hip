@@ -164,6 +164,10 @@ extern "C" hsap_status hsap_cache_compact(const hsap_cache_desc* desc, const hsa
   if (total_keep < 0 || total_keep > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_keep %lld", (long long)total_keep);
   if (desc->num_seqs == 0) return HSAP_OK;
   if (!cu_keep || (total_keep && !keep)) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL pointer argument");
+  // (head 0's workgroups write new_lens while others still read first)
+  const uintptr_t lens = (uintptr_t)new_lens, kept = (uintptr_t)first, bytes = (uintptr_t)desc->num_seqs * sizeof(int32_t);
+  if (new_lens && first && lens < kept + bytes && kept < lens + bytes)
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "first and new_lens must not overlap");
   CompactArgs a{*desc, *cache, keep, cu_keep, total_keep, first, dst_table, new_lens};
   const int64_t items = dst_table ? item_base(total_keep, 1, desc->page_size, 2, desc->num_seqs) : desc->num_seqs;
   const int64_t blocks = items * desc->heads_kv;

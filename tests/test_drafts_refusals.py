@@ -1,0 +1,21 @@
+"""Calls of the drafts' entry points that are refused, or are not, at the edges of what their arguments may be (no GPU)."""
+import ctypes
+
+from paper_2606_30460_amd import _lib as L
+from test_drafts_abi import BAD, FAKE, _compact, _desc
+
+
+def _at(address):
+    return ctypes.c_void_p(address)
+
+
+def test_compaction_whose_lengths_overlap_its_first_places():
+    # head 0 writes new_lens[s] while the other heads, and in fresh pages the other pages, still read first
+    for dst in (None, FAKE):
+        for lens in (8192, 8192 - 8, 8192 + 8):                 # three sequences: twelve bytes
+            assert _compact(first=_at(8192), lens=_at(lens), dst=dst) == BAD, lens
+            assert "overlap" in L.lib().hsap_last_error().decode()
+        for first, lens in ((None, 8192), (8192, None), (8192, 8192 + 12), (8192, 8192 - 12)):
+            # (nothing is launched: these have too many heads)
+            assert _compact(d=_desc(heads_kv=2 ** 24), first=first and _at(first), lens=lens and _at(lens), dst=dst) == BAD
+            assert "too many" in L.lib().hsap_last_error().decode()
