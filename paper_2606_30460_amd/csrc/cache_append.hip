@@ -426,7 +426,7 @@ extern "C" hsap_status hsap_cache_append_at(const hsap_cache_desc* desc, const h
   if ((st = check_new(desc, cu_new, total_new)) != HSAP_OK) return st;
   Turns t{};
   if ((st = check_rotation(rotation, desc->head_dim, &t)) != HSAP_OK) return st;
-  if (!positions) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL positions");
+  if (!positions && total_new > 0 && desc->num_seqs > 0) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "NULL positions");
   t.positions = positions;
   t.stride = total_new;
   return append(desc, cache, k, k_stride, v, v_stride, cu_new, total_new, t, k_out, q, q_stride, heads_q, q_out, hip_stream);

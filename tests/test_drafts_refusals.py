@@ -2,7 +2,7 @@
 import ctypes
 
 from paper_2606_30460_amd import _lib as L
-from test_drafts_abi import BAD, FAKE, _compact, _desc
+from test_drafts_abi import BAD, FAKE, _append, _compact, _desc
 
 
 def _at(address):
@@ -19,3 +19,11 @@ def test_compaction_whose_lengths_overlap_its_first_places():
             # (nothing is launched: these have too many heads)
             assert _compact(d=_desc(heads_kv=2 ** 24), first=first and _at(first), lens=lens and _at(lens), dst=dst) == BAD
             assert "too many" in L.lib().hsap_last_error().decode()
+
+
+def test_an_append_of_nothing_needs_no_positions():
+    # (an empty tensor has no address)
+    assert _append(cu=FAKE, total=0, positions=None) == L.HSAP_OK
+    assert _append(d=_desc(num_seqs=0), total=0, positions=None) == L.HSAP_OK
+    assert _append(d=_desc(num_seqs=0), cu=FAKE, total=5, positions=None) == L.HSAP_OK
+    assert _append(positions=None) == BAD and _append(cu=FAKE, positions=None) == BAD

@@ -97,3 +97,14 @@ def test_the_scale_kept_is_that_of_tokens_before(former):
     _step(cache, p, np.full(3, 39), [4, 4, 4], at, pair_axis, cs, 1, False)
     _same(cache, p)
     assert (p.scales["k"][p.table[:, 1]] == former).all() == (former > 1)
+
+
+def test_an_append_of_nothing():
+    """A step without new tokens: empty tensors, which have no address."""
+    p = Pages([20] * 3, 16, HKV, 64, 1).fill([20] * 3)
+    cache = p.device()
+    k = torch.empty(0, HKV, 64, dtype=torch.bfloat16, device="cuda")
+    r = L.Rotation(_cos_sin(ROWS, 64), np.arange(32) % 2)
+    L.cache_append_at(cache, k, k, _int32([0] * 4), r, torch.empty(2, 0, dtype=torch.int32, device="cuda"), k_out=k, q=k, q_out=k)
+    torch.cuda.synchronize()
+    _same(cache, p)
