@@ -952,6 +952,7 @@ int64_t hsap_pages_reserve_workspace(const hsap_cache_desc* desc, int64_t total_
  *               through) is changed then: look at it before the append where that can be.
  *   workspace   device, 16-byte aligned, workspace_bytes >= hsap_pages_reserve_workspace; contents ignored.  Calls that
  *               overlap in time need workspaces of their own.
+ * total_new / page_size + 2 * num_seqs <= 2^29, else HSAP_ERR_INVALID_ARG.
  * Places behind the table are left out, as by the append.  Without sequences missing alone is written; the arrays may be NULL.
  * One launch on `stream`.
  */

@@ -395,6 +395,9 @@ static hsap_status check_reserve(const hsap_cache_desc* desc, int64_t total_new,
   const hsap_status st = check_cache_desc(desc, pages);
   if (st != HSAP_OK) return st;
   if (total_new < 0 || total_new > INT32_MAX) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "bad total_new %lld", (long long)total_new);
+  // (numbers of places are int32, negative ones mark pages, and loops go on by 1024)
+  if (reserve_items(*desc, false, total_new) > (int64_t(1) << 29))
+    HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many places: %lld tokens of %d sequences", (long long)total_new, desc->num_seqs);
   return HSAP_OK;
 }
 

@@ -2,7 +2,7 @@
 import ctypes
 
 from paper_2606_30460_amd import _lib as L
-from test_drafts_abi import BAD, FAKE, _append, _compact, _desc
+from test_drafts_abi import BAD, FAKE, _append, _compact, _desc, _reserve
 
 
 def _at(address):
@@ -27,3 +27,15 @@ def test_an_append_of_nothing_needs_no_positions():
     assert _append(d=_desc(num_seqs=0), total=0, positions=None) == L.HSAP_OK
     assert _append(d=_desc(num_seqs=0), cu=FAKE, total=5, positions=None) == L.HSAP_OK
     assert _append(positions=None) == BAD and _append(cu=FAKE, positions=None) == BAD
+
+
+def test_reservations_of_more_places_than_their_numbers_hold():
+    # places are counted in 32 bits, with a sign
+    lib = L.lib()
+    for seqs, total in ((2 ** 31 - 1, 5), (2 ** 30, 5), (2 ** 28, 2 ** 20), (2 ** 28 - 2 ** 20, 2 ** 31 - 1)):
+        wide = _desc(num_seqs=seqs)
+        assert lib.hsap_pages_reserve_workspace(ctypes.byref(wide), total) == -1, (seqs, total)
+        assert _reserve(d=wide, total=total) == BAD, (seqs, total)
+        assert "too many" in lib.hsap_last_error().decode()
+        assert _reserve(d=wide, cu=None, total=seqs) == BAD
+    assert lib.hsap_pages_reserve_workspace(ctypes.byref(_desc(num_seqs=2 ** 27)), 2 ** 31 - 1) == 8 * (2 ** 28 + (2 ** 31 - 1) // 16)
