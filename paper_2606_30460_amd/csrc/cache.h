@@ -109,9 +109,10 @@ constexpr int kChunkRows = 128;  // rows of a workgroup of cache_chunk_kernel
 constexpr int kMaxSplits = 128;  // of a row tile's tokens
 constexpr int kMaxMaskWords = HSAP_MAX_MASK_WORDS;
 
-// How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip, each of at least 256 tokens.
+// How a call is cut: row tiles, and splits of a tile's tokens so that the grid fills the chip (each of at least 256 of the
+// table's tokens, a tree's of 128 to 1024).
 struct CacheCut {
-  int rows;  // of a tile: 16 or 32 (cache_attn_kernel), kChunkRows (cache_chunk_kernel)
+  int rows;  // of a tile: 16 or 32 (cache_attn_kernel), kChunkRows (cache_chunk_kernel), of a tree 64 or 128 (cache_tree_kernel)
   bool once;  // cache_attn_kernel's ONCE
   int64_t tiles;
   int32_t splits;
@@ -170,9 +171,12 @@ inline CacheCut cache_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tot
 //   head_dim 128, 32 -> 128 rows:  30 rows 58 -> 64 (16 sequences of 8k tokens), 60 rows 83 -> 78 (32 of 4k), 80 rows 98 -> 79 (16
 //     of 8k) and 189 -> 150 (64 of 8k), 160 rows 265 -> 198 (8 of 32k)
 //   head_dim 64, 32 -> 64 rows:  30 rows 44 -> 34 (16 of 8k), 60 rows 65 -> 53 (64 of 2k), 250 rows 78 -> 56 (4 of 16k)
-// Splits: as many as fill the chip about once, but not shorter than their beginning, end and partials are worth (16 sequences
-// of 80 rows over 8k tokens: four splits 102, eight 79, sixteen 97); while there are few workgroups, down to 128 tokens (one of
-// 512 rows over 4k, two K/V heads: four splits 41, sixteen 24, 32 23; eight of 160 rows over 2k: two 47, four 35, eight 38).
+// Splits: so many that the grid, counted as if sequences' rows filled their tiles one behind the other, has kTreeGrid workgroups at
+// most, but not shorter than their beginning, end and partials are worth (16 sequences of 80 rows over 8k tokens: four splits 102,
+// eight 79, sixteen 97); while there are few workgroups, down to 128 tokens (one of 512 rows over 4k, two K/V heads: four splits
+// 41, sixteen 24, 32 23; eight of 160 rows over 2k: two 47, four 35, eight 38).  A tile never spans sequences, so that short ones give
+// more workgroups than counted (32 sequences of up to 96 rows, eight heads: 416 counted, 992 with work), and the constants are what these
+// calls took best, not what the chip holds at once (768 at head_dim 128, 1024 at 64).
 constexpr int64_t kTreeGrid128 = 1024, kTreeGrid64 = 768, kTreeFew = 320;
 inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t total_q, bool one_each, int64_t tokens) {
   CacheCut c;
@@ -182,7 +186,7 @@ inline CacheCut tree_cut(const hsap_cache_desc& d, int32_t heads_q, int64_t tota
   c.once = false;
   c.rows = rows <= 16 ? 16 : narrow ? 64 : rows <= 32 ? 32 : 128;
   c.tiles = one_each ? (int64_t)d.num_seqs * ((group + c.rows - 1) / c.rows) : item_base(total_q, group, c.rows, 1, d.num_seqs);
-  // (workgroups that do something: c.tiles counts a tile more per sequence)
+  // (workgroups of full tiles without splits; c.tiles counts a tile more per sequence)
   const int64_t full = std::max<int64_t>(1, (one_each ? c.tiles : (total_q * group + c.rows - 1) / c.rows) * d.heads_kv);
   const int64_t grid = c.rows <= 32 ? kCacheGrid / std::max<int64_t>(1, c.tiles * d.heads_kv) : (narrow ? kTreeGrid64 : kTreeGrid128) / full;
   const int64_t shortest = c.rows <= 32 ? 256 : narrow ? 512 : 1024;

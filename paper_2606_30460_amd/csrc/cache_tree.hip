@@ -1,9 +1,11 @@
 // Trees of drafted tokens: masks and positions from each one's parent, and the attention of many rows.
 //
 // A token's mask names itself and its ancestors among the drafted tokens of its sequence, its position is that of its
-// depth: the drafted tokens stand behind `base` tokens, a token without a parent at position base.  A thread walks one
-// chain of parents (their numbers fall, so every walk ends) and collects one word of a mask: a launch and as many reads
-// of LDS as the tree is deep (32 trees of 24: 2.8 us).
+// depth: the drafted tokens stand behind `base` tokens, a token without a parent at position base.  A thread forms one word
+// of a token's mask, and walks the token's whole chain of parents for it (their numbers fall, so every walk ends): of a sequence
+// 256 words at a time, each as many dependent reads of LDS as its token is deep.  A launch for the trees of a batch (32 of 24 in
+// one word 2.8 us, 32 chains of 64: 3.9), but the longer part of a step with long ones: eight of 300 tokens in five words, parents
+// within eight 17 us, chains 60; of 1024 in sixteen words 430, chains 1800.
 #include <algorithm>
 
 #include "cache_attn.h"
@@ -47,9 +49,13 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* seq_lens
 // product (2^-8 relative at most, summed in fp32), O once at the end.  Steps before the drafted tokens and inside every row's
 // window have no masks; the others (few) form a row's bits once.
 //
-// Bound by instructions: 8 sequences of 64 drafted tokens over 32768, 32 heads over 8 of 128: 150 us with the join, 521 TFLOP/s (an
-// 8192^3 product 1248); a wave's products (16 of 32 cycles), exponentials and other vector instructions add up to 70 % of its
-// SIMD's cycles.  32 of 24 over 4096: 83 us; 5 of 100 through a window of 1024, head_dim 64: 16.
+// Bound by no one pipe.  8 sequences of up to 64 drafted tokens over up to 32768, 32 heads over 8 of 128: 150 us with the join,
+// 521 TFLOP/s (an 8192^3 product 1248); of the cycles of compute units with work the matrix pipes take 0.29, the vector units 0.42
+// (the issue of products among them), LDS 0.43, and waves wait for 0.35 of theirs, at a step's two barriers, for codes and for LDS.
+// Tiles are not full either: a wave without rows only loads and decodes (82 % of the waves' steps multiply), 74 % of the rows that
+// are multiplied are a sequence's, and a sequence of more than 128 has its tokens decoded twice (1.5 times on average).  32 of up
+// to 24 over up to 4096: 83 us, 54 % of the waves' steps and 41 % of the rows; 5 of 100 through a window of 1024, head_dim 64: 16.
+// (Three registers are spilled at head_dim 128; a variant without was no faster.)
 // Order of N products with two LDS reads each: the reads of three are under way before the first.  (Left to itself the
 // compiler, short of registers, waits for each product's reads.)
 template <int N>

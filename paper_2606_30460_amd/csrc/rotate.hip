@@ -4,7 +4,7 @@
 //
 // and with the sine's sign turned for the inverse, which is the transpose: the gradient of the rotated rows goes back by it.
 // Bound by memory: every row is read and written once (32768 tokens, 32 heads and 8 of 128: 148 us, 4.8 TB/s where a copy reaches
-// 5.0; 1999 tokens of 6 and 2 heads of 64: 4.6 us).  A wave takes one token's rows of all heads (several tokens where it
+// 5.0; with fp32 rows in 189 us, out 216, both 250: 5.3, 4.7, 5.4 TB/s; 1999 tokens of 6 and 2 heads of 64: 4.6 us).  A wave takes one token's rows of all heads (several tokens where it
 // has few), so that a lane forms its unit's cosines and sines, whose rows differ from pair to pair, once for all heads, and
 // has the rows of several heads in flight.
 #include "hsap_internal.h"
