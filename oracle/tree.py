@@ -5,7 +5,8 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
 * A drafted token's mask names itself and those that it follows, directly or not; its position is the number of tokens
   before it on its own path.
 * A row at position p sees the tokens at places j before the drafted ones with p - j < window or j < sinks, and a drafted
-  token at position y that its mask names with p - y < window or y < sinks; a row at a position below 0 sees nothing.
+  token at position y that its mask names with p - y < window or y < sinks; a row at a position below 0 sees nothing.  A
+  window of 2^31 - 1 ends nothing.
 
 Pins: ``tests/test_drafts_oracle.py``.
 """
@@ -50,7 +51,7 @@ def visible(n, count, named, positions, t0, t, window, sinks, capacity):
     inside = drafted & (x < named.shape[1])
     ok[inside] = named[t, x[inside]]
     place = np.where(drafted, positions[t0 + np.clip(x, 0, max(count - 1, 0))], j)
-    return j[ok & ((p - place < window) | (place < sinks))]
+    return j[ok & ((p - place < window) | (place < sinks) | (window == 2 ** 31 - 1))]
 
 
 def attention(q, codes_k, scale_k, codes_v, scale_v, table, lens, cu, named, positions, window: int, sinks: int, scale: float):

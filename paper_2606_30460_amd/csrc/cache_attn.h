@@ -31,6 +31,7 @@ struct CacheAttnArgs {
   const uint64_t* mask;      // TREE kernels: [total_q, words]
   const int32_t* positions;  // TREE kernels: [total_q]
   int32_t words;
+  int32_t furthest;  // TREE kernels: rows behind this position count as at it
 };
 
 // Steps of each split, of `total` steps dealt to `splits` (the last ones may have none).
@@ -106,6 +107,8 @@ __device__ __forceinline__ uint64_t seen_bits(const CacheAttnArgs& a, const RowT
   }
   return pos < 0 ? 0 : m & ~bits_from((int64_t)top + 1 - j0);
 }
+// A row's position.  A window of 2^31 - 1 ends nothing, not even place 0 for a row at 2^31 - 1: it counts as at the position before.
+__device__ __forceinline__ int32_t row_position(const CacheAttnArgs& a, int32_t row) { return min(a.positions[row], a.furthest); }
 // Least and largest position of the rows that see anything (a position below 0 sees nothing): over the lanes that differ in
 // the bits of LANES.
 template <int LANES>

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
     phi = -1;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int32_t p = a.positions[rt.t0 + min(rt.row0 + 16 * mt + l16, last_row) / a.group];
+      const int32_t p = row_position(a, rt.t0 + min(rt.row0 + 16 * mt + l16, last_row) / a.group);
       plo = min(plo, p < 0 ? INT32_MAX : p);
       phi = max(phi, p);
     }
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs a) {
   for (int mt = 0; mt < MT; ++mt) {
     const int32_t r = min(rt.row0 + 16 * mt + l16, nrows - 1);
     const int32_t t = r / a.group;
-    pos[mt] = TREE ? a.positions[rt.t0 + t] : pos0 + t;
+    pos[mt] = TREE ? row_position(a, rt.t0 + t) : pos0 + t;
     const __bf16* qp = a.q + (int64_t)(rt.t0 + t) * a.q_stride + (int64_t)(g * a.group + (r - t * a.group)) * D + 16 * grp;
 #pragma unroll
     for (int x = 0; x < KX; ++x) {
@@ -808,6 +808,7 @@ static hsap_status attend(const char* name, const hsap_cache_desc* desc, const h
   a.mask = mask;
   a.positions = positions;
   a.words = words;
+  a.furthest = window == INT32_MAX ? INT32_MAX - 1 : INT32_MAX;
   const int64_t blocks = c.tiles * c.splits * desc->heads_kv;
   if (blocks > kMaxBlocks256) HSAP_FAIL(HSAP_ERR_INVALID_ARG, "too many rows x heads");
   hipStream_t s = (hipStream_t)hip_stream;

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   int32_t plo = INT32_MAX, phi = -1, least = INT32_MAX;  // positions of the tile's rows
 #pragma unroll
   for (int r = 0; r < ROWS; r += 64) {
-    const int32_t p = a.positions[rt.t0 + min(rt.row0 + r + lane, last_row) / a.group];
+    const int32_t p = row_position(a, rt.t0 + min(rt.row0 + r + lane, last_row) / a.group);
     least = min(least, p);
     plo = min(plo, p < 0 ? INT32_MAX : p);
     phi = max(phi, p);
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_tree_kernel(CacheA
   const int rb = RB == 2 ? w & 1 : w, b0 = RB == 2 ? w >> 1 : 0;
   const bool busy = rt.row0 + 32 * rb <= last_row;
   const int32_t row = min(rt.row0 + 32 * rb + l32, last_row), tok = row / a.group;
-  const int32_t pos = a.positions[rt.t0 + tok];
+  const int32_t pos = row_position(a, rt.t0 + tok);
   const int h = g * a.group + (row - tok * a.group);
 #pragma unroll
   for (int i = 0; i < ROWS * CPR / 256; ++i) {
